@@ -15,6 +15,7 @@
 
 #include "assign_kernels.hpp"
 #include "assign_ordered_kernels.hpp"
+#include "host_common.hpp"
 #include "sweep_kernels.hpp"
 #include "partition_kernels.hpp"
 #include "probe_kernels.hpp"
@@ -88,25 +89,6 @@ struct maaso_ctx {
 
 namespace {
 
-struct DeviceGuard {
-  int prev = -1;
-  bool ok = true;
-  explicit DeviceGuard(int dev) {
-    if (hipGetDevice(&prev) != hipSuccess) { ok = false; (void)hipGetLastError(); return; }
-    if (prev != dev && hipSetDevice(dev) != hipSuccess) { ok = false; (void)hipGetLastError(); }
-  }
-  ~DeviceGuard() {
-    int cur = -1;
-    if (prev >= 0 && hipGetDevice(&cur) == hipSuccess && cur != prev) (void)hipSetDevice(prev);
-  }
-};
-
-inline bool hip_ok(hipError_t e) {
-  if (e == hipSuccess) return true;
-  (void)hipGetLastError();
-  return false;
-}
-
 // Event pair around the dominant kernel of a call, when timing is on and slots are left.
 struct TimedRegion {
   maaso_ctx* ctx;
@@ -123,12 +105,6 @@ struct TimedRegion {
 // Compute calls never allocate: a call whose shape needs more than the context holds is refused.
 int need_workspace(const maaso_ctx* ctx, size_t bytes) {
   return bytes <= ctx->ws_bytes ? MAASO_OK : MAASO_E_WORKSPACE;
-}
-
-bool is_captured(hipStream_t s) {
-  if (s == nullptr) return false;  // (the null stream cannot be)
-  hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
-  return hip_ok(hipStreamIsCapturing(s, &status)) && status != hipStreamCaptureStatusNone;
 }
 
 // Calls that are charged with no workspace, the windowed sweep and the scores, lay requests out at its end, and keep out of what
