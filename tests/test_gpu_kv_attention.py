@@ -1,0 +1,362 @@
+"""Attention over pages against its formula in 64 bits.
+
+What may differ, relative to 64 bits: a score, a sum of head_dim products in 32 bits, by (head_dim + 4) 2^-24 of
+sum |q k| scale (d below); a weight by that, twice, and by half a step of the 16-bit type that it is rounded to; the
+output by half a step of its type.  So |out - ref| <= half |ref| + (half + 2 d + 2^-18) sum w |v|, and where weights are
+fp16 values, whose steps end at 2^-24, keys * 2^-25 of the largest |v|; |lse - ref| <= d + 2^-20 max(1, |ref|)."""
+import math
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+from paper_2509_06362_amd import instance as I  # noqa: E402
+
+BF16, FP16, E4M3 = torch.bfloat16, torch.float16, torch.float8_e4m3fn
+
+
+@pytest.fixture(scope="module")
+def inst():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a GPU (run with -m 'not gpu' on CPU-only machines)")
+    with I.maaso_instance_create() as x:
+        yield x
+
+
+def i32(a):
+    return torch.tensor(np.array(a), dtype=torch.int32, device="cuda")
+
+
+class Batch:
+    """Sequences of `held` + `new` tokens; groups [(first, end, shared)]: shared tokens lie in the same pages."""
+
+    def __init__(self, held, new, heads, kv, dim, page, dtype, cache=None, groups=(), seed=0, layers=1, layer=0, spread=0, q_pad=0, extra_rows=2, gain=1.0):
+        rng, g = np.random.default_rng(seed), torch.Generator().manual_seed(seed)
+        self.held, self.new, self.heads, self.kv, self.dim, self.page, self.dtype, self.layer = held, new, heads, kv, dim, page, dtype, layer
+        self.cache, self.groups, n = cache or dtype, groups, len(held)
+        self.total = [h + w for h, w in zip(held, new)]
+        need = [-(-t // page) for t in self.total]
+        width, pool = max(need + [1]) + 1, sum(need) + 4
+        ids, at = rng.permutation(pool), 0
+        table = np.full((n, width), -1, np.int32)
+        for i, m in enumerate(need):
+            table[i, :m] = ids[at:at + m]
+            at += m
+        for f, e, shared in groups:  # whole pages are the same; of a partly shared page each has a copy
+            whole = shared // page
+            for i in range(f + 1, e):
+                table[i, :whole] = table[f, :whole]
+        self.rows = rng.permutation(n + extra_rows)[:n]
+        placed, length = np.full((n + extra_rows, width), -1, np.int32), np.zeros(n + extra_rows, np.int32)
+        placed[self.rows], length[self.rows] = table, self.total
+        self.table_host = table
+        stride = kv * page * dim + spread
+        shape_k, shape_v = (layers, pool, kv, page, dim), (layers, pool, kv, dim, page)
+        flat = [torch.full((layers * pool * stride,), math.nan, device="cuda").to(self.cache) for _ in range(2)]
+        views = [f.as_strided(s, (pool * stride, stride, s[3] * s[4], s[4], 1)) for f, s in zip(flat, (shape_k, shape_v))]
+        self.k, self.v = views
+        # what is held is written; everything else stays NaN
+        self.ks, self.vs = (torch.rand(2, kv, generator=g) + 0.5) if self.cache == E4M3 else torch.ones(2, kv)
+        self.K, self.V = [], []
+        for i, t in enumerate(self.total):
+            kk, vv = (gain * torch.randn(t, kv, dim, generator=g)).to(self.cache), torch.randn(t, kv, dim, generator=g).to(self.cache)
+            for f, e, shared in groups:
+                if f < i < e:
+                    kk, vv = kk.float(), vv.float()
+                    kk[:shared], vv[:shared] = self.K[f][:shared].float(), self.V[f][:shared].float()
+                    kk, vv = kk.to(self.cache), vv.to(self.cache)
+            self.K.append(kk)
+            self.V.append(vv)
+            self.write(i)
+        tokens = sum(new)
+        q = torch.randn(tokens, heads * dim + q_pad, generator=g).to(dtype)
+        self.q_host = q[:, :heads * dim].unflatten(1, (heads, dim))
+        self.q = q.cuda()[:, :heads * dim].unflatten(1, (heads, dim))
+        self.refs, self.table, self.length = i32(np.zeros(pool)), i32(placed), i32(length)
+        self.pages = I.KvPages(self.refs, self.table, self.length, page)
+        scales = (self.ks.cuda(), self.vs.cuda()) if self.cache == E4M3 else (None, None)
+        self.view = I.KvCache(self.k, self.v, *scales)
+        self.q_start = i32(np.concatenate([[0], np.cumsum(new)]))
+        self.out = torch.full((tokens, heads * dim + q_pad), 9.0, dtype=dtype, device="cuda")[:, :heads * dim].unflatten(1, (heads, dim))
+        self.lse = torch.full((tokens, heads), 9.0, device="cuda")
+        self.scale = dim ** -0.5
+
+    def write(self, i):
+        t = self.total[i]
+        if t == 0:
+            return
+        at = torch.arange(t)
+        page, place = torch.tensor(self.table_host[i])[at // self.page].long().cuda(), (at % self.page).cuda()
+        raw = (lambda x: x.view(torch.uint8)) if self.cache == E4M3 else (lambda x: x)
+        raw(self.k[self.layer])[page, :, place] = raw(self.K[i].cuda())
+        raw(self.v[self.layer])[page, :, :, place] = raw(self.V[i].cuda())
+
+    def run(self, inst, **over):
+        g = self.groups
+        args = dict(layer=self.layer, q=self.q, out=self.out, lse=self.lse, q_start=self.q_start, rows=i32(self.rows), scale=self.scale,
+                    max_q=max(self.new), max_len=max(self.total), total_len=sum(self.total))
+        if g:
+            bounds = []
+            for f, e, _ in g:
+                bounds.append(f)
+            args.update(group_start=i32(bounds + [g[-1][1]]), shared=i32([s for _, _, s in g]), max_shared=max(s for _, _, s in g))
+        args.update(over)
+        I.maaso_kv_attention(inst, self.view, self.pages, **args)
+        return self
+
+    def check(self, which=None):
+        half, at, group = torch.finfo(self.dtype).eps / 2, 0, self.heads // self.kv
+        for i, (h, w) in enumerate(zip(self.held, self.new)):
+            q = self.q_host[at:at + w].double().cuda()
+            out, lse = self.out[at:at + w].double(), self.lse[at:at + w].double()
+            at += w
+            if w == 0 or (which is not None and i not in which):
+                continue
+            K = (self.K[i].float() * self.ks[:, None]).double().cuda().repeat_interleave(group, 1)
+            V = (self.V[i].float() * self.vs[:, None]).double().cuda().repeat_interleave(group, 1)
+            t = h + w
+            s = torch.einsum("qhd,khd->qhk", q, K) * self.scale
+            d = torch.einsum("qhd,khd->qhk", q.abs(), K.abs()).amax(-1) * abs(self.scale) * (self.dim + 4) * 2.0 ** -24 if t else torch.zeros_like(lse)
+            sees = torch.arange(t, device="cuda") <= (h + torch.arange(w, device="cuda"))[:, None]
+            s = s.masked_fill(~sees[:, None], -math.inf)
+            ref_lse = torch.logsumexp(s, -1) if t else torch.full_like(lse, -math.inf)
+            p = torch.exp(s - torch.where(ref_lse == -math.inf, 0.0, ref_lse)[..., None])
+            Vs = V.masked_fill(~sees.any(0)[:, None, None], 0.0) if t else V
+            ref = torch.stack([torch.einsum("hk,khd->hd", p[j][:, :max(0, h + j + 1)], Vs[:max(0, h + j + 1)]) for j in range(w)])
+            mean = torch.stack([torch.einsum("hk,khd->hd", p[j][:, :max(0, h + j + 1)], Vs[:max(0, h + j + 1)].abs()) for j in range(w)])
+            tol = half * ref.abs() + (half + 2 * d[..., None] + 2.0 ** -18) * mean + 1e-30
+            if self.dtype == FP16 and t:
+                tol = tol + (t + 1) * 2.0 ** -25 * Vs.nan_to_num(0, 0, 0).abs().amax()
+            nan = ref.isnan()
+            assert torch.equal(nan, out.isnan()), (i, "NaN elsewhere")
+            bad = ((out - ref).abs() > tol) & ~nan & (out != ref)
+            assert not bad.any(), (i, float((out - ref).abs().max()), float(tol.min()))
+            off = (lse - ref_lse).abs()
+            assert bool(((lse == ref_lse) | (off <= d + 2.0 ** -20 * ref_lse.abs().clamp(min=1)) | ref_lse.isnan()).all()), (i, "lse")
+
+
+SIZES = [  # heads, key heads, head dim, page
+    (1, 1, 64, 16), (8, 8, 64, 32), (6, 2, 128, 64), (7, 1, 128, 16), (16, 1, 64, 128), (5, 5, 256, 64), (8, 2, 256, 16), (24, 1, 128, 32), (40, 2, 64, 64)]
+
+
+@pytest.mark.parametrize("dtype, cache", [(BF16, BF16), (FP16, FP16), (BF16, E4M3), (FP16, E4M3)])
+@pytest.mark.parametrize("heads, kv, dim, page", SIZES)
+def test_single_tokens(inst, dtype, cache, heads, kv, dim, page):
+    held = [0, 1, 14, 15, 16, 31, 32, 33, 62, 63, 64, 127, 200, 511, 700, 1300]
+    Batch(held, [1] * len(held), heads, kv, dim, page, dtype, cache).run(inst).check()
+    assert I.maaso_instance_status(inst) == 0
+
+
+@pytest.mark.parametrize("dtype, cache", [(BF16, BF16), (FP16, FP16), (BF16, E4M3)])
+@pytest.mark.parametrize("heads, kv, dim, page", SIZES)
+def test_several_new_tokens(inst, dtype, cache, heads, kv, dim, page):
+    held, new = [0, 5, 0, 64, 200, 17, 0, 31, 300], [1, 2, 3, 64, 5, 0, 130, 33, 257]
+    Batch(held, new, heads, kv, dim, page, dtype, cache).run(inst).check()
+    assert I.maaso_instance_status(inst) == 0
+
+
+@pytest.mark.parametrize("dtype, cache", [(BF16, BF16), (FP16, FP16), (FP16, E4M3)])
+@pytest.mark.parametrize("heads, kv, dim, page", SIZES)
+@pytest.mark.parametrize("shared", [16, 100, 640])
+def test_a_shared_beginning(inst, dtype, cache, heads, kv, dim, page, shared):
+    own = [0, 1, 30, 31, 32, 100, 7, 64, 255, 12, 3]
+    n = len(own)
+    b = Batch([shared + h for h in own], [1] * n, heads, kv, dim, page, dtype, cache, groups=[(0, n, shared)])
+    b.run(inst).check()
+    assert I.maaso_instance_status(inst) == 0
+
+
+@pytest.mark.parametrize("heads, kv, dim, page", [(8, 2, 128, 32), (4, 4, 64, 16), (2, 1, 256, 64)])
+def test_groups_and_sequences_outside(inst, heads, kv, dim, page):
+    """Groups from sequence 2 on, one of a single sequence, one that shares nothing; several new tokens."""
+    held = [50, 0, 200, 260, 201, 333, 40, 41, 64, 90, 70, 500]
+    new = [1, 4, 3, 1, 7, 2, 1, 0, 5, 1, 1, 20]
+    Batch(held, new, heads, kv, dim, page, BF16, groups=[(2, 6, 200), (6, 7, 33), (7, 9, 0), (9, 11, 64)]).run(inst).check()
+    assert I.maaso_instance_status(inst) == 0
+
+
+@pytest.mark.parametrize("n", [1, 3, 70, 200])
+def test_many_groups(inst, n):
+    groups = [(i, i + 1, 17 + i % 5) for i in range(n)] if n < 70 else [(2 * i, 2 * i + 2, 16 * (i % 4)) for i in range(n // 2)]
+    held = [80 + i % 7 for i in range(n)]
+    Batch(held, [1 + i % 2 for i in range(n)], 4, 2, 64, 16, FP16, groups=groups).run(inst).check()
+    assert I.maaso_instance_status(inst) == 0
+
+
+@pytest.mark.parametrize("dtype, cache", [(BF16, BF16), (FP16, E4M3)])
+@pytest.mark.parametrize("tokens", [9000, 70001])
+def test_long_rows_in_parts(inst, dtype, cache, tokens):
+    Batch([tokens], [1], 8, 2, 128, 64, dtype, cache).run(inst).check()
+    Batch([tokens, 3, tokens // 3], [3, 1, 1], 4, 4, 64, 16, dtype, cache).run(inst).check()
+    Batch([tokens, tokens + 700, tokens], [1, 1, 2], 4, 1, 64, 32, dtype, cache, groups=[(0, 3, tokens - 5)]).run(inst).check()
+
+
+def test_more_queries_than_the_row_holds(inst):
+    """The first queries of a row with fewer tokens than queries see nothing: zeros, and minus infinity."""
+    b = Batch([-3, -1, 0], [5, 1, 2], 4, 2, 64, 16, BF16)
+    b.run(inst).check()
+    assert (b.out[:3] == 0).all() and (b.lse[:3] == -math.inf).all() and (b.out[5] == 0).all() and (b.lse[5] == -math.inf).all()
+
+
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("heads, dim", [(2, 64), (8, 128)])
+def test_what_a_query_does_not_see_has_no_part(inst, value, dtype, heads, dim):
+    """Keys and values that are not finite, visible to the later queries of a sequence only: the earlier ones as without."""
+    b = Batch([37, 0, 100], [12, 40, 150], heads, 2, dim, 32, dtype)
+    for i, at in ((0, 44), (1, 17), (2, 200)):
+        b.V[i][at, 1, 3] = value
+        b.write(i)
+    b.run(inst).check()
+    for i, at in ((0, 44), (1, 17), (2, 200)):
+        b.K[i][at, 0, 5] = value
+        b.write(i)
+    b.run(inst)
+    first = 0
+    for i, (h, w) in enumerate(zip(b.held, b.new)):
+        at = (44, 17, 200)[i]
+        seen = at - h  # queries before this one do not see it
+        out = b.out[first:first + w].float()
+        assert out[:seen].isfinite().all() and b.lse[first:first + seen].isfinite().all()
+        first += w
+
+
+def test_weights_of_one_key_alone(inst):
+    """Scores so far apart that one key has all the weight, large and small ones among them."""
+    Batch([300, 40], [1, 9], 4, 2, 128, 16, BF16, gain=60.0).run(inst).check()
+    Batch([300, 40], [1, 9], 4, 2, 128, 16, FP16, gain=60.0).run(inst).check()
+    Batch([300, 40], [1, 9], 4, 2, 64, 16, FP16, gain=1e-6).run(inst).check()
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.3, 5.0])
+def test_scales(inst, scale):
+    b = Batch([90, 3], [1, 20], 4, 2, 64, 16, BF16)
+    b.scale = scale
+    b.run(inst).check()
+
+
+def test_strides_layers_and_rows_as_they_are(inst):
+    Batch([90, 3, 77], [1, 20, 2], 4, 2, 64, 16, BF16, layers=3, layer=2, spread=8 * 24, q_pad=40).run(inst).check()
+    b = Batch([90, 3, 77], [1, 20, 2], 4, 2, 64, 16, FP16, extra_rows=0)
+    b.table.copy_(b.table[torch.tensor(b.rows).cuda()].clone())
+    b.length.copy_(b.length[torch.tensor(b.rows).cuda()].clone())
+    b.run(inst, rows=None).check()
+
+
+def test_without_the_logarithm_of_the_sum_and_without_a_length(inst):
+    b = Batch([90, 3, 2000], [1, 20, 2], 4, 2, 64, 16, BF16).run(inst)
+    want = b.out.clone()
+    b.out.fill_(9.0)
+    b.run(inst, lse=None)
+    assert torch.equal(b.out, want)
+    b.run(inst, total_len=0).check()
+    b.run(inst, max_len=b.page * b.table.shape[1] - 1).check()
+
+
+def test_a_pool_beyond_32_bits(inst):
+    """Pages 2^28 elements apart: offsets of 12 GiB."""
+    b = Batch([60, 33], [1, 2], 2, 1, 64, 16, BF16)
+    pool, stride = b.k.shape[1], 1 << 28
+    k = torch.empty(pool * stride, dtype=BF16, device="cuda").as_strided(b.k.shape, (pool * stride, stride, 16 * 64, 64, 1))
+    v = torch.empty(pool * stride, dtype=BF16, device="cuda").as_strided(b.v.shape, (pool * stride, stride, 16 * 64, 16, 1))
+    k.copy_(b.k)
+    v.copy_(b.v)
+    b.k, b.v, b.view = k, v, I.KvCache(k, v)
+    b.run(inst).check()
+    pairs = i32([[int(b.table_host[0, 0]), pool - 1]]) if int(b.table_host[0, 0]) != pool - 1 else i32([[pool - 1, 0]])
+    src, dst = pairs[0].tolist()
+    I.maaso_kv_copy(inst, b.view, pairs=pairs)
+    assert torch.equal(k[0, dst].nan_to_num(7), k[0, src].nan_to_num(7)) and torch.equal(v[0, dst].nan_to_num(7), v[0, src].nan_to_num(7))
+
+
+def test_the_same_bits_every_time(inst):
+    b = Batch([3000, 900, 3100], [1, 1, 3], 8, 2, 128, 64, BF16, groups=[(0, 3, 850)]).run(inst)
+    out, lse = b.out.clone(), b.lse.clone()
+    for _ in range(3):
+        b.out.fill_(9.0)
+        b.run(inst)
+        assert torch.equal(b.out, out) and torch.equal(b.lse, lse)
+
+
+def test_another_stream_and_a_graph(inst):
+    b = Batch([3000, 40], [1, 2], 4, 2, 64, 16, FP16, groups=[(0, 2, 32)])
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    b.run(inst, stream=s)
+    torch.cuda.current_stream().wait_stream(s)
+    b.check()
+    want = b.out.clone()
+    rows, shared, start = i32(b.rows), i32([32]), i32([0, 2])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        I.maaso_kv_attention(inst, b.view, b.pages, layer=0, q=b.q, out=b.out, lse=b.lse, q_start=b.q_start, rows=rows, group_start=start, shared=shared,
+                             scale=b.scale, max_q=2, max_len=3001, max_shared=32, total_len=3043)
+    for _ in range(3):
+        b.out.fill_(9.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(b.out, want)
+        b.run(inst).check()
+
+
+def test_a_small_workspace_takes_fewer_parts_or_refuses(inst):
+    b = Batch([9000], [1], 8, 2, 128, 64, BF16)
+    for size in (1 << 12, 1 << 15, 1 << 17):
+        with I.maaso_instance_create(workspace_bytes=size) as small:
+            b.out.fill_(9.0)
+            b.run(small).check()
+    b = Batch([300, 200], [1, 1], 8, 2, 128, 64, BF16, groups=[(0, 2, 128)])
+    with I.maaso_instance_create(workspace_bytes=1 << 12) as small:
+        with pytest.raises(I.MaasoError) as e:
+            b.run(small)
+        assert e.value.status == -7
+
+
+def test_bad_entries_are_not_followed(inst):
+    b = Batch([100, 70], [1, 1], 4, 2, 64, 16, BF16)
+    good = b.table.clone()
+    for entry in (-1, b.k.shape[1], 2 ** 31 - 1):
+        b.table.copy_(good)
+        b.table[int(b.rows[0]), 2] = entry
+        b.run(inst)
+        assert I.maaso_instance_status(inst) == I.BAD_PAGE
+        b.check(which=[1])
+        assert b.out[0].isfinite().all()
+    b.table.copy_(good)
+    rows = b.rows.copy()
+    for bad in (-1, b.table.shape[0]):
+        b.rows = np.array([rows[0], bad])
+        b.run(inst)
+        assert I.maaso_instance_status(inst) == I.BAD_ROW
+        b.check(which=[0])
+        assert (b.out[1] == 0).all()
+    b.rows = rows
+    b.length[int(rows[1])] = -1
+    b.run(inst)
+    assert I.maaso_instance_status(inst) == I.BAD_ROW
+    b.length[int(rows[1])] = 16 * b.table.shape[1] + 1
+    b.run(inst)
+    assert I.maaso_instance_status(inst) == I.BAD_ROW
+    b.check(which=[0])
+
+
+@pytest.mark.parametrize("over", [dict(max_len=90), dict(max_q=1), dict(q_start=[0, 4, 3]), dict(q_start=[0, 1, 9]), dict(q_start=[-1, 1, 3])])
+def test_bounds_that_do_not_hold(inst, over):
+    b = Batch([100, 70], [1, 2], 4, 2, 64, 16, BF16)
+    over = {k: i32(v) if isinstance(v, list) else v for k, v in over.items()}
+    b.run(inst, **over)
+    assert I.maaso_instance_status(inst) & I.BAD_BOUND
+
+
+@pytest.mark.parametrize("over", [dict(shared=[200]), dict(max_shared=32), dict(group_start=[0, 9]), dict(group_start=[-1, 2]), dict(group_start=[2, 0])])
+def test_groups_that_do_not_hold(inst, over):
+    b = Batch([100, 70], [1, 2], 4, 2, 64, 16, BF16, groups=[(0, 2, 64)])
+    over = {k: i32(v) if isinstance(v, list) else v for k, v in over.items()}
+    if "shared" in over:
+        over["max_shared"] = 200
+        over["max_len"] = 300
+    b.run(inst, **over)
+    assert I.maaso_instance_status(inst) & I.BAD_BOUND

@@ -1,0 +1,324 @@
+"""The pages of a cache against a model in Python, exactly: growing, forking, trimming, compacting, copying."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+from paper_2509_06362_amd import instance as I  # noqa: E402
+
+
+@pytest.fixture(scope="module")
+def inst():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a GPU (run with -m 'not gpu' on CPU-only machines)")
+    with I.maaso_instance_create() as x:
+        yield x
+
+
+def dev(a, dtype=torch.int32):
+    return torch.tensor(np.array(a), dtype=dtype, device="cuda")
+
+
+class Model:
+    """The definition, one page at a time."""
+
+    def __init__(self, n_pages, page, n_rows, width):
+        self.page, self.width = page, width
+        self.refs = np.zeros(n_pages, np.int32)
+        self.table = np.full((n_rows, width), -1, np.int32)
+        self.length = np.zeros(n_rows, np.int32)
+
+    def held(self, tokens):
+        return -(-int(tokens) // self.page)
+
+    def extend(self, rows, new):
+        free = [int(p) for p in np.nonzero(self.refs == 0)[0]]
+        before, plan, copies = self.refs.copy(), [], []
+        for r, n in zip(rows, new):
+            had, has = self.held(self.length[r]), self.held(self.length[r] + n)
+            last = int(self.table[r, had - 1]) if self.length[r] % self.page and n else -1
+            shared = last >= 0 and before[last] > 1
+            if has > self.width:
+                return None
+            plan.append((r, n, had - shared, has, last if shared else -1))
+        if sum(has - first for _, _, first, has, _ in plan) > len(free):
+            return None
+        slot, pos = [], []
+        for r, n, first, has, last in plan:
+            ids, free = free[:has - first], free[has - first:]
+            self.table[r, first:has] = ids
+            self.refs[ids] = 1
+            copies.append((last, ids[0]) if last >= 0 else (-1, -1))
+            if last >= 0:
+                self.refs[last] -= 1
+            for p in range(self.length[r], self.length[r] + n):
+                pos.append(p)
+                slot.append(int(self.table[r, p // self.page]) * self.page + p % self.page)
+            self.length[r] += n
+        return slot, pos, copies
+
+    def fork(self, parents, children):
+        for p, c in zip(parents, children):
+            n = self.held(self.length[p])
+            self.table[c, :n] = self.table[p, :n]
+            self.refs[self.table[p, :n]] += 1
+            self.length[c] = self.length[p]
+
+    def trim(self, rows, keep):
+        for r, k in zip(rows, keep):
+            if k < self.length[r]:
+                a, b = self.held(k), self.held(self.length[r])
+                np.subtract.at(self.refs, self.table[r, a:b], 1)
+                self.table[r, a:b] = -1
+                self.length[r] = k
+
+    def compact(self):
+        live = np.nonzero(self.refs > 0)[0]
+        n = len(live)
+        holes = [p for p in range(n) if self.refs[p] == 0]
+        goes = np.arange(len(self.refs))
+        moves = np.full((len(self.refs) // 2, 2), -1, np.int32)
+        for k, (p, to) in enumerate(zip([p for p in live if p >= n], holes)):
+            goes[p] = to
+            moves[k] = p, to
+        refs = np.zeros_like(self.refs)
+        refs[goes[live]] = self.refs[live]
+        self.refs, self.table = refs, np.where(self.table >= 0, goes[self.table], -1).astype(np.int32)
+        return moves, n
+
+
+class Both:
+    def __init__(self, inst, *size):
+        self.m, self.inst = Model(*size), inst
+        n_pages, page, n_rows, width = size
+        self.refs = torch.zeros(n_pages, dtype=torch.int32, device="cuda")
+        self.table = torch.full((n_rows, width), -1, dtype=torch.int32, device="cuda")
+        self.length = torch.zeros(n_rows, dtype=torch.int32, device="cuda")
+        self.pages = I.KvPages(self.refs, self.table, self.length, page)
+
+    def same(self):
+        assert np.array_equal(self.refs.cpu().numpy(), self.m.refs)
+        assert np.array_equal(self.table.cpu().numpy(), self.m.table)
+        assert np.array_equal(self.length.cpu().numpy(), self.m.length)
+
+    def extend(self, rows, new, status=0):
+        tokens = int(sum(new))
+        slot, pos = torch.full((tokens,), 7, dtype=torch.int64, device="cuda"), torch.full((tokens,), 7, dtype=torch.int32, device="cuda")
+        copies = torch.full((len(rows), 2), 7, dtype=torch.int32, device="cuda")
+        I.maaso_kv_extend(self.inst, self.pages, rows=dev(rows), q_start=dev(np.concatenate([[0], np.cumsum(new)])), slot=slot, pos=pos, copies=copies)
+        assert I.maaso_instance_status(self.inst) == status
+        want = self.m.extend(rows, new) if not status else None
+        if want is None:
+            assert status and (slot == -1).all() and (pos == -1).all() and (copies == -1).all()
+        else:
+            assert slot.tolist() == want[0] and pos.tolist() == want[1] and [tuple(x) for x in copies.tolist()] == want[2]
+        self.same()
+        return copies
+
+    def fork(self, parents, children):
+        I.maaso_kv_fork(self.inst, self.pages, parents=dev(parents), children=dev(children))
+        self.m.fork(parents, children)
+        self.same()
+
+    def trim(self, rows, keep):
+        I.maaso_kv_trim(self.inst, self.pages, rows=dev(rows), keep=dev(keep))
+        self.m.trim(rows, keep)
+        self.same()
+
+    def compact(self, in_place):
+        n = len(self.m.refs)
+        refs, table = (self.refs, self.table) if in_place else (torch.empty_like(self.refs), torch.empty_like(self.table))
+        moves, live = torch.full((n // 2, 2), 7, dtype=torch.int32, device="cuda"), dev([7])
+        I.maaso_kv_compact(self.inst, self.pages, refs_out=refs, table_out=table, moves=moves, n_live=live)
+        want, n_live = self.m.compact()
+        assert np.array_equal(moves.cpu().numpy(), want) and int(live) == n_live
+        if not in_place:
+            self.refs.copy_(refs)
+            self.table.copy_(table)
+        self.same()
+        return moves
+
+
+@pytest.mark.parametrize("page", [16, 32, 64, 128])
+@pytest.mark.parametrize("n_pages, n_rows, width, seed", [(37, 9, 6, 0), (1000, 70, 11, 1), (4099, 130, 33, 2), (9001, 1500, 6, 3)])
+def test_a_life_of_a_pool(inst, page, n_pages, n_rows, width, seed):
+    rng = np.random.default_rng(seed)
+    b = Both(inst, n_pages, page, n_rows, width)
+    for step in range(12):
+        empty, full = np.nonzero(b.m.length == 0)[0], np.nonzero(b.m.length > 0)[0]
+        if len(empty) > 1 and len(full):
+            n = min(len(empty), 1 + step)
+            b.fork(rng.choice(full, n), rng.permutation(empty)[:n])
+        rows = rng.permutation(n_rows)[:max(1, n_rows - step)]
+        new = rng.integers(0, 2 * page + 3 if step < 2 else 4, len(rows))
+        before = b.m.refs.copy(), b.m.table.copy(), b.m.length.copy()
+        if b.m.extend(rows, new) is None:
+            status = I.NO_PAGES
+        else:
+            status = 0
+            b.m.refs, b.m.table, b.m.length = before
+        b.extend(rows, new, status)
+        rows = rng.permutation(n_rows)[:n_rows // 2 + 1]
+        b.trim(rows, rng.integers(0, np.maximum(1, b.m.length[rows] + 2)) * rng.integers(0, 2, len(rows)))
+        if step % 3 == 2:
+            b.compact(in_place=step % 2 == 0)
+    assert I.maaso_instance_status(inst) == 0
+
+
+def test_many_tokens_in_one_call(inst):
+    b = Both(inst, 2000, 16, 40, 400)
+    b.extend(np.arange(40)[::-1], np.arange(40) * 20)     # 15,600 tokens: more than one block's
+    b.extend(np.arange(40), np.full(40, 110))
+    b.trim(np.arange(40), np.zeros(40, int))
+    assert not b.m.refs.any()
+
+
+def test_one_token_at_a_time(inst):
+    b = Both(inst, 5, 16, 2, 3)
+    for _ in range(33):
+        b.extend([1], [1])
+    b.extend([0], [16])
+    b.extend([0], [0])
+    b.extend([0], [17], I.NO_PAGES)      # two pages, one is free
+    b.extend([1], [16], I.NO_PAGES)      # the row has three
+    b.extend([1, 0], [1, 16])
+
+
+def test_all_holders_of_a_page_grow_at_once(inst):
+    b = Both(inst, 20, 32, 5, 4)
+    b.extend([0], [40])
+    b.fork([0, 0, 0], [1, 2, 4])
+    copies = b.extend([4, 0, 1, 2], [1, 1, 2, 40])
+    assert (copies[:, 0] == 1).all() and b.m.refs[1] == 0 and b.m.refs[0] == 4
+    b.extend([0, 4], [1, 1])             # their own by now
+
+
+def test_a_whole_last_page_is_shared_on(inst):
+    b = Both(inst, 20, 32, 3, 4)
+    b.extend([0], [64])
+    b.fork([0], [2])
+    copies = b.extend([2, 0], [1, 0])
+    assert (copies == -1).all() and list(b.m.refs[:3]) == [2, 2, 1]
+
+
+@pytest.mark.parametrize("rows, q_start, bit", [
+    ([3], [0, 1], I.BAD_ROW), ([-1], [0, 1], I.BAD_ROW), ([0], [0, 2], I.BAD_BOUND), ([0], [1, 1], I.BAD_BOUND), ([0], [0, 0], I.BAD_BOUND),
+    ([0, 1], [0, 2, 1], I.BAD_BOUND), ([0, 1], [0, -1, 1], I.BAD_BOUND)])
+def test_extend_refuses(inst, rows, q_start, bit):
+    b = Both(inst, 20, 32, 3, 4)
+    b.extend([0, 1, 2], [5, 0, 64])
+    slot, pos, copies = torch.zeros(1, dtype=torch.int64, device="cuda"), dev([0]), dev([[0, 0]] * len(rows))
+    I.maaso_kv_extend(inst, b.pages, rows=dev(rows), q_start=dev(q_start), slot=slot, pos=pos, copies=copies)
+    assert I.maaso_instance_status(inst) == bit
+    assert int(slot) == -1 and int(pos) == -1 and (copies == -1).all()
+    b.same()
+
+
+def test_extend_refuses_what_the_table_holds_wrongly(inst):
+    b = Both(inst, 20, 32, 3, 4)
+    b.extend([0], [5])
+    for length, entry, bit in ((5, 20, I.BAD_PAGE), (5, -1, I.BAD_PAGE), (-1, 0, I.BAD_ROW), (129, 0, I.BAD_ROW)):
+        b.length[0], b.table[0, 0] = length, entry
+        slot, copies = torch.zeros(1, dtype=torch.int64, device="cuda"), dev([[0, 0]])
+        I.maaso_kv_extend(inst, b.pages, rows=dev([0]), q_start=dev([0, 1]), slot=slot, copies=copies)
+        assert I.maaso_instance_status(inst) == bit and int(slot) == -1
+
+
+def test_fork_and_trim_leave_bad_rows_alone(inst):
+    b = Both(inst, 20, 32, 4, 4)
+    b.extend([0, 1], [40, 3])
+    for parents, children in (([0], [1]), ([0], [4]), ([-1], [2]), ([0], [-2])):
+        I.maaso_kv_fork(inst, b.pages, parents=dev(parents), children=dev(children))
+        assert I.maaso_instance_status(inst) == I.BAD_ROW
+        b.same()
+    for rows, keep in (([4], [0]), ([-1], [0]), ([0], [-1])):
+        I.maaso_kv_trim(inst, b.pages, rows=dev(rows), keep=dev(keep))
+        assert I.maaso_instance_status(inst) == I.BAD_ROW
+        b.same()
+    b.trim([0, 1, 2], [40, 100, 0])      # nothing to give back
+    assert I.maaso_instance_status(inst) == 0
+
+
+def test_trim_gives_back_only_what_is_held(inst):
+    b = Both(inst, 20, 32, 2, 4)
+    b.extend([0], [100])
+    b.table[0, 1], b.table[0, 2] = 20, -1
+    b.refs[0] = 0
+    I.maaso_kv_trim(inst, b.pages, rows=dev([0]), keep=dev([0]))
+    assert I.maaso_instance_status(inst) == I.BAD_PAGE
+    assert b.refs.tolist() == [0, 1, 1, 0] + [0] * 16 and (b.table == -1).all() and int(b.length[0]) == 0
+
+
+@pytest.mark.parametrize("n_pages, live", [(1, [0]), (1, []), (2, [1]), (5, []), (5, [0, 1, 2, 3, 4]), (4097, [4096]), (12289, list(range(1, 12289, 2)))])
+def test_compact_ends(inst, n_pages, live):
+    b = Both(inst, n_pages, 16, 2, max(1, len(live)))
+    b.m.refs[live] = 1
+    b.m.table[1, :len(live)] = live
+    b.m.length[1] = 16 * len(live)
+    b.refs.copy_(dev(b.m.refs))
+    b.table.copy_(dev(b.m.table))
+    b.length.copy_(dev(b.m.length))
+    b.compact(in_place=False)
+    b.compact(in_place=True)
+    assert I.maaso_instance_status(inst) == 0
+
+
+def test_compact_does_not_follow_bad_entries(inst):
+    b = Both(inst, 10, 16, 2, 4)
+    b.refs[7] = 1
+    b.table[0] = dev([7, 10, 3, -5])
+    refs, table, moves, live = torch.empty_like(b.refs), torch.empty_like(b.table), dev([[0, 0]] * 5), dev([0])
+    I.maaso_kv_compact(inst, b.pages, refs_out=refs, table_out=table, moves=moves, n_live=live)
+    assert I.maaso_instance_status(inst) == I.BAD_PAGE
+    assert table[0].tolist() == [0, -1, -1, -1] and refs.tolist() == [1] + [0] * 9 and moves[0].tolist() == [7, 0] and int(live) == 1
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float8_e4m3fn])
+@pytest.mark.parametrize("layers, heads, page, dim", [(1, 1, 16, 64), (3, 5, 32, 128), (2, 2, 128, 256)])
+def test_copy(inst, dtype, layers, heads, page, dim):
+    g = torch.Generator(device="cuda").manual_seed(1)
+    raw = torch.randint(0, 256, (2, layers, 9, heads * page * dim * dtype.itemsize), dtype=torch.uint8, device="cuda", generator=g)
+    k, v = raw[0].view(dtype).view(layers, 9, heads, page, dim), raw[1].view(dtype).view(layers, 9, heads, dim, page)
+    want = raw.clone()
+    pairs = [(3, 1), (-1, 4), (8, 0), (2, -1), (8, 5)]
+    for a, b in pairs:
+        if a >= 0 and b >= 0:
+            want[:, :, b] = raw[:, :, a]
+    I.maaso_kv_copy(inst, I.KvCache(k, v), pairs=dev(pairs))
+    assert torch.equal(raw, want)
+    I.maaso_kv_copy(inst, I.KvCache(k, v), pairs=dev([(9, 1), (1, 9)]))
+    assert I.maaso_instance_status(inst) == I.BAD_PAGE and torch.equal(raw, want)
+
+
+def test_copy_keeps_to_strided_pages(inst):
+    big = torch.randn(2, 2, 6, 3, 2, 16 * 64, device="cuda").half()  # [k and v, layers, pages, gap, heads, ...]
+    want = big.clone()
+    want[:, :, 4, 0] = big[:, :, 2, 0]
+    k, v = big[0][:, :, 0].unflatten(-1, (16, 64)), big[1][:, :, 0].unflatten(-1, (64, 16))
+    I.maaso_kv_copy(inst, I.KvCache(k, v), pairs=dev([(2, 4)]))
+    assert torch.equal(big, want)
+
+
+def test_captured_calls_replay(inst):
+    b = Both(inst, 50, 16, 4, 8)
+    b.extend([0, 1], [20, 7])
+    rows, start, keep = dev([1, 0]), dev([0, 3, 4]), dev([7, 20])
+    slot, pos, copies = torch.zeros(4, dtype=torch.int64, device="cuda"), dev([0] * 4), dev([[0, 0]] * 2)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        I.maaso_kv_extend(inst, b.pages, rows=rows, q_start=start, slot=slot, pos=pos, copies=copies)
+        I.maaso_kv_trim(inst, b.pages, rows=rows, keep=keep)
+    b.same()
+    for _ in range(3):
+        slot.fill_(-9)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert slot.tolist() == [2 * 16 + 7, 2 * 16 + 8, 2 * 16 + 9, 1 * 16 + 4] and pos.tolist() == [7, 8, 9, 20]
+        b.same()
+        b.extend([2], [17])
+        b.trim([2], [0])
+    assert I.maaso_instance_status(inst) == 0
