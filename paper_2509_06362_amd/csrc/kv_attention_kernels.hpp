@@ -23,7 +23,7 @@
 namespace maaso {
 
 constexpr float kLn2 = 0.693147180559945309f;
-constexpr uint32_t kStreamRows = 16;  // rows of an item
+constexpr uint32_t kStreamRows = 16;  // most rows of an item that one wave's registers take; more are taken in tiles
 constexpr uint32_t kStreamKeys = 32;  // keys of a wave's step
 
 struct AttentionArgs {
@@ -47,8 +47,8 @@ struct AttentionArgs {
   uint32_t max_q, max_len, max_shared;
   uint32_t own_chunk, shared_chunk;    // keys of a part, multiples of kStreamKeys
   uint32_t own_parts, shared_parts;    // most parts of a row
-  uint32_t own_tiles, shared_tiles;    // most tiles of rows
-  uint32_t shared_blocks;              // blocks that take shared parts; those behind them take own ones
+  uint32_t own_tiles, shared_tiles;    // most tiles of kTileRows rows
+  uint32_t shared_blocks;              // of the launch: blocks that take shared parts; those behind them take own ones
   float scale_log2;
   // workspace, where a row has several parts
   float* part_o;   // [part][n_tok * n_heads][D]
@@ -82,6 +82,17 @@ __device__ inline SequenceSpan sequence_span(const AttentionArgs& a, uint32_t i)
 __device__ inline uint32_t seen_keys(const SequenceSpan& s, uint32_t q_all, uint32_t j) {
   const int64_t limit = (int64_t)s.len - q_all + j + 1;
   return limit < 0 ? 0u : (uint32_t)limit;
+}
+
+// Whether group g's sequences, and their queries, are a range.
+__device__ inline bool group_good(const AttentionArgs& a, uint32_t g) {
+  const int32_t f = a.group_start[g], e = a.group_start[g + 1];
+  if (f >= 0 && e >= f && (uint32_t)e <= a.n) {
+    const int32_t q0 = a.q_start[f], q1 = a.q_start[e];
+    if (q0 >= 0 && q1 >= q0 && (uint32_t)q1 <= a.n_tok) return true;
+  }
+  raise(a.status, MAASO_INST_BAD_BOUND);
+  return false;
 }
 
 // Keys of group g's common part: what the caller says, within the bound and the first sequence's row.
@@ -122,8 +133,8 @@ __device__ inline uint32_t sequence_of(const AttentionArgs& a, uint32_t t) {
   return lo;
 }
 
-// Item `tile` counted through all sequences' (or groups') tiles of `rows` rows: which one, and its first row there.
-// Taken by every lane of a wave alike.
+// Tile `tile` of `rows` rows, counted through the sequences (or groups) with more than kStreamRows rows: which one, and
+// its first row there.  Taken by every lane of a wave alike.
 __device__ inline bool find_tile(const AttentionArgs& a, bool groups, uint32_t rows, uint32_t tile, uint32_t& which, uint32_t& row0) {
   const uint32_t count = groups ? a.n_groups : a.n, lane = threadIdx.x & 63u;
   uint32_t before = 0;
@@ -131,18 +142,11 @@ __device__ inline bool find_tile(const AttentionArgs& a, bool groups, uint32_t r
     const uint32_t i = base + lane;
     uint32_t tiles = 0;
     if (i < count) {
-      uint32_t f = i, e = i + 1u;
-      bool good = true;
-      if (groups) {
-        const int32_t gf = a.group_start[i], ge = a.group_start[i + 1];
-        good = gf >= 0 && ge >= gf && (uint32_t)ge <= a.n;
-        f = good ? (uint32_t)gf : 0u;
-        e = good ? (uint32_t)ge : 0u;
-      }
-      const int32_t q0 = a.q_start[f], q1 = a.q_start[e];
-      good = good && q0 >= 0 && q1 >= q0 && (uint32_t)q1 <= a.n_tok;
-      if (!good) raise(a.status, MAASO_INST_BAD_BOUND);
-      else tiles = (uint32_t)(((uint64_t)(uint32_t)(q1 - q0) * a.group + rows - 1u) / rows);
+      const bool known = !groups || group_good(a, i);
+      const int32_t q0 = known ? a.q_start[groups ? (uint32_t)a.group_start[i] : i] : 0;
+      const int32_t q1 = known ? a.q_start[groups ? (uint32_t)a.group_start[i + 1u] : i + 1u] : 0;
+      if (q0 < 0 || q1 < q0 || (uint32_t)q1 > a.n_tok) raise(a.status, MAASO_INST_BAD_BOUND);
+      else if ((uint64_t)(uint32_t)(q1 - q0) * a.group > kStreamRows) tiles = (uint32_t)(((uint64_t)(uint32_t)(q1 - q0) * a.group + rows - 1u) / rows);
     }
     uint32_t sum = tiles;
     for (uint32_t d = 1; d < 64u; d <<= 1) {
@@ -159,6 +163,47 @@ __device__ inline bool find_tile(const AttentionArgs& a, bool groups, uint32_t r
     before += __shfl(sum, 63);
   }
   return false;
+}
+
+// An item's rows and keys.
+struct ItemKeys {
+  uint32_t tok0, n_rows, begin, end, page_row, n_q, len;
+};
+
+// False where there is nothing to do for part `part` of sequence or group `which` from row row0 on.
+__device__ inline bool item_keys(const AttentionArgs& a, bool is_shared, uint32_t which, uint32_t part, uint32_t row0, ItemKeys& k) {
+  if (is_shared) {
+    const uint32_t f = (uint32_t)a.group_start[which], e = (uint32_t)a.group_start[which + 1];  // (group_good has seen them)
+    k.tok0 = (uint32_t)a.q_start[f];
+    k.n_rows = ((uint32_t)a.q_start[e] - k.tok0) * a.group;
+    k.page_row = a.rows ? (uint32_t)a.rows[f] : f;  // (group_keys has checked it where there are keys)
+    const uint32_t all = group_keys(a, which);
+    k.begin = part * a.shared_chunk;
+    k.end = k.begin + a.shared_chunk < all ? k.begin + a.shared_chunk : all;
+  } else {
+    const SequenceSpan s = sequence_span(a, which);
+    k.tok0 = s.tok0;
+    k.n_q = s.n_q;
+    k.len = s.len;
+    k.n_rows = s.n_q * a.group;
+    k.page_row = s.row;
+    const uint64_t b = (uint64_t)shared_of(a, which) + (uint64_t)part * a.own_chunk;
+    k.begin = b < s.len ? (uint32_t)b : s.len;
+    k.end = s.len - k.begin < a.own_chunk ? s.len : k.begin + a.own_chunk;
+  }
+  // Without keys there is nothing to join; where rows have one part only, it writes their results all the same.
+  if (k.begin >= k.end) {
+    if (a.part_o || part) return false;
+    k.end = k.begin;
+  }
+  return row0 < k.n_rows;
+}
+
+// Keys that token tok of the item sees.
+__device__ inline uint32_t row_limit(const AttentionArgs& a, bool is_shared, const ItemKeys& k, uint32_t tok) {
+  if (!is_shared) return seen_keys({k.page_row, k.tok0, k.n_q, k.len}, k.n_q, tok - k.tok0);
+  const SequenceSpan s = sequence_span(a, sequence_of(a, tok));
+  return seen_keys(s, s.n_q, tok - s.tok0);
 }
 
 template <typename T, typename C> struct KeyLoad;
@@ -311,49 +356,17 @@ __global__ void __launch_bounds__(256) attention_stream_kernel(AttentionArgs a) 
   uint32_t id = is_shared ? blockIdx.x : blockIdx.x - a.shared_blocks;
   const uint32_t head = id % a.n_kv_heads;
   id /= a.n_kv_heads;
-  const uint32_t tiles = is_shared ? a.shared_tiles : a.own_tiles;
-  const uint32_t tile = id % tiles, part = id / tiles;
-  uint32_t which, row0;
-  if (!is_shared && a.max_q * a.group <= kStreamRows) { which = tile; row0 = 0; }
-  else if (!find_tile(a, is_shared, kStreamRows, tile, which, row0)) return;
-  // the tile's rows and keys
-  uint32_t tok0, n_rows, begin, end, page_row;
-  SequenceSpan span{0u, 0u, 0u, 0u};
-  uint32_t q_all = 0;
-  if (is_shared) {
-    const uint32_t f = (uint32_t)a.group_start[which], e = (uint32_t)a.group_start[which + 1];  // (find_tile has checked them)
-    tok0 = (uint32_t)a.q_start[f];
-    n_rows = ((uint32_t)a.q_start[e] - tok0) * a.group;
-    page_row = a.rows ? (uint32_t)a.rows[f] : f;  // (group_keys has checked it where there are keys)
-    const uint32_t keys = group_keys(a, which);
-    begin = part * a.shared_chunk;
-    end = begin + a.shared_chunk < keys ? begin + a.shared_chunk : keys;
-  } else {
-    span = sequence_span(a, which);
-    q_all = span.n_q;
-    tok0 = span.tok0;
-    n_rows = span.n_q * a.group;
-    page_row = span.row;
-    const uint32_t own = shared_of(a, which);
-    const uint64_t b = (uint64_t)own + (uint64_t)part * a.own_chunk;
-    begin = b < span.len ? (uint32_t)b : span.len;
-    end = span.len - begin < a.own_chunk ? span.len : begin + a.own_chunk;
-  }
-  // A block without keys has nothing to join, except that rows without any part at all are written by part 0.
+  const uint32_t count = is_shared ? a.n_groups : a.n, which = id % count, part = id / count, row0 = 0;
+  if (is_shared && !group_good(a, which)) return;
+  ItemKeys keys;
+  if (!item_keys(a, is_shared, which, part, row0, keys) || keys.n_rows > kStreamRows) return;
   const bool direct = a.part_o == nullptr;
-  if (begin >= end && !(direct && part == 0)) return;
+  const uint32_t tok0 = keys.tok0, n_rows = keys.n_rows, begin = keys.begin;
+  uint32_t end = keys.end;
   const uint32_t r = row0 + col;
   const bool real = r < n_rows;
   const uint32_t tok = tok0 + (real ? r : row0) / a.group, h = head * a.group + (real ? r : row0) % a.group;
-  if (row0 >= n_rows) return;
-  uint32_t limit;
-  if (is_shared) {
-    const uint32_t i = sequence_of(a, tok);
-    const SequenceSpan s = sequence_span(a, i);
-    limit = seen_keys(s, s.n_q, tok - s.tok0);
-  } else {
-    limit = seen_keys(span, q_all, tok - tok0);
-  }
+  const uint32_t limit = row_limit(a, is_shared, keys, tok);
   uint32_t lowest = limit, highest = limit;
 #pragma unroll
   for (int d = 1; d < 16; d <<= 1) {
@@ -369,7 +382,7 @@ __global__ void __launch_bounds__(256) attention_stream_kernel(AttentionArgs a) 
   st.clear();
   const float scale = a.scale_log2 * (sizeof(C) == 1 && a.k_scale ? a.k_scale[head] : 1.0f);
   if (begin < end)
-    st.run(a, a.table + (uint64_t)page_row * a.width, head, scale, begin, end, wave, 4u, limit, lowest);
+    st.run(a, a.table + (uint64_t)keys.page_row * a.width, head, scale, begin, end, wave, 4u, limit, lowest);
   // join the waves
   float l = st.l;
   l += __shfl_xor(l, 16);
@@ -410,12 +423,384 @@ __global__ void __launch_bounds__(256) attention_stream_kernel(AttentionArgs a) 
   }
 }
 
-// Joins a row's parts: a wave for each (token, head).
-template <typename T, typename C, int D>
+// Many rows: a block of four waves takes 128 rows, 32 a wave, and steps through the keys kKeys at a time.  Keys and
+// values of a step are brought to shared memory once for all four waves, the next step's while this one's are
+// multiplied (asynchronously from the pages, without passing registers; from a cache of 8 bits through registers, where they
+// are widened).  The products are the turned ones again, on 32 x 32 x 16 instructions, whose result holds key 8 j + 4 h + i
+// of its 32 in element 4 j + i of lane half h: key rows are read in the order that makes those eight neighbours.
+//
+// Rows lie in shared memory as they come from the pages, but for their 16-byte pieces, of which piece c lies at place
+// c ^ f(row): the sixteen lanes that are served at once then meet sixteen different places of the 256 bytes of a cycle.
+constexpr uint32_t kTileRows = 128;
+
+template <typename T, typename C, int D, int kKeys>
+struct RowTile {
+  using X8 = typename Vec<T>::x8;
+  static constexpr uint32_t kKeyBytes = kKeys * D * 2, kBuffer = 2 * kKeyBytes;
+  static constexpr uint32_t kKeyRows = 1024 / (D * 2), kValueRows = 1024 / (kKeys * 2);  // rows that a wave brings at once
+  static constexpr uint32_t kKeyLoads = kKeys / 4 / kKeyRows, kValueLoads = D / 4 / kValueRows;
+  static constexpr bool kDirect = sizeof(C) == 2;  // from the pages to shared memory as they are
+
+  char* lds;
+  uint32_t lds_base;  // its address in shared memory
+  uint32_t lane, wave, half, col, per;
+  uint32_t key_at, value_at;  // where this lane reads operands, the place's lowest bits crossed with f
+  const C* kp;
+  const C* vp;
+  uint64_t page_stride;
+  uint32_t page_log2;
+  u32x2 raw_k[kDirect ? 1 : kKeyLoads], raw_v[kDirect ? 1 : kValueLoads];
+
+  // By the lane that reads the row (key rows are read in another order, see key()): its low four bits; the next three
+  // where two rows of eight places fill 256 bytes, two where four rows of four do.
+  static __device__ inline uint32_t by_lane(uint32_t c, uint32_t places) {
+    return places >= 16u ? c & 15u : places == 8u ? c >> 1 & 7u : c >> 2 & 3u;
+  }
+  static __device__ inline uint32_t fk(uint32_t row) {
+    return by_lane((row & 3u) | (row >> 3 & 1u) << 2 | (row >> 2 & 1u) << 3, D / 8);
+  }
+  static __device__ inline uint32_t fv(uint32_t row) { return by_lane(row, kKeys / 8); }
+
+  // 16 bytes a lane from the pages to 1024 bytes of shared memory from `to` on.  Written out, because the compiler would
+  // have every later read of shared memory wait for it; the loop waits itself, once a step.
+  __device__ inline void async16(const void* from, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_base + to), "v"(from) : "memory");
+  }
+
+  // Brings keys and values from `base` on; ids: lane c < kKeys / 8 (and every kKeys / 8 after it) holds the page of keys base + 8 c.
+  __device__ inline void bring(uint32_t buffer, uint32_t base, int32_t ids) {
+    constexpr uint32_t kChunks = D / 8, kPieces = kKeys / 8;
+    const uint32_t row0 = wave * (kKeys / 4);
+    const uint32_t kpage = (uint32_t)__builtin_amdgcn_readlane(ids, (int)__builtin_amdgcn_readfirstlane((int)(row0 / 8u)));
+    const C* kb = kp + (uint64_t)kpage * page_stride;
+#pragma unroll
+    for (uint32_t it = 0; it < kKeyLoads; ++it) {
+      const uint32_t row = row0 + it * kKeyRows + lane / kChunks, place = lane % kChunks;
+      const C* from = kb + ((base + row) & (per - 1u)) * (uint32_t)D + (place ^ fk(row)) * 8u;
+      if constexpr (kDirect) async16(from, buffer * kBuffer + (row0 + it * kKeyRows) * (D * 2));
+      else raw_k[it] = *reinterpret_cast<const u32x2*>(from);
+    }
+    // (f of a value row has a bit that changes with `it`: two pieces, by turns)
+    const C* vb[2];
+#pragma unroll
+    for (uint32_t turn = 0; turn < 2u; ++turn) {
+      const uint32_t piece = lane % kPieces ^ fv(turn * kValueRows + lane / kPieces);
+      const uint32_t vpage = (uint32_t)__shfl(ids, (int)piece);
+      vb[turn] = vp + (uint64_t)vpage * page_stride + ((base + 8u * piece) & (per - 1u));
+    }
+#pragma unroll
+    for (uint32_t it = 0; it < kValueLoads; ++it) {
+      const uint32_t row = wave * (D / 4) + it * kValueRows + lane / kPieces;
+      const C* from = vb[it & 1u] + ((uint64_t)row << page_log2);
+      if constexpr (kDirect) async16(from, buffer * kBuffer + kKeyBytes + (wave * (D / 4) + it * kValueRows) * (kKeys * 2));
+      else raw_v[it] = *reinterpret_cast<const u32x2*>(from);
+    }
+  }
+
+  // What bring() has left in registers goes to shared memory.
+  __device__ inline void settle(uint32_t buffer) {
+    if constexpr (kDirect) {
+      (void)buffer;
+    } else {
+      char* to = lds + buffer * kBuffer + lane * 16u;
+#pragma unroll
+      for (uint32_t it = 0; it < kKeyLoads; ++it)
+        *reinterpret_cast<X8*>(to + (wave * (kKeys / 4) + it * kKeyRows) * (D * 2)) = widen8<T>(raw_k[it]);
+#pragma unroll
+      for (uint32_t it = 0; it < kValueLoads; ++it)
+        *reinterpret_cast<X8*>(to + kKeyBytes + (wave * (D / 4) + it * kValueRows) * (kKeys * 2)) = widen8<T>(raw_v[it]);
+    }
+  }
+
+  __device__ inline void aim() {
+    const uint32_t row = 16u * (col >> 4) + 8u * (col >> 2 & 1u) + 4u * (col >> 3 & 1u) + (col & 3u);
+    key_at = row * (D * 2) + ((half ^ fk(row)) << 4);
+    value_at = kKeyBytes + col * (kKeys * 2) + ((half ^ fv(col)) << 4);
+  }
+  // (piece 2 s + half: bits above the first cross with what aim() has left there)
+  __device__ inline X8 key(uint32_t buffer, uint32_t block, uint32_t s) const {
+    constexpr uint32_t kCrossed = D == 64 ? 4u : 8u;
+    return *reinterpret_cast<const X8*>(lds + ((buffer * kBuffer + key_at) ^ (s % kCrossed << 5)) + block * 32u * (D * 2) + s / kCrossed * 256u);
+  }
+  __device__ inline X8 value(uint32_t buffer, uint32_t d, uint32_t t) const {
+    return *reinterpret_cast<const X8*>(lds + ((buffer * kBuffer + value_at) ^ (t << 5)) + d * 32u * (kKeys * 2));
+  }
+};
+
+// Asks the scheduler for kProducts products, each with its operand read kAhead products before it.
+template <int kProducts>
+__device__ inline void feed() {
+  constexpr int kAhead = kProducts < 6 ? kProducts : 6;
+  __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);  // reads of shared memory
+#pragma unroll
+  for (int k = kAhead; k < kProducts; ++k) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // a product
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
+}
+
+template <typename T, typename C, int D, int kKeys>
+__global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attention_tile_kernel(AttentionArgs a) {
+  using X8 = typename Vec<T>::x8;
+  using Tile = RowTile<T, C, D, kKeys>;
+  constexpr int kBlocks = kKeys / 32, kSteps = kKeys / 16;
+  __shared__ __align__(128) char lds[2 * Tile::kBuffer];
+  const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31u, half = lane >> 5;
+  const bool is_shared = blockIdx.x < a.shared_blocks;
+  uint32_t id = is_shared ? blockIdx.x : blockIdx.x - a.shared_blocks;
+  const uint32_t head = id % a.n_kv_heads;
+  id /= a.n_kv_heads;
+  const uint32_t tiles = is_shared ? a.shared_tiles : a.own_tiles;
+  uint32_t which, row0;
+  const uint32_t part = id / tiles;
+  if (!find_tile(a, is_shared, kTileRows, id % tiles, which, row0)) return;
+  ItemKeys keys;
+  if (!item_keys(a, is_shared, which, part, row0, keys)) return;
+  // this lane's row
+  const uint32_t r = row0 + wave * 32u + col;
+  const bool real = r < keys.n_rows;
+  const uint32_t tok = keys.tok0 + (real ? r : row0) / a.group, h = head * a.group + (real ? r : row0) % a.group;
+  const uint32_t limit = real ? row_limit(a, is_shared, keys, tok) : 0u;
+  uint32_t lowest = real ? limit : 0xffffffffu, highest = limit;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const uint32_t x = __shfl_xor(lowest, d), y = __shfl_xor(highest, d);
+    lowest = x < lowest ? x : lowest;
+    highest = y > highest ? y : highest;
+  }
+  __shared__ uint32_t lowest_of[4];
+  if (lane == 0) lowest_of[wave] = lowest;
+  __syncthreads();
+  const uint32_t low2 = lowest_of[0] < lowest_of[1] ? lowest_of[0] : lowest_of[1], low3 = lowest_of[2] < lowest_of[3] ? lowest_of[2] : lowest_of[3];
+  const uint32_t block_lowest = low2 < low3 ? low2 : low3;
+  // A sequence's rows see more with every token: what the block's last row sees is the end.
+  const uint32_t begin = keys.begin;
+  uint32_t end = keys.end;
+  if (!is_shared) {
+    const uint32_t last = row0 + kTileRows < keys.n_rows ? row0 + kTileRows - 1u : keys.n_rows - 1u;
+    const uint32_t most = row_limit(a, false, keys, keys.tok0 + last / a.group);
+    end = most < end ? most : end;
+    end = end < begin ? begin : end;
+  }
+  const float scale0 = a.scale_log2 * (sizeof(C) == 1 && a.k_scale ? a.k_scale[head] : 1.0f);
+  const float scale = scale0 == 0.0f ? 1.0f : fabsf(scale0);
+  X8 q[D / 16];
+  {
+    // (a negative scale turns the queries' signs, a scale of zero makes them zero: so the largest score is the largest product)
+    const T* qp = static_cast<const T*>(a.q) + (uint64_t)tok * a.q_stride + (uint64_t)h * D + half * 8u;
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) {
+      q[s] = *reinterpret_cast<const X8*>(qp + s * 16);
+      if (!(scale0 > 0.0f)) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) q[s][k] = scale0 == 0.0f ? (T)0.0f : -q[s][k];
+      }
+    }
+  }
+  // (the queries have come: a wait for them inside the loop would wait for the step's loads as well)
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) asm volatile("" : "+v"(q[s]));
+  f32x16 o[D / 32];
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[d][e] = 0.0f;
+  float m = -INFINITY, l = 0.0f;
+
+  Tile tile;
+  tile.lds = lds;
+  tile.lane = lane;
+  tile.wave = wave;
+  tile.half = half;
+  tile.col = col;
+  tile.lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+  tile.aim();
+  tile.per = 1u << a.page_log2;
+  tile.page_log2 = a.page_log2;
+  tile.page_stride = a.page_stride;
+  tile.kp = reinterpret_cast<const C*>(a.k_pages) + ((uint64_t)head << a.page_log2) * D;
+  tile.vp = reinterpret_cast<const C*>(a.v_pages) + ((uint64_t)head << a.page_log2) * D;
+  const int32_t* list = a.table + (uint64_t)keys.page_row * a.width;
+  // The table's entry for keys at + 8 (lane % (kKeys / 8)); then the page, 0 where there is none, and which keys have one.
+  auto entry_at = [&](uint32_t at) {
+    const uint32_t key8 = at + 8u * (lane % (kKeys / 8));
+    return key8 < end && (key8 | 15u) >= begin ? list[key8 >> a.page_log2] : -1;  // (a wave's key rows go by the page of the first of sixteen)
+  };
+  auto page_of = [&](int32_t entry, uint32_t at, uint32_t& good) {
+    const bool held = entry >= 0 && (uint32_t)entry < a.n_pages;
+    const uint32_t key8 = at + 8u * (lane % (kKeys / 8));
+    if (!held && key8 < end && (key8 | 15u) >= begin) raise(a.status, MAASO_INST_BAD_PAGE);
+    good = (uint32_t)__ballot(held) & ((1u << (kKeys / 8)) - 1u);
+    return held ? entry : 0;
+  };
+  const uint32_t first = begin & ~(uint32_t)(kKeys - 1);
+  uint32_t good = 0, buffer = 0;
+  int32_t entry = -1;
+  if (begin < end) {
+    tile.bring(0, first, page_of(entry_at(first), first, good));
+    tile.settle(0);
+    entry = entry_at(first + kKeys);
+  }
+  for (uint32_t base = first; begin < end && base < end; base += kKeys) {
+    // This step's keys and values, and the next one's entries, have come; everybody is done with the other buffer.
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    const bool more = base + kKeys < end;
+    const uint32_t good_now = good;
+    if (more) {
+      tile.bring(buffer ^ 1u, base + kKeys, page_of(entry, base + kKeys, good));
+      entry = entry_at(base + 2 * kKeys);
+    }
+    // Keys of a step that not every row of the block sees.  Values of keys that no row sees become zeros in shared memory,
+    // whatever their place holds; where one that some rows see is not finite, the second product is taken row by row.
+    const bool plain = base >= begin && base + kKeys <= block_lowest && base + kKeys <= end && good_now == (1u << (kKeys / 8)) - 1u;
+    bool by_row = false;
+    if (!plain) {
+      bool odd = false;
+#pragma unroll 1
+      for (uint32_t e = threadIdx.x; e < D * (kKeys / 8); e += 256u) {
+        const uint32_t row = e / (kKeys / 8), piece = e % (kKeys / 8) ^ Tile::fv(row), k0 = base + piece * 8u;
+        X8* at = reinterpret_cast<X8*>(lds + buffer * Tile::kBuffer + Tile::kKeyBytes + e * 16u);
+        X8 v = *at;
+        const bool none = !(good_now >> piece & 1u);
+        bool changed = false;
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (none || k0 + k < begin || k0 + k >= end) { v[k] = (T)0.0f; changed = true; }
+        if (changed) *at = v;
+        odd = odd || !finite16(v);
+      }
+      by_row = __syncthreads_or(odd);
+    }
+    if (base < highest) {  // (none of the wave's rows sees anything from its highest limit on)
+      f32x16 x[kBlocks];
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[b][e] = 0.0f;
+#pragma unroll
+      for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) x[b] = mfma_32x32x16(tile.key(buffer, b, s), q[s], x[b]);
+      feed<kBlocks * (D / 16)>();
+      if (!plain) {
+        const uint32_t lim = limit < end ? limit : end;
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const uint32_t at = b * 32 + (e >> 3) * 16 + half * 8u + (e & 7), k = base + at;
+            if (k < begin || k >= lim || !(good_now >> (at >> 3) & 1u)) x[b][e] = -INFINITY;
+          }
+      }
+      float top = x[0][0];
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, x[b][e]);
+      top = fmaxf(top, __shfl_xor(top, 32)) * scale;
+      // The maximum follows only where it has grown by more than 8 (weights up to 256 are as exact as up to 1): else the
+      // sums need not be scaled.
+      if (__any(top > m + 8.0f)) {
+        const float now = fmaxf(m, top), turn = __builtin_amdgcn_exp2f(m - (now == -INFINITY ? 0.0f : now));
+        m = now;
+        l *= turn;
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d) o[d] = o[d] * turn;
+      }
+      const float zero = m == -INFINITY ? 0.0f : m;
+      X8 p[kSteps];
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b) {
+        float sum = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          x[b][e] = __builtin_amdgcn_exp2f(fmaf(x[b][e], scale, -zero));
+          sum += x[b][e];
+        }
+        l += sum;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          float y[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) y[k] = x[b][t * 8 + k];
+          p[b * 2 + t] = narrow8<T>(y);
+        }
+      }
+      if (!by_row) {
+#pragma unroll
+        for (int t = 0; t < kSteps; ++t)
+#pragma unroll
+          for (int d = 0; d < D / 32; ++d) o[d] = mfma_32x32x16(tile.value(buffer, d, t), p[t], o[d]);
+        feed<kSteps * (D / 32)>();
+      } else {
+        // (rare: written to need few registers)
+#pragma unroll 1
+        for (uint32_t turn = 0; turn < 32u * kSteps; ++turn) {
+          const uint32_t one = turn / kSteps, t = turn % kSteps, sees = __shfl(limit, (int)one);
+          X8 w = p[0];
+#pragma unroll
+          for (uint32_t k = 1; k < (uint32_t)kSteps; ++k)
+            if (t == k) w = p[k];
+#pragma unroll
+          for (int d = 0; d < D / 32; ++d) {
+            X8 v = tile.value(buffer, d, t);
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+              if (base + t * 16u + half * 8u + k >= sees) v[k] = (T)0.0f;
+            const f32x16 y = mfma_32x32x16(v, w, o[d]);
+            if (col == one) o[d] = y;
+            asm volatile("" ::: "memory");
+          }
+        }
+      }
+    }
+    if (more) tile.settle(buffer ^ 1u);
+    buffer ^= 1u;
+  }
+  l += __shfl_xor(l, 32);
+  if (!real) return;
+  const bool direct = a.part_o == nullptr;
+  if (direct) {
+    const float vs = sizeof(C) == 1 && a.v_scale ? a.v_scale[head] : 1.0f;
+    const float by = l == 0.0f ? 0.0f : vs / l;
+    T* to = static_cast<T*>(a.out) + (uint64_t)tok * a.out_stride + (uint64_t)h * D;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t at = d * 32 + j * 8 + half * 4u;
+        float y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = l == 0.0f ? 0.0f : o[d][4 * j + i] * by;
+        const auto lo = narrow2<T>(y[0], y[1]), hi = narrow2<T>(y[2], y[3]);
+        typename Vec<T>::x2* w = reinterpret_cast<typename Vec<T>::x2*>(to + at);
+        w[0] = lo;
+        w[1] = hi;
+      }
+    if (a.lse && half == 0u) a.lse[(uint64_t)tok * a.n_heads + h] = l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2;
+  } else {
+    const uint64_t slot = (uint64_t)(is_shared ? part : a.shared_parts + part) * a.n_tok * a.n_heads + (uint64_t)tok * a.n_heads + h;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<f32x4*>(a.part_o + slot * D + d * 32 + j * 8 + half * 4u) = (f32x4){o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]};
+    if (half == 0u) { a.part_ml[slot * 2] = m; a.part_ml[slot * 2 + 1] = l; }
+  }
+}
+
+// Joins a row's parts: kWaves waves for each (token, head).  A wave reads the maxima and sums of 64 parts at once, a part a
+// lane, and then its parts' sums, four of them in flight.  Few rows have many parts, and four waves each.
+template <typename T, typename C, int D, int kWaves>
 __global__ void __launch_bounds__(256) attention_join_kernel(AttentionArgs a) {
-  const uint32_t lane = threadIdx.x & 63u;
-  const uint64_t row = (uint64_t)blockIdx.x * 4u + (threadIdx.x >> 6), rows = (uint64_t)a.n_tok * a.n_heads;
-  if (row >= rows) return;
+  constexpr int kPer = D / 64;
+  typedef float Out __attribute__((ext_vector_type(kPer)));
+  __shared__ float sum_of[4][D], ml_of[4][2];
+  const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint64_t rows = (uint64_t)a.n_tok * a.n_heads, row = kWaves == 4 ? blockIdx.x : (uint64_t)blockIdx.x * 4u + wave;
+  if (row >= rows) return;  // (with four waves to a row there are as many blocks as rows)
   const uint32_t tok = (uint32_t)(row / a.n_heads), h = (uint32_t)(row % a.n_heads);
   const uint32_t i = sequence_of(a, tok);
   const SequenceSpan s = sequence_span(a, i);
@@ -425,28 +810,72 @@ __global__ void __launch_bounds__(256) attention_join_kernel(AttentionArgs a) {
   uint32_t n_shared = 0, n_own = 0;
   if (mine && own0) n_shared = (own0 + a.shared_chunk - 1u) / a.shared_chunk;
   if (mine && s.len > own0) n_own = (s.len - own0 + a.own_chunk - 1u) / a.own_chunk;
-  float m = -INFINITY;
-  const uint32_t parts = n_shared + n_own;
+  const uint32_t parts = n_shared + n_own, first = kWaves == 4 ? wave : 0u;
   auto slot = [&](uint32_t p) { return (uint64_t)(p < n_shared ? p : a.shared_parts + (p - n_shared)) * rows + row; };
-  for (uint32_t p = lane; p < parts; p += 64u) m = fmaxf(m, a.part_ml[slot(p) * 2]);
+  float m = -INFINITY, l = 0.0f;
+  Out acc;
 #pragma unroll
-  for (int d = 32; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-  const float zero = m == -INFINITY ? 0.0f : m;
-  float l = 0.0f, acc[D / 64];
+  for (int k = 0; k < kPer; ++k) acc[k] = 0.0f;
+  for (uint32_t p0 = first; p0 < parts; p0 += 64u * kWaves) {
+    const uint32_t p = p0 + lane * kWaves;
+    float pm = -INFINITY, pl = 0.0f;
+    if (p < parts) {
+      const uint64_t at = slot(p);
+      pm = a.part_ml[at * 2];
+      pl = a.part_ml[at * 2 + 1];
+    }
+    float top = fmaxf(m, pm);
 #pragma unroll
-  for (int k = 0; k < D / 64; ++k) acc[k] = 0.0f;
-  for (uint32_t p = 0; p < parts; ++p) {
-    const uint64_t at = slot(p);
-    const float turn = __builtin_amdgcn_exp2f(a.part_ml[at * 2] - zero);
-    l = fmaf(a.part_ml[at * 2 + 1], turn, l);
+    for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    const float zero = top == -INFINITY ? 0.0f : top, turn = __builtin_amdgcn_exp2f(m - zero);
+    const float weight = __builtin_amdgcn_exp2f(pm - zero);
+    m = top;
+    float sum = pl * weight;
 #pragma unroll
-    for (int k = 0; k < D / 64; ++k) acc[k] = fmaf(a.part_o[at * D + lane * (D / 64) + k], turn, acc[k]);
+    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+    l = fmaf(l, turn, sum);
+    acc = acc * turn;
+    const uint32_t left = (parts - p0 + kWaves - 1u) / kWaves, n = left < 64u ? left : 64u;
+    for (uint32_t k0 = 0; k0 < n; k0 += 4u) {
+      Out v[4];
+#pragma unroll
+      for (uint32_t k = 0; k < 4u; ++k) {
+        const uint32_t at = k0 + k < n ? k0 + k : n - 1u;  // (not added below)
+        v[k] = *reinterpret_cast<const Out*>(a.part_o + slot(p0 + at * kWaves) * D + lane * kPer);
+      }
+#pragma unroll
+      for (uint32_t k = 0; k < 4u; ++k) {
+        const float w = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(weight), (int)((k0 + k) & 63u)));
+        if (k0 + k >= n) break;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) acc[e] = fmaf(v[k][e], w, acc[e]);
+      }
+    }
+  }
+  if constexpr (kWaves == 4) {
+    *reinterpret_cast<Out*>(&sum_of[wave][lane * kPer]) = acc;
+    if (lane == 0) { ml_of[wave][0] = m; ml_of[wave][1] = l; }
+    __syncthreads();
+    if (wave != 0) return;
+    m = fmaxf(fmaxf(ml_of[0][0], ml_of[1][0]), fmaxf(ml_of[2][0], ml_of[3][0]));
+    const float zero = m == -INFINITY ? 0.0f : m;
+    l = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) acc[k] = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float turn = __builtin_amdgcn_exp2f(ml_of[w][0] - zero);
+      l = fmaf(ml_of[w][1], turn, l);
+      const Out v = *reinterpret_cast<const Out*>(&sum_of[w][lane * kPer]);
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) acc[e] = fmaf(v[e], turn, acc[e]);
+    }
   }
   const float vs = sizeof(C) == 1 && a.v_scale ? a.v_scale[h / a.group] : 1.0f;
   const float by = l == 0.0f ? 0.0f : vs / l;
-  T* to = static_cast<T*>(a.out) + (uint64_t)tok * a.out_stride + (uint64_t)h * D + lane * (D / 64);
+  T* to = static_cast<T*>(a.out) + (uint64_t)tok * a.out_stride + (uint64_t)h * D + lane * kPer;
 #pragma unroll
-  for (int k = 0; k < D / 64; ++k) to[k] = (T)(l == 0.0f ? 0.0f : acc[k] * by);
+  for (int k = 0; k < kPer; ++k) to[k] = (T)(l == 0.0f ? 0.0f : acc[k] * by);
   if (a.lse && lane == 0) a.lse[row] = l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 

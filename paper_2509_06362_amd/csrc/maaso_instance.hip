@@ -281,12 +281,27 @@ void launch_append_d(uint32_t d, const AppendArgs& a, uint32_t blocks, bool wide
   else launch_append<T, C, 256>(a, blocks, wide, interleaved, s);
 }
 
+// Few rows of a sequence or group go through the stream kernel, more through the tile kernel; which, the kernels see
+// from the device's arrays, the host leaves out a launch that would have nothing.
 template <typename T, typename C, int D>
-void launch_attention(const AttentionArgs& a, hipStream_t s) {
-  const uint32_t own_blocks = a.own_tiles * a.n_kv_heads * a.own_parts;
-  hipLaunchKernelGGL((attention_stream_kernel<T, C, D>), dim3(a.shared_blocks + own_blocks), dim3(256), 0, s, a);
-  if (a.part_o)
-    hipLaunchKernelGGL((attention_join_kernel<T, C, D>), dim3((uint32_t)(((uint64_t)a.n_tok * a.n_heads + 3u) / 4u)), dim3(256), 0, s, a);
+void launch_attention(AttentionArgs a, hipStream_t s) {
+  const uint32_t heads = a.n_kv_heads;
+  const bool tiles = a.max_q * a.group > kStreamRows, shared_tiles = a.shared_parts && (uint64_t)a.n_tok * a.group > kStreamRows;
+  if (tiles || shared_tiles) {
+    AttentionArgs t = a;
+    t.shared_blocks = shared_tiles ? a.shared_tiles * heads * a.shared_parts : 0u;
+    const uint32_t blocks = t.shared_blocks + (tiles ? a.own_tiles * heads * a.own_parts : 0u);
+    hipLaunchKernelGGL((attention_tile_kernel<T, C, D, D == 256 ? 32 : 64>), dim3(blocks), dim3(256), 0, s, t);
+  }
+  if (!tiles || a.n_groups || (uint64_t)a.n * a.max_q != a.n_tok) {
+    a.shared_blocks = a.n_groups * heads * a.shared_parts;
+    hipLaunchKernelGGL((attention_stream_kernel<T, C, D>), dim3(a.shared_blocks + a.n * heads * a.own_parts), dim3(256), 0, s, a);
+  }
+  if (a.part_o) {
+    const uint64_t rows = (uint64_t)a.n_tok * a.n_heads;
+    if (rows < 4096u) hipLaunchKernelGGL((attention_join_kernel<T, C, D, 4>), dim3((uint32_t)rows), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((attention_join_kernel<T, C, D, 1>), dim3((uint32_t)((rows + 3u) / 4u)), dim3(256), 0, s, a);
+  }
 }
 
 template <typename T, typename C>
@@ -394,16 +409,16 @@ int maaso_kv_attention(maaso_instance* inst, const maaso_kv_cache* cache, uint32
   a.scale_log2 = (float)((double)p->scale * 1.4426950408889634);
   a.status = inst->status;
   const uint64_t group_rows = (uint64_t)p->n_tok * a.group;
-  a.own_tiles = (uint64_t)p->max_q * a.group <= kStreamRows ? p->n : (uint32_t)(group_rows / kStreamRows + p->n);
-  a.shared_tiles = a.n_groups ? (uint32_t)(group_rows / kStreamRows + a.n_groups) : 0u;
-  // Keys are split until there are some four blocks to a compute unit.
-  const uint64_t want = 4u * (uint64_t)inst->n_cu;
-  auto chunk_of = [&](uint64_t keys, uint64_t items) {
-    const uint64_t parts = items >= want ? 1u : (want + items - 1u) / items;
+  a.own_tiles = (uint32_t)(group_rows / kTileRows + p->n);
+  a.shared_tiles = a.n_groups ? (uint32_t)(group_rows / kTileRows + a.n_groups) : 0u;
+  const bool tiles = (uint64_t)p->max_q * a.group > kStreamRows, shared_tiles = group_rows > kStreamRows;
+  // Keys are split until there are some four blocks to a compute unit, two of the larger ones.
+  auto chunk_of = [&](uint64_t keys, uint64_t items, uint64_t per_cu) {
+    const uint64_t want = per_cu * (uint64_t)inst->n_cu, parts = items >= want ? 1u : (want + items - 1u) / items;
     return std::max(256u, round_up((keys + parts - 1u) / parts, 256u));
   };
-  a.own_chunk = chunk_of(p->max_len, (uint64_t)a.own_tiles * a.n_kv_heads);
-  a.shared_chunk = a.n_groups ? chunk_of(a.max_shared, (uint64_t)a.shared_tiles * a.n_kv_heads) : 256u;
+  a.own_chunk = chunk_of(p->max_len, (uint64_t)(tiles ? a.own_tiles : p->n) * a.n_kv_heads, tiles ? 2u : 4u);
+  a.shared_chunk = a.n_groups ? chunk_of(a.max_shared, (uint64_t)(shared_tiles ? a.shared_tiles : a.n_groups) * a.n_kv_heads, shared_tiles ? 2u : 4u) : 256u;
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
   InstanceCall call(inst, s);
   if (call.rc != MAASO_OK) return call.rc;
@@ -421,10 +436,9 @@ int maaso_kv_attention(maaso_instance* inst, const maaso_kv_cache* cache, uint32
     if (a.own_parts >= a.shared_parts) a.own_chunk *= 2u;
     else a.shared_chunk *= 2u;
   }
-  const uint64_t shared_blocks = (uint64_t)a.shared_tiles * a.n_kv_heads * a.shared_parts;
-  const uint64_t own_blocks = (uint64_t)a.own_tiles * a.n_kv_heads * a.own_parts;
+  const uint64_t shared_blocks = (uint64_t)(a.shared_tiles + a.n_groups) * a.n_kv_heads * a.shared_parts;
+  const uint64_t own_blocks = (uint64_t)(a.own_tiles + p->n) * a.n_kv_heads * a.own_parts;
   if (shared_blocks + own_blocks > 0x7fffffffull || (rows + 3u) / 4u > 0x7fffffffull) return MAASO_E_SHAPE;
-  a.shared_blocks = (uint32_t)shared_blocks;
   if (p->type == MAASO_BF16 && cache->type == MAASO_BF16) launch_attention_d<__bf16, __bf16>(d, a, s);
   else if (p->type == MAASO_BF16) launch_attention_d<__bf16, E4m3>(d, a, s);
   else if (cache->type == MAASO_FP16) launch_attention_d<_Float16, _Float16>(d, a, s);
