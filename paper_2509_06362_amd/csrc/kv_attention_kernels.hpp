@@ -168,7 +168,16 @@ __device__ inline bool find_tile(const AttentionArgs& a, bool groups, uint32_t r
 // An item's rows and keys.
 struct ItemKeys {
   uint32_t tok0, n_rows, begin, end, page_row, n_q, len;
+  bool alone;  // its rows have no other part: their results are written as they are, not joined
 };
+
+// Parts of a row: those of its group's keys, those of the sequence's own.
+struct RowParts {
+  uint32_t n_shared, n_own;
+};
+__device__ inline RowParts row_parts(const AttentionArgs& a, uint32_t len, uint32_t shared) {
+  return {(shared + a.shared_chunk - 1u) / a.shared_chunk, len > shared ? (len - shared + a.own_chunk - 1u) / a.own_chunk : 0u};
+}
 
 // False where there is nothing to do for part `part` of sequence or group `which` from row row0 on.
 __device__ inline bool item_keys(const AttentionArgs& a, bool is_shared, uint32_t which, uint32_t part, uint32_t row0, ItemKeys& k) {
@@ -178,6 +187,7 @@ __device__ inline bool item_keys(const AttentionArgs& a, bool is_shared, uint32_
     k.n_rows = ((uint32_t)a.q_start[e] - k.tok0) * a.group;
     k.page_row = a.rows ? (uint32_t)a.rows[f] : f;  // (group_keys has checked it where there are keys)
     const uint32_t all = group_keys(a, which);
+    k.alone = false;
     k.begin = part * a.shared_chunk;
     k.end = k.begin + a.shared_chunk < all ? k.begin + a.shared_chunk : all;
   } else {
@@ -187,13 +197,16 @@ __device__ inline bool item_keys(const AttentionArgs& a, bool is_shared, uint32_
     k.len = s.len;
     k.n_rows = s.n_q * a.group;
     k.page_row = s.row;
-    const uint64_t b = (uint64_t)shared_of(a, which) + (uint64_t)part * a.own_chunk;
+    const uint32_t shared = shared_of(a, which);
+    const RowParts parts = row_parts(a, s.len, shared);
+    k.alone = parts.n_shared + parts.n_own <= 1u && parts.n_shared == 0u;
+    const uint64_t b = (uint64_t)shared + (uint64_t)part * a.own_chunk;
     k.begin = b < s.len ? (uint32_t)b : s.len;
     k.end = s.len - k.begin < a.own_chunk ? s.len : k.begin + a.own_chunk;
   }
-  // Without keys there is nothing to join; where rows have one part only, it writes their results all the same.
+  // Without keys there is nothing to join; rows without any are written all the same, by the first part.
   if (k.begin >= k.end) {
-    if (a.part_o || part) return false;
+    if (!k.alone || part) return false;
     k.end = k.begin;
   }
   return row0 < k.n_rows;
@@ -360,7 +373,7 @@ __global__ void __launch_bounds__(256) attention_stream_kernel(AttentionArgs a) 
   if (is_shared && !group_good(a, which)) return;
   ItemKeys keys;
   if (!item_keys(a, is_shared, which, part, row0, keys) || keys.n_rows > kStreamRows) return;
-  const bool direct = a.part_o == nullptr;
+  const bool direct = keys.alone;
   const uint32_t tok0 = keys.tok0, n_rows = keys.n_rows, begin = keys.begin;
   uint32_t end = keys.end;
   const uint32_t r = row0 + col;
@@ -761,8 +774,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attention_tile_kernel(A
   }
   l += __shfl_xor(l, 32);
   if (!real) return;
-  const bool direct = a.part_o == nullptr;
-  if (direct) {
+  if (keys.alone) {
     const float vs = sizeof(C) == 1 && a.v_scale ? a.v_scale[head] : 1.0f;
     const float by = l == 0.0f ? 0.0f : vs / l;
     T* to = static_cast<T*>(a.out) + (uint64_t)tok * a.out_stride + (uint64_t)h * D;
@@ -791,92 +803,90 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attention_tile_kernel(A
   }
 }
 
-// Joins a row's parts: kWaves waves for each (token, head).  A wave reads the maxima and sums of 64 parts at once, a part a
-// lane, and then its parts' sums, four of them in flight.  Few rows have many parts, and four waves each.
-template <typename T, typename C, int D, int kWaves>
+// Joins rows' parts.  A block takes kTokens tokens and some heads; 256 / D heads share a wave, a lane has four neighbouring
+// elements of one.  With many rows each wave has heads of its own, with few (kSplit 4) the four waves share the parts of the
+// same heads.  Four parts are in flight.  Bound by memory: 4 D + 8 bytes a part in, 2 D a row out.
+template <typename T, typename C, int D, int kSplit, int kTokens>
 __global__ void __launch_bounds__(256) attention_join_kernel(AttentionArgs a) {
-  constexpr int kPer = D / 64;
-  typedef float Out __attribute__((ext_vector_type(kPer)));
-  __shared__ float sum_of[4][D], ml_of[4][2];
+  constexpr uint32_t kHeads = 256 / D, kLanes = D / 4;
+  __shared__ f32x4 sum_of[kSplit][64];
+  __shared__ float ml_of[kSplit][64][2];
   const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint64_t rows = (uint64_t)a.n_tok * a.n_heads, row = kWaves == 4 ? blockIdx.x : (uint64_t)blockIdx.x * 4u + wave;
-  if (row >= rows) return;  // (with four waves to a row there are as many blocks as rows)
-  const uint32_t tok = (uint32_t)(row / a.n_heads), h = (uint32_t)(row % a.n_heads);
-  const uint32_t i = sequence_of(a, tok);
-  const SequenceSpan s = sequence_span(a, i);
-  const uint32_t own0 = shared_of(a, i), j = tok - s.tok0;
-  const bool mine = tok >= s.tok0 && j < s.n_q;
-  // parts that were written: those of the group's keys, those of the sequence's
-  uint32_t n_shared = 0, n_own = 0;
-  if (mine && own0) n_shared = (own0 + a.shared_chunk - 1u) / a.shared_chunk;
-  if (mine && s.len > own0) n_own = (s.len - own0 + a.own_chunk - 1u) / a.own_chunk;
-  const uint32_t parts = n_shared + n_own, first = kWaves == 4 ? wave : 0u;
-  auto slot = [&](uint32_t p) { return (uint64_t)(p < n_shared ? p : a.shared_parts + (p - n_shared)) * rows + row; };
-  float m = -INFINITY, l = 0.0f;
-  Out acc;
-#pragma unroll
-  for (int k = 0; k < kPer; ++k) acc[k] = 0.0f;
-  for (uint32_t p0 = first; p0 < parts; p0 += 64u * kWaves) {
-    const uint32_t p = p0 + lane * kWaves;
-    float pm = -INFINITY, pl = 0.0f;
-    if (p < parts) {
-      const uint64_t at = slot(p);
-      pm = a.part_ml[at * 2];
-      pl = a.part_ml[at * 2 + 1];
+  const uint32_t h = (kSplit == 4 ? blockIdx.y : blockIdx.y * 4u + wave) * kHeads + lane / kLanes, at = lane % kLanes * 4u;
+  const uint64_t rows = (uint64_t)a.n_tok * a.n_heads;
+  uint32_t known = 0;  // the token behind the last one that `s` and `parts` are of
+  SequenceSpan s{0u, 0u, 0u, 0u};
+  RowParts of{0u, 0u};
+  for (uint32_t tok = blockIdx.x * kTokens; tok < blockIdx.x * kTokens + kTokens && tok < a.n_tok; ++tok) {
+    if (tok >= known) {
+      const uint32_t i = sequence_of(a, tok);
+      s = sequence_span(a, i);
+      const bool mine = tok >= s.tok0 && tok - s.tok0 < s.n_q;
+      of = mine ? row_parts(a, s.len, shared_of(a, i)) : RowParts{0u, 0u};
+      known = mine ? s.tok0 + s.n_q : tok + 1u;
     }
-    float top = fmaxf(m, pm);
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-    const float zero = top == -INFINITY ? 0.0f : top, turn = __builtin_amdgcn_exp2f(m - zero);
-    const float weight = __builtin_amdgcn_exp2f(pm - zero);
-    m = top;
-    float sum = pl * weight;
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
-    l = fmaf(l, turn, sum);
-    acc = acc * turn;
-    const uint32_t left = (parts - p0 + kWaves - 1u) / kWaves, n = left < 64u ? left : 64u;
-    for (uint32_t k0 = 0; k0 < n; k0 += 4u) {
-      Out v[4];
+    if (of.n_shared == 0u && of.n_own == 1u) {  // (written already)
+      if (known > tok + 1u) tok = known - 1u;
+      continue;
+    }
+    const bool real = h < a.n_heads;
+    const uint64_t row = (uint64_t)tok * a.n_heads + (real ? h : 0u);
+    const uint32_t parts = of.n_shared + of.n_own;
+    float m = -INFINITY, l = 0.0f;
+    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (uint32_t p0 = kSplit == 4 ? wave : 0u; p0 < parts; p0 += 4u * kSplit) {
+      f32x4 v[4];
+      float pm[4], pl[4];
 #pragma unroll
       for (uint32_t k = 0; k < 4u; ++k) {
-        const uint32_t at = k0 + k < n ? k0 + k : n - 1u;  // (not added below)
-        v[k] = *reinterpret_cast<const Out*>(a.part_o + slot(p0 + at * kWaves) * D + lane * kPer);
+        const uint32_t p = p0 + k * kSplit < parts ? p0 + k * kSplit : p0;
+        const uint64_t slot = (uint64_t)(p < of.n_shared ? p : a.shared_parts + (p - of.n_shared)) * rows + row;
+        const f32x2 ml = *reinterpret_cast<const f32x2*>(a.part_ml + slot * 2);
+        v[k] = *reinterpret_cast<const f32x4*>(a.part_o + slot * D + at);
+        pm[k] = p0 + k * kSplit < parts ? ml[0] : -INFINITY;
+        pl[k] = ml[1];
       }
+      const float top = fmaxf(fmaxf(fmaxf(m, pm[0]), fmaxf(pm[1], pm[2])), pm[3]), zero = top == -INFINITY ? 0.0f : top;
+      const float turn = __builtin_amdgcn_exp2f(m - zero);
+      m = top;
+      l *= turn;
+      acc = acc * turn;
 #pragma unroll
       for (uint32_t k = 0; k < 4u; ++k) {
-        const float w = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(weight), (int)((k0 + k) & 63u)));
-        if (k0 + k >= n) break;
+        const float w = __builtin_amdgcn_exp2f(pm[k] - zero);
+        if (p0 + k * kSplit >= parts) break;
+        l = fmaf(pl[k], w, l);
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) acc[e] = fmaf(v[k][e], w, acc[e]);
+        for (int e = 0; e < 4; ++e) acc[e] = fmaf(v[k][e], w, acc[e]);
       }
     }
-  }
-  if constexpr (kWaves == 4) {
-    *reinterpret_cast<Out*>(&sum_of[wave][lane * kPer]) = acc;
-    if (lane == 0) { ml_of[wave][0] = m; ml_of[wave][1] = l; }
-    __syncthreads();
-    if (wave != 0) return;
-    m = fmaxf(fmaxf(ml_of[0][0], ml_of[1][0]), fmaxf(ml_of[2][0], ml_of[3][0]));
-    const float zero = m == -INFINITY ? 0.0f : m;
-    l = 0.0f;
+    if constexpr (kSplit == 4) {
+      __syncthreads();
+      sum_of[wave][lane] = acc;
+      ml_of[wave][lane][0] = m;
+      ml_of[wave][lane][1] = l;
+      __syncthreads();
+      if (wave != 0u) continue;
+      m = fmaxf(fmaxf(ml_of[0][lane][0], ml_of[1][lane][0]), fmaxf(ml_of[2][lane][0], ml_of[3][lane][0]));
+      const float zero = m == -INFINITY ? 0.0f : m;
+      l = 0.0f;
+      acc = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int k = 0; k < kPer; ++k) acc[k] = 0.0f;
+      for (int w = 0; w < 4; ++w) {
+        const float turn = __builtin_amdgcn_exp2f(ml_of[w][lane][0] - zero);
+        l = fmaf(ml_of[w][lane][1], turn, l);
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const float turn = __builtin_amdgcn_exp2f(ml_of[w][0] - zero);
-      l = fmaf(ml_of[w][1], turn, l);
-      const Out v = *reinterpret_cast<const Out*>(&sum_of[w][lane * kPer]);
-#pragma unroll
-      for (int e = 0; e < kPer; ++e) acc[e] = fmaf(v[e], turn, acc[e]);
+        for (int e = 0; e < 4; ++e) acc[e] = fmaf(sum_of[w][lane][e], turn, acc[e]);
+      }
     }
+    if (!real) continue;
+    const float vs = sizeof(C) == 1 && a.v_scale ? a.v_scale[h / a.group] : 1.0f;
+    const float by = l == 0.0f ? 0.0f : vs / l;
+    typename Vec<T>::x2* to = reinterpret_cast<typename Vec<T>::x2*>(static_cast<T*>(a.out) + (uint64_t)tok * a.out_stride + (uint64_t)h * D + at);
+    to[0] = l == 0.0f ? narrow2<T>(0.0f, 0.0f) : narrow2<T>(acc[0] * by, acc[1] * by);
+    to[1] = l == 0.0f ? narrow2<T>(0.0f, 0.0f) : narrow2<T>(acc[2] * by, acc[3] * by);
+    if (a.lse && at == 0u) a.lse[row] = l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2;
   }
-  const float vs = sizeof(C) == 1 && a.v_scale ? a.v_scale[h / a.group] : 1.0f;
-  const float by = l == 0.0f ? 0.0f : vs / l;
-  T* to = static_cast<T*>(a.out) + (uint64_t)tok * a.out_stride + (uint64_t)h * D + lane * kPer;
-#pragma unroll
-  for (int k = 0; k < kPer; ++k) to[k] = (T)(l == 0.0f ? 0.0f : acc[k] * by);
-  if (a.lse && lane == 0) a.lse[row] = l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
 }  // namespace maaso

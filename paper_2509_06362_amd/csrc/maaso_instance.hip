@@ -298,9 +298,14 @@ void launch_attention(AttentionArgs a, hipStream_t s) {
     hipLaunchKernelGGL((attention_stream_kernel<T, C, D>), dim3(a.shared_blocks + a.n * heads * a.own_parts), dim3(256), 0, s, a);
   }
   if (a.part_o) {
-    const uint64_t rows = (uint64_t)a.n_tok * a.n_heads;
-    if (rows < 4096u) hipLaunchKernelGGL((attention_join_kernel<T, C, D, 4>), dim3((uint32_t)rows), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((attention_join_kernel<T, C, D, 1>), dim3((uint32_t)((rows + 3u) / 4u)), dim3(256), 0, s, a);
+    constexpr uint32_t kHeads = 256 / D;  // of a wave
+    const uint32_t groups = (a.n_heads + kHeads - 1u) / kHeads;
+    if ((uint64_t)a.n_tok * groups < 1024u)
+      hipLaunchKernelGGL((attention_join_kernel<T, C, D, 4, 1>), dim3(a.n_tok, groups), dim3(256), 0, s, a);
+    else if (a.n_tok < 1024u)
+      hipLaunchKernelGGL((attention_join_kernel<T, C, D, 1, 1>), dim3(a.n_tok, (groups + 3u) / 4u), dim3(256), 0, s, a);
+    else
+      hipLaunchKernelGGL((attention_join_kernel<T, C, D, 1, 8>), dim3((a.n_tok + 7u) / 8u, (groups + 3u) / 4u), dim3(256), 0, s, a);
   }
 }
 
@@ -412,13 +417,15 @@ int maaso_kv_attention(maaso_instance* inst, const maaso_kv_cache* cache, uint32
   a.own_tiles = (uint32_t)(group_rows / kTileRows + p->n);
   a.shared_tiles = a.n_groups ? (uint32_t)(group_rows / kTileRows + a.n_groups) : 0u;
   const bool tiles = (uint64_t)p->max_q * a.group > kStreamRows, shared_tiles = group_rows > kStreamRows;
-  // Keys are split until there are some four blocks to a compute unit, two of the larger ones.
-  auto chunk_of = [&](uint64_t keys, uint64_t items, uint64_t per_cu) {
-    const uint64_t want = per_cu * (uint64_t)inst->n_cu, parts = items >= want ? 1u : (want + items - 1u) / items;
-    return std::max(256u, round_up((keys + parts - 1u) / parts, 256u));
+  // Keys are split until there are some four blocks to a compute unit, or two of the larger ones; and where there are less
+  // than eight of these to a unit, into parts of no more than 2048 keys, so that long rows end when the others do.
+  auto chunk_of = [&](uint64_t keys, uint64_t items, bool large) {
+    const uint64_t cus = (uint64_t)inst->n_cu, want = large ? 2u * cus : 4u * cus, parts = items >= want ? 1u : (want + items - 1u) / items;
+    const uint32_t chunk = std::max(256u, round_up((keys + parts - 1u) / parts, 256u));
+    return large && items < 8u * cus ? std::min(chunk, 2048u) : chunk;
   };
-  a.own_chunk = chunk_of(p->max_len, (uint64_t)(tiles ? a.own_tiles : p->n) * a.n_kv_heads, tiles ? 2u : 4u);
-  a.shared_chunk = a.n_groups ? chunk_of(a.max_shared, (uint64_t)(shared_tiles ? a.shared_tiles : a.n_groups) * a.n_kv_heads, shared_tiles ? 2u : 4u) : 256u;
+  a.own_chunk = chunk_of(p->max_len, (uint64_t)(tiles ? a.own_tiles : p->n) * a.n_kv_heads, tiles);
+  a.shared_chunk = a.n_groups ? chunk_of(a.max_shared, (uint64_t)(shared_tiles ? a.shared_tiles : a.n_groups) * a.n_kv_heads, shared_tiles) : 256u;
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
   InstanceCall call(inst, s);
   if (call.rc != MAASO_OK) return call.rc;
