@@ -44,17 +44,21 @@ struct AttentionArgs {
   const int32_t* shared;
   uint32_t n, n_tok, n_heads, n_kv_heads, group, n_groups;
   uint32_t n_pages, page_log2, n_rows, width;
-  uint32_t max_q, max_len, max_shared;
-  uint32_t own_chunk, shared_chunk;    // keys of a part, multiples of kStreamKeys
+  uint32_t max_q, max_len, most_shared;  // most_shared: the caller's bound, within max_len and a row's width
+  uint32_t own_least, shared_chunk;    // keys of an own part at least, of a shared one; multiples of 64
   uint32_t own_parts, shared_parts;    // most parts of a row
   uint32_t own_tiles, shared_tiles;    // most tiles of kTileRows rows
   uint32_t shared_blocks;              // of the launch: blocks that take shared parts; those behind them take own ones
+  bool alone;                          // items of few rows: a wave each, not a block
   float scale_log2;
   // workspace, where a row has several parts
   float* part_o;   // [part][n_tok * n_heads][D]
   float* part_ml;  // [part][n_tok * n_heads][2]
   uint32_t* status;
 };
+
+// A value that all lanes of a wave have alike, as one.
+__device__ inline uint32_t uniform(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
 
 // What a sequence or a group has of rows and keys, from the device's arrays; everything within its bounds.
 struct SequenceSpan {
@@ -95,31 +99,25 @@ __device__ inline bool group_good(const AttentionArgs& a, uint32_t g) {
   return false;
 }
 
-// Keys of group g's common part: what the caller says, within the bound and the first sequence's row.
-__device__ inline uint32_t group_keys(const AttentionArgs& a, uint32_t g) {
-  const int32_t v = a.shared[g], f = a.group_start[g];
-  if (v <= 0 || f < 0 || (uint32_t)f >= a.n) return 0u;
-  const int32_t row = a.rows ? a.rows[f] : f;
-  if (row < 0 || (uint32_t)row >= a.n_rows) return 0u;
-  const int32_t len = a.length[row];
-  if (len < 0 || (uint64_t)len > (uint64_t)a.width << a.page_log2) return 0u;
-  const uint32_t most = a.max_shared < a.max_len ? a.max_shared : a.max_len;
-  uint32_t keys = (uint32_t)v < (uint32_t)len ? (uint32_t)v : (uint32_t)len;
-  if (keys < (uint32_t)v || keys > most) raise(a.status, MAASO_INST_BAD_BOUND);
-  return keys < most ? keys : most;
-}
-
-// Tokens that sequence i begins with like its group, 0 outside every group.
+// Tokens that sequence i begins with like its group, as far as the caller's bound and a row's width go; 0 outside every
+// group.  All lanes of the wave have the same i: 64 groups are looked at in one go, for every load in a row of loads that
+// wait for each other is a microsecond of a short item.
 __device__ inline uint32_t shared_of(const AttentionArgs& a, uint32_t i) {
-  if (a.n_groups == 0u || a.max_shared == 0u) return 0u;
-  uint32_t lo = 0, hi = a.n_groups;
-  while (hi - lo > 1u) {
-    const uint32_t mid = (lo + hi) >> 1;
-    if (a.group_start[mid] <= (int32_t)i) lo = mid; else hi = mid;
+  const uint32_t lane = threadIdx.x & 63u;
+  uint32_t found = 0;
+  for (uint32_t base = 0; base < a.n_groups; base += 64u) {
+    const uint32_t g = base + lane < a.n_groups ? base + lane : a.n_groups - 1u;
+    const int32_t f = a.group_start[g], e = a.group_start[g + 1u], v = a.shared[g];
+    const bool in = f >= 0 && f <= (int32_t)i && e > (int32_t)i && (uint32_t)e <= a.n;
+    const uint64_t which = __ballot(in);
+    if (which) {
+      const int32_t keys = __shfl(v, __builtin_ctzll(which));
+      if (keys < 0 || (uint32_t)keys > a.most_shared) raise(a.status, MAASO_INST_BAD_BOUND);
+      found = keys < 0 ? 0u : (uint32_t)keys < a.most_shared ? (uint32_t)keys : a.most_shared;
+      break;
+    }
   }
-  const int32_t f = a.group_start[lo], e = a.group_start[lo + 1];
-  if (f < 0 || f > (int32_t)i || e <= (int32_t)i || (uint32_t)e > a.n) return 0u;
-  return group_keys(a, lo);
+  return found;
 }
 
 // The sequence of token t: the last one that begins at t or before.
@@ -171,25 +169,58 @@ struct ItemKeys {
   bool alone;  // its rows have no other part: their results are written as they are, not joined
 };
 
-// Parts of a row: those of its group's keys, those of the sequence's own.
+// The end of an item's keys [begin, end), begin < end, as far as its page list holds pages: a bad entry is not followed, what
+// lies behind it in the item is left out.  All lanes of the wave have the same item; `entries` becomes the list's first 64
+// entries from begin's page on, a lane each.
+__device__ inline uint32_t held_end(const AttentionArgs& a, const int32_t* list, uint32_t begin, uint32_t end, int32_t& entries) {
+  const uint32_t first = begin >> a.page_log2, last = (end - 1u) >> a.page_log2, lane = threadIdx.x & 63u;
+  for (uint32_t page0 = first; page0 <= last; page0 += 64u) {
+    const int32_t page = page0 + lane <= last ? list[page0 + lane] : 0;
+    if (page0 == first) entries = page;
+    const uint64_t bad = __ballot(page < 0 || (uint32_t)page >= a.n_pages);
+    if (bad) {
+      raise(a.status, MAASO_INST_BAD_PAGE);
+      const uint32_t stop = (page0 + (uint32_t)__builtin_ctzll(bad)) << a.page_log2;
+      return stop < begin ? begin : stop;
+    }
+  }
+  return end;
+}
+
+// Parts of a row: those of its group's keys, those of the sequence's own.  The own keys are cut into as many equal parts,
+// of a multiple of 64 keys, as there are at most, but into none below own_least keys.
 struct RowParts {
-  uint32_t n_shared, n_own;
+  uint32_t n_shared, n_own, own_chunk;
 };
 __device__ inline RowParts row_parts(const AttentionArgs& a, uint32_t len, uint32_t shared) {
-  return {(shared + a.shared_chunk - 1u) / a.shared_chunk, len > shared ? (len - shared + a.own_chunk - 1u) / a.own_chunk : 0u};
+  RowParts p{(shared + a.shared_chunk - 1u) / a.shared_chunk, 0u, a.own_least};
+  if (len > shared) {
+    const uint32_t own = len - shared, most = (own + a.own_least - 1u) / a.own_least, parts = most < a.own_parts ? most : a.own_parts;
+    p.own_chunk = ((own + parts - 1u) / parts + 63u) & ~63u;
+    p.n_own = (own + p.own_chunk - 1u) / p.own_chunk;
+  }
+  return p;
 }
 
 // False where there is nothing to do for part `part` of sequence or group `which` from row row0 on.
 __device__ inline bool item_keys(const AttentionArgs& a, bool is_shared, uint32_t which, uint32_t part, uint32_t row0, ItemKeys& k) {
   if (is_shared) {
     const uint32_t f = (uint32_t)a.group_start[which], e = (uint32_t)a.group_start[which + 1];  // (group_good has seen them)
+    const int32_t keys = a.shared[which];
+    const SequenceSpan lead = sequence_span(a, f < a.n ? f : 0u);
     k.tok0 = (uint32_t)a.q_start[f];
     k.n_rows = ((uint32_t)a.q_start[e] - k.tok0) * a.group;
-    k.page_row = a.rows ? (uint32_t)a.rows[f] : f;  // (group_keys has checked it where there are keys)
-    const uint32_t all = group_keys(a, which);
+    k.page_row = lead.row;
+    const uint32_t all = keys < 0 ? 0u : (uint32_t)keys < a.most_shared ? (uint32_t)keys : a.most_shared;
+    if (keys < 0 || (uint32_t)keys > a.most_shared || all > lead.len) raise(a.status, MAASO_INST_BAD_BOUND);
     k.alone = false;
     k.begin = part * a.shared_chunk;
     k.end = k.begin + a.shared_chunk < all ? k.begin + a.shared_chunk : all;
+    // (each part of `all` is written, whatever the first row holds of it: the join counts them)
+    if (k.begin >= k.end || k.n_rows == 0u) return false;
+    k.end = k.end < lead.len ? k.end : lead.len;
+    k.end = k.end < k.begin ? k.begin : k.end;
+    return row0 < k.n_rows;
   } else {
     const SequenceSpan s = sequence_span(a, which);
     k.tok0 = s.tok0;
@@ -200,9 +231,9 @@ __device__ inline bool item_keys(const AttentionArgs& a, bool is_shared, uint32_
     const uint32_t shared = shared_of(a, which);
     const RowParts parts = row_parts(a, s.len, shared);
     k.alone = parts.n_shared + parts.n_own <= 1u && parts.n_shared == 0u;
-    const uint64_t b = (uint64_t)shared + (uint64_t)part * a.own_chunk;
+    const uint64_t b = (uint64_t)shared + (uint64_t)part * parts.own_chunk;
     k.begin = b < s.len ? (uint32_t)b : s.len;
-    k.end = s.len - k.begin < a.own_chunk ? s.len : k.begin + a.own_chunk;
+    k.end = s.len - k.begin < parts.own_chunk ? s.len : k.begin + parts.own_chunk;
   }
   // Without keys there is nothing to join; rows without any are written all the same, by the first part.
   if (k.begin >= k.end) {
@@ -236,13 +267,25 @@ template <typename V> __device__ inline bool finite16(V v) {
   return f;
 }
 
-// Keys [begin, end) of page list `list` against one tile of rows, by this wave's steps begin + (step0 + i * stride) * 32.
+// One tile of rows against this wave's steps of 32 keys.  First the steps that not all rows see in full, if there are any,
+// then the others, of which the next one's keys and values are asked for before this one's are multiplied: two steps' loads
+// are always under way.
 template <typename T, typename C, int D>
 struct StreamTile {
   using X8 = typename Vec<T>::x8;
+  using L = KeyLoad<T, C>;
+  struct Step {
+    typename L::raw k0[D / 32], k1[D / 32], v[D / 16];
+  };
   X8 q[D / 32];
   f32x4 o[D / 16];
-  float m, l;
+  float m, l, scale;
+  const C* kp;  // the head's
+  const C* vp;
+  const int32_t* list;
+  uint32_t begin, end, limit, lowest;  // keys of the item; those that this lane's row sees; the least that any row sees
+  int32_t entries;                     // the page list's, 64 of them from entry0 on, a lane each
+  uint32_t entry0;
 
   __device__ inline void clear() {
 #pragma unroll
@@ -251,134 +294,187 @@ struct StreamTile {
     l = 0.0f;
   }
 
-  // limit: keys that this lane's row sees; lowest, highest: over all rows of the tile
-  __device__ inline void run(const AttentionArgs& a, const int32_t* list, uint32_t head, float scale, uint32_t begin, uint32_t end,
-                             uint32_t first, uint32_t stride, uint32_t limit, uint32_t lowest) {
-    using L = KeyLoad<T, C>;
+  // The keys from `base` on, a multiple of 32: two pages at most.
+  __device__ inline void ask(const AttentionArgs& a, Step& s, uint32_t base) {
     const uint32_t lane = threadIdx.x & 63u, col = lane & 15u, g = lane >> 4, per = 1u << a.page_log2;
-    const C* kp = reinterpret_cast<const C*>(a.k_pages) + ((uint64_t)head << a.page_log2) * D;
-    const C* vp = reinterpret_cast<const C*>(a.v_pages) + ((uint64_t)head << a.page_log2) * D;
-    for (uint32_t base = (begin & ~(kStreamKeys - 1u)) + first * kStreamKeys; base < end; base += stride * kStreamKeys) {
-      const uint32_t key8 = base + 8u * g;  // this lane's eight keys of the second product
-      int32_t page = 0;
-      bool held = false;
-      if (key8 < end && key8 + 8u > begin) {
-        page = list[key8 >> a.page_log2];
-        held = page >= 0 && (uint32_t)page < a.n_pages;
-        if (!held) { page = 0; raise(a.status, MAASO_INST_BAD_PAGE); }
-      }
-      const int from = (int)((col >> 2) << 4);
-      const int32_t kpage = __shfl(page, from);
-      const uint32_t row = (base + 8u * (col >> 2) + (col & 3u)) & (per - 1u);
-      const C* kr = kp + (uint64_t)(uint32_t)kpage * a.page_stride + (uint64_t)row * D + g * 8u;
-      const C* vr = vp + (uint64_t)(uint32_t)page * a.page_stride + (key8 & (per - 1u)) + ((uint64_t)col << a.page_log2);
-      typename L::raw kr0[D / 32], kr1[D / 32], vv[D / 16];
+    const uint32_t last = (end - 1u) >> a.page_log2, page_at = base >> a.page_log2;
+    if (page_at - entry0 >= 63u) {
+      entry0 = page_at;
+      entries = entry0 + lane <= last ? list[entry0 + lane] : 0;
+    }
+    const int32_t at = (int32_t)uniform(page_at - entry0);
+    const uint32_t page0 = (uint32_t)__builtin_amdgcn_readlane(entries, at);
+    const uint32_t page1 = (uint32_t)__builtin_amdgcn_readlane(entries, per < 32u ? at + 1 : at);
+    const uint32_t kpage = col >> 3 ? page1 : page0, vpage = g >> 1 ? page1 : page0;
+    const uint32_t row = (base + 8u * (col >> 2) + (col & 3u)) & (per - 1u);
+    const C* kr = kp + (uint64_t)kpage * a.page_stride + row * (uint32_t)D + g * 8u;
+    const C* vr = vp + (uint64_t)vpage * a.page_stride + ((base + 8u * g) & (per - 1u)) + (col << a.page_log2);
 #pragma unroll
-      for (int s = 0; s < D / 32; ++s) {
-        kr0[s] = *reinterpret_cast<const typename L::raw*>(kr + s * 32);
-        kr1[s] = *reinterpret_cast<const typename L::raw*>(kr + 4 * D + s * 32);
-      }
+    for (int t = 0; t < D / 32; ++t) {
+      s.k0[t] = *reinterpret_cast<const typename L::raw*>(kr + t * 32);
+      s.k1[t] = *reinterpret_cast<const typename L::raw*>(kr + 4 * D + t * 32);
+    }
 #pragma unroll
-      for (int d = 0; d < D / 16; ++d) vv[d] = *reinterpret_cast<const typename L::raw*>(vr + ((uint64_t)(d * 16) << a.page_log2));
-      f32x4 s0 = {0.0f, 0.0f, 0.0f, 0.0f}, s1 = s0;
+    for (int d = 0; d < D / 16; ++d) {
+      s.v[d] = *reinterpret_cast<const typename L::raw*>(vr);
+      vr += 16u << a.page_log2;
+      asm volatile("" : "+v"(vr));  // (one address, moved on)
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+
+  __device__ inline void scores(const Step& s, float (&x)[8]) const {
+    f32x4 s0 = {0.0f, 0.0f, 0.0f, 0.0f}, s1 = s0;
 #pragma unroll
-      for (int s = 0; s < D / 32; ++s) {
-        s0 = mfma_16x16x32(L::wide(kr0[s]), q[s], s0);
-        s1 = mfma_16x16x32(L::wide(kr1[s]), q[s], s1);
-      }
-      float x[8];
-      const bool inner = base >= begin && base + kStreamKeys <= lowest && base + kStreamKeys <= end;
+    for (int t = 0; t < D / 32; ++t) {
+      s0 = mfma_16x16x32(L::wide(s.k0[t]), q[t], s0);
+      s1 = mfma_16x16x32(L::wide(s.k1[t]), q[t], s1);
+    }
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        x[k] = s0[k] * scale;
-        x[k + 4] = s1[k] * scale;
-      }
-      const bool plain = inner && __all(held);
-      if (!plain) {
+    for (int k = 0; k < 4; ++k) {
+      x[k] = s0[k] * scale;
+      x[k + 4] = s1[k] * scale;
+    }
+  }
+
+  __device__ inline X8 weights(const float (&x)[8]) {
+    float top = x[0];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const uint32_t key = key8 + k;
-          if (!held || key < begin || key >= end || key >= limit) x[k] = -INFINITY;
-        }
-      }
-      float top = x[0];
-#pragma unroll
-      for (int k = 1; k < 8; ++k) top = fmaxf(top, x[k]);
+    for (int k = 1; k < 8; ++k) top = fmaxf(top, x[k]);
+    // The maximum follows only where it has grown by more than 8 (weights up to 256 are as exact as up to 1); else the sums
+    // need not be scaled, and the lanes of a row need not hear of each other.
+    if (__any(top > m + 8.0f)) {
       top = fmaxf(top, __shfl_xor(top, 16));
       top = fmaxf(top, __shfl_xor(top, 32));
-      const float now = fmaxf(m, top), zero = now == -INFINITY ? 0.0f : now;
-      const float turn = __builtin_amdgcn_exp2f(m - zero);
-      float p[8], sum = 0.0f;
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        p[k] = __builtin_amdgcn_exp2f(x[k] - zero);
-        sum += p[k];
-      }
-      l = fmaf(l, turn, sum);
+      const float now = fmaxf(m, top), turn = __builtin_amdgcn_exp2f(m - (now == -INFINITY ? 0.0f : now));
+      l *= turn;
       m = now;
 #pragma unroll
       for (int d = 0; d < D / 16; ++d) o[d] = o[d] * turn;
-      const X8 w = narrow8<T>(p);
-      X8 v[D / 16];
+    }
+    const float zero = m == -INFINITY ? 0.0f : m;
+    float p[8], sum = 0.0f;
 #pragma unroll
-      for (int d = 0; d < D / 16; ++d) v[d] = L::wide(vv[d]);
-      if (!plain) {
-        // Keys that no row sees: zeros, whatever their place holds.
-        bool odd = false;
+    for (int k = 0; k < 8; ++k) {
+      p[k] = __builtin_amdgcn_exp2f(x[k] - zero);
+      sum += p[k];
+    }
+    l += sum;
+    return narrow8<T>(p);
+  }
+
+  // Keys that every row sees.
+  __device__ inline void take(const Step& s) {
+    float x[8];
+    scores(s, x);
+    const X8 w = weights(x);
 #pragma unroll
-        for (int d = 0; d < D / 16; ++d) {
+    for (int d = 0; d < D / 16; ++d) o[d] = mfma_16x16x32(L::wide(s.v[d]), w, o[d]);
+  }
+
+  // Keys of which some are not of the item, or not seen by all rows.
+  __device__ inline void take_some(Step& s, uint32_t base) {
+    const uint32_t lane = threadIdx.x & 63u, col = lane & 15u, key8 = base + 8u * (lane >> 4);
+    float x[8];
+    scores(s, x);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const uint32_t key = key8 + k;
-            if (!held || key < begin || key >= end) v[d][k] = (T)0.0f;
-          }
-          odd = odd || !finite16(v[d]);
-        }
-        if (__any(odd)) {
-          // A value that is not finite, which some rows see and others do not: row by row.
-          for (int r = 0; r < 16; ++r) {
-            const uint32_t sees = __shfl(limit, r);
+    for (int k = 0; k < 8; ++k)
+      if (key8 + k < begin || key8 + k >= end || key8 + k >= limit) x[k] = -INFINITY;
+    const X8 w = weights(x);
+    // Values of keys that no row sees are taken as zeros, whatever their place holds; where one that some rows may see and others
+    // not is not finite, row by row.
+    auto value = [&](int d, uint32_t sees) {
+      asm volatile("" : "+v"(s.v[d]));  // (one after the other, and each from anew: registers are few)
+      X8 v = L::wide(s.v[d]);
 #pragma unroll
-            for (int d = 0; d < D / 16; ++d) {
-              X8 vr1 = v[d];
+      for (int k = 0; k < 8; ++k)
+        if (key8 + k < begin || key8 + k >= sees) v[k] = (T)0.0f;
+      return v;
+    };
+    bool odd = false;
 #pragma unroll
-              for (int k = 0; k < 8; ++k)
-                if (key8 + k >= sees) vr1[k] = (T)0.0f;
-              const f32x4 t = mfma_16x16x32(vr1, w, o[d]);
-              if (col == (uint32_t)r) o[d] = t;
-            }
-          }
-          continue;
-        }
+    for (int d = 0; d < D / 16; ++d) odd = odd || !finite16(value(d, end));
+    if (!__any(odd)) {
+#pragma unroll
+      for (int d = 0; d < D / 16; ++d) o[d] = mfma_16x16x32(value(d, end), w, o[d]);
+      return;
+    }
+#pragma unroll 1
+    for (int r = 0; r < 16; ++r) {
+      const uint32_t most = __shfl(limit, r), sees = most < end ? most : end;
+#pragma unroll
+      for (int d = 0; d < D / 16; ++d) {
+        const f32x4 t = mfma_16x16x32(value(d, sees), w, o[d]);
+        if (col == (uint32_t)r) o[d] = t;
       }
-#pragma unroll
-      for (int d = 0; d < D / 16; ++d) o[d] = mfma_16x16x32(v[d], w, o[d]);
+    }
+  }
+
+  // This wave's steps, one of every kSplit.
+  template <uint32_t kSplit>
+  __device__ inline void run(const AttentionArgs& a, uint32_t wave) {
+    constexpr uint32_t kStride = 32u * kSplit;
+    end = uniform(held_end(a, list, begin, end, entries));
+    entry0 = begin >> a.page_log2;
+    if (begin >= end) return;
+    const uint32_t whole0 = (begin + 31u) & ~31u, seen = lowest < end ? lowest : end;
+    const uint32_t whole1 = (seen & ~31u) > whole0 ? seen & ~31u : whole0;  // [whole0, whole1): steps that all rows see in full
+    const uint32_t before = begin < whole0 && begin / 32u < (end + 31u) / 32u ? 1u : 0u;
+    const uint32_t others = before + (end > whole1 ? (end - whole1 + 31u) / 32u : 0u);
+    // (the last waves have the fewest whole steps)
+#pragma unroll 1
+    for (uint32_t n = kSplit - 1u - wave; n < others; n += kSplit) {
+      const uint32_t at = n < before ? begin & ~31u : whole1 + (n - before) * 32u;
+      Step s;
+      ask(a, s, at);
+      take_some(s, at);
+    }
+    uint32_t base = whole0 + wave * 32u;
+    if constexpr (sizeof(Step) > 256u) {  // (two of them are more than the registers hold)
+#pragma unroll 1
+      for (; base < whole1; base += kStride) {
+        Step s;
+        ask(a, s, base);
+        take(s);
+      }
+      return;
+    }
+    if (base >= whole1) return;
+    Step s0, s1;
+    ask(a, s0, base);
+    for (;;) {
+      base += kStride;
+      if (base >= whole1) { take(s0); return; }
+      ask(a, s1, base);
+      take(s0);
+      base += kStride;
+      if (base >= whole1) { take(s1); return; }
+      ask(a, s0, base);
+      take(s1);
     }
   }
 };
 
-template <typename T, typename C, int D>
-__global__ void __launch_bounds__(256) attention_stream_kernel(AttentionArgs a) {
+// Items of few rows.  kSplit 1: a wave takes an item, alone; kSplit 4: the four waves of a block share an item's keys and join
+// in shared memory, for when there are few items and the parts of a row would be many.
+template <typename T, typename C, int D, int kSplit>
+__global__ void __launch_bounds__(256, 2) attention_stream_kernel(AttentionArgs a) {
   using X8 = typename Vec<T>::x8;
-  constexpr int kPad = D + 4;
-  __shared__ float so[4][16][kPad];
-  __shared__ float sm[4][16], sl[4][16];
-  const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, col = lane & 15u, g = lane >> 4;
-  // block -> (part, head, tile)
-  const bool is_shared = blockIdx.x < a.shared_blocks;
-  uint32_t id = is_shared ? blockIdx.x : blockIdx.x - a.shared_blocks;
+  const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6), col = lane & 15u, g = lane >> 4;
+  // item -> (part, head, sequence or group)
+  uint32_t id = kSplit == 1 ? blockIdx.x * 4u + wave : blockIdx.x;
+  const bool is_shared = id < a.shared_blocks;
+  if (!is_shared) id -= a.shared_blocks;
   const uint32_t head = id % a.n_kv_heads;
   id /= a.n_kv_heads;
-  const uint32_t count = is_shared ? a.n_groups : a.n, which = id % count, part = id / count, row0 = 0;
+  const uint32_t count = is_shared ? a.n_groups : a.n, which = id % count, part = id / count;
+  if (!is_shared && part >= a.own_parts) return;  // (the last block's waves)
   if (is_shared && !group_good(a, which)) return;
   ItemKeys keys;
-  if (!item_keys(a, is_shared, which, part, row0, keys) || keys.n_rows > kStreamRows) return;
-  const bool direct = keys.alone;
-  const uint32_t tok0 = keys.tok0, n_rows = keys.n_rows, begin = keys.begin;
-  uint32_t end = keys.end;
-  const uint32_t r = row0 + col;
-  const bool real = r < n_rows;
-  const uint32_t tok = tok0 + (real ? r : row0) / a.group, h = head * a.group + (real ? r : row0) % a.group;
+  if (!item_keys(a, is_shared, which, part, 0u, keys) || keys.n_rows > kStreamRows) return;
+  const uint32_t n_rows = keys.n_rows;
+  const bool real = col < n_rows;
+  const uint32_t tok = keys.tok0 + (real ? col : 0u) / a.group, h = head * a.group + (real ? col : 0u) % a.group;
   const uint32_t limit = row_limit(a, is_shared, keys, tok);
   uint32_t lowest = limit, highest = limit;
 #pragma unroll
@@ -387,52 +483,82 @@ __global__ void __launch_bounds__(256) attention_stream_kernel(AttentionArgs a) 
     lowest = x < lowest ? x : lowest;
     highest = y > highest ? y : highest;
   }
-  if (end > highest) end = highest;
   StreamTile<T, C, D> st;
   const T* qp = static_cast<const T*>(a.q) + (uint64_t)tok * a.q_stride + (uint64_t)h * D + g * 8u;
 #pragma unroll
   for (int s = 0; s < D / 32; ++s) st.q[s] = *reinterpret_cast<const X8*>(qp + s * 32);
   st.clear();
-  const float scale = a.scale_log2 * (sizeof(C) == 1 && a.k_scale ? a.k_scale[head] : 1.0f);
-  if (begin < end)
-    st.run(a, a.table + (uint64_t)keys.page_row * a.width, head, scale, begin, end, wave, 4u, limit, lowest);
-  // join the waves
+  st.kp = reinterpret_cast<const C*>(a.k_pages) + ((uint64_t)head << a.page_log2) * D;
+  st.vp = reinterpret_cast<const C*>(a.v_pages) + ((uint64_t)head << a.page_log2) * D;
+  st.list = a.table + (uint64_t)keys.page_row * a.width;
+  st.begin = uniform(keys.begin);
+  st.end = uniform(keys.end < highest ? keys.end : highest);
+  st.limit = limit;
+  st.lowest = uniform(lowest);
+  st.scale = a.scale_log2 * (sizeof(C) == 1 && a.k_scale ? a.k_scale[head] : 1.0f);
+  if (st.begin < st.end) st.template run<kSplit>(a, kSplit == 1 ? 0u : wave);
   float l = st.l;
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
-  if (g == 0) { sm[wave][col] = st.m; sl[wave][col] = l; }
-  __syncthreads();
-  float top = -INFINITY;
+  const float vs = sizeof(C) == 1 && a.v_scale ? a.v_scale[head] : 1.0f;
+  const uint64_t slot0 = (uint64_t)(is_shared ? part : a.shared_parts + part) * a.n_tok * a.n_heads;
+  if constexpr (kSplit == 1) {
+    if (!real) return;
+    const uint64_t row = (uint64_t)tok * a.n_heads + h;
+    if (keys.alone) {
+      const float by = l == 0.0f ? 0.0f : vs / l;
+      T* to = static_cast<T*>(a.out) + (uint64_t)tok * a.out_stride + (uint64_t)h * D + 4u * g;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) top = fmaxf(top, sm[w][col]);
-  const float turn = __builtin_amdgcn_exp2f(st.m - (top == -INFINITY ? 0.0f : top));
+      for (int d = 0; d < D / 16; ++d) {
+        const f32x4 y = l == 0.0f ? (f32x4){0.0f, 0.0f, 0.0f, 0.0f} : st.o[d] * by;
+        typename Vec<T>::x2* at = reinterpret_cast<typename Vec<T>::x2*>(to + d * 16);
+        at[0] = narrow2<T>(y[0], y[1]);
+        at[1] = narrow2<T>(y[2], y[3]);
+      }
+      if (a.lse && g == 0u) a.lse[row] = l == 0.0f ? -INFINITY : (st.m + log2f(l)) * kLn2;
+    } else {
+      float* to = a.part_o + (slot0 + row) * D + 4u * g;
 #pragma unroll
-  for (int d = 0; d < D / 16; ++d) *reinterpret_cast<f32x4*>(&so[wave][col][d * 16 + 4 * g]) = st.o[d] * turn;
-  __syncthreads();
-  const uint32_t orow = threadIdx.x >> 4, at = (threadIdx.x & 15u) * (D / 16);
-  if (row0 + orow >= n_rows) return;
-  float mm = -INFINITY, ll = 0.0f;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) mm = fmaxf(mm, sm[w][orow]);
-  const float zero = mm == -INFINITY ? 0.0f : mm;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) ll += sl[w][orow] * __builtin_amdgcn_exp2f(sm[w][orow] - zero);
-  float acc[D / 16];
-#pragma unroll
-  for (int k = 0; k < D / 16; ++k) acc[k] = (so[0][orow][at + k] + so[1][orow][at + k]) + (so[2][orow][at + k] + so[3][orow][at + k]);
-  const uint32_t otok = tok0 + (row0 + orow) / a.group, oh = head * a.group + (row0 + orow) % a.group;
-  if (direct) {
-    const float vs = sizeof(C) == 1 && a.v_scale ? a.v_scale[head] : 1.0f;
-    const float by = ll == 0.0f ? 0.0f : vs / ll;
-    T* to = static_cast<T*>(a.out) + (uint64_t)otok * a.out_stride + (uint64_t)oh * D + at;
-#pragma unroll
-    for (int k = 0; k < D / 16; ++k) to[k] = (T)(ll == 0.0f ? 0.0f : acc[k] * by);
-    if (a.lse && at == 0) a.lse[(uint64_t)otok * a.n_heads + oh] = ll == 0.0f ? -INFINITY : (mm + log2f(ll)) * kLn2;
+      for (int d = 0; d < D / 16; ++d) *reinterpret_cast<f32x4*>(to + d * 16) = st.o[d];
+      if (g == 0u) *reinterpret_cast<f32x2*>(a.part_ml + (slot0 + row) * 2) = (f32x2){st.m, l};
+    }
   } else {
-    const uint64_t slot = (uint64_t)(is_shared ? part : a.shared_parts + part) * a.n_tok * a.n_heads + (uint64_t)otok * a.n_heads + oh;
+    // join the waves
+    __shared__ float so[4][16][D + 4];
+    __shared__ float sm[4][16], sl[4][16];
+    if (g == 0) { sm[wave][col] = st.m; sl[wave][col] = l; }
+    __syncthreads();
+    float top = -INFINITY;
 #pragma unroll
-    for (int k = 0; k < D / 16; ++k) a.part_o[slot * D + at + k] = acc[k];
-    if (at == 0) { a.part_ml[slot * 2] = mm; a.part_ml[slot * 2 + 1] = ll; }
+    for (int w = 0; w < 4; ++w) top = fmaxf(top, sm[w][col]);
+    const float turn = __builtin_amdgcn_exp2f(st.m - (top == -INFINITY ? 0.0f : top));
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d) *reinterpret_cast<f32x4*>(&so[wave][col][d * 16 + 4 * g]) = st.o[d] * turn;
+    __syncthreads();
+    const uint32_t orow = threadIdx.x >> 4, at = (threadIdx.x & 15u) * (D / 16);
+    if (orow >= n_rows) return;
+    float mm = -INFINITY, ll = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) mm = fmaxf(mm, sm[w][orow]);
+    const float zero = mm == -INFINITY ? 0.0f : mm;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) ll += sl[w][orow] * __builtin_amdgcn_exp2f(sm[w][orow] - zero);
+    float acc[D / 16];
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) acc[k] = (so[0][orow][at + k] + so[1][orow][at + k]) + (so[2][orow][at + k] + so[3][orow][at + k]);
+    const uint32_t otok = keys.tok0 + orow / a.group, oh = head * a.group + orow % a.group;
+    const uint64_t row = (uint64_t)otok * a.n_heads + oh;
+    if (keys.alone) {
+      const float by = ll == 0.0f ? 0.0f : vs / ll;
+      T* to = static_cast<T*>(a.out) + (uint64_t)otok * a.out_stride + (uint64_t)oh * D + at;
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k) to[k] = (T)(ll == 0.0f ? 0.0f : acc[k] * by);
+      if (a.lse && at == 0) a.lse[row] = ll == 0.0f ? -INFINITY : (mm + log2f(ll)) * kLn2;
+    } else {
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k) a.part_o[(slot0 + row) * D + at + k] = acc[k];
+      if (at == 0) *reinterpret_cast<f32x2*>(a.part_ml + (slot0 + row) * 2) = (f32x2){mm, ll};
+    }
   }
 }
 
@@ -588,7 +714,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attention_tile_kernel(A
   const uint32_t low2 = lowest_of[0] < lowest_of[1] ? lowest_of[0] : lowest_of[1], low3 = lowest_of[2] < lowest_of[3] ? lowest_of[2] : lowest_of[3];
   const uint32_t block_lowest = low2 < low3 ? low2 : low3;
   // A sequence's rows see more with every token: what the block's last row sees is the end.
-  const uint32_t begin = keys.begin;
+  const uint32_t begin = uniform(keys.begin);
   uint32_t end = keys.end;
   if (!is_shared) {
     const uint32_t last = row0 + kTileRows < keys.n_rows ? row0 + kTileRows - 1u : keys.n_rows - 1u;
@@ -635,23 +761,20 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attention_tile_kernel(A
   tile.kp = reinterpret_cast<const C*>(a.k_pages) + ((uint64_t)head << a.page_log2) * D;
   tile.vp = reinterpret_cast<const C*>(a.v_pages) + ((uint64_t)head << a.page_log2) * D;
   const int32_t* list = a.table + (uint64_t)keys.page_row * a.width;
-  // The table's entry for keys at + 8 (lane % (kKeys / 8)); then the page, 0 where there is none, and which keys have one.
+  if (begin < end) {
+    int32_t unused;
+    end = uniform(held_end(a, list, begin, end, unused));
+  }
+  // The table's entry for keys at + 8 (lane % (kKeys / 8)), 0 outside the item.
   auto entry_at = [&](uint32_t at) {
     const uint32_t key8 = at + 8u * (lane % (kKeys / 8));
-    return key8 < end && (key8 | 15u) >= begin ? list[key8 >> a.page_log2] : -1;  // (a wave's key rows go by the page of the first of sixteen)
-  };
-  auto page_of = [&](int32_t entry, uint32_t at, uint32_t& good) {
-    const bool held = entry >= 0 && (uint32_t)entry < a.n_pages;
-    const uint32_t key8 = at + 8u * (lane % (kKeys / 8));
-    if (!held && key8 < end && (key8 | 15u) >= begin) raise(a.status, MAASO_INST_BAD_PAGE);
-    good = (uint32_t)__ballot(held) & ((1u << (kKeys / 8)) - 1u);
-    return held ? entry : 0;
+    return key8 < end && (key8 | 15u) >= begin ? list[key8 >> a.page_log2] : 0;  // (a wave's key rows go by the page of the first of sixteen)
   };
   const uint32_t first = begin & ~(uint32_t)(kKeys - 1);
-  uint32_t good = 0, buffer = 0;
-  int32_t entry = -1;
+  uint32_t buffer = 0;
+  int32_t entry = 0;
   if (begin < end) {
-    tile.bring(0, first, page_of(entry_at(first), first, good));
+    tile.bring(0, first, entry_at(first));
     tile.settle(0);
     entry = entry_at(first + kKeys);
   }
@@ -660,14 +783,13 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attention_tile_kernel(A
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     const bool more = base + kKeys < end;
-    const uint32_t good_now = good;
     if (more) {
-      tile.bring(buffer ^ 1u, base + kKeys, page_of(entry, base + kKeys, good));
+      tile.bring(buffer ^ 1u, base + kKeys, entry);
       entry = entry_at(base + 2 * kKeys);
     }
     // Keys of a step that not every row of the block sees.  Values of keys that no row sees become zeros in shared memory,
     // whatever their place holds; where one that some rows see is not finite, the second product is taken row by row.
-    const bool plain = base >= begin && base + kKeys <= block_lowest && base + kKeys <= end && good_now == (1u << (kKeys / 8)) - 1u;
+    const bool plain = base >= begin && base + kKeys <= block_lowest && base + kKeys <= end;
     bool by_row = false;
     if (!plain) {
       bool odd = false;
@@ -676,11 +798,10 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attention_tile_kernel(A
         const uint32_t row = e / (kKeys / 8), piece = e % (kKeys / 8) ^ Tile::fv(row), k0 = base + piece * 8u;
         X8* at = reinterpret_cast<X8*>(lds + buffer * Tile::kBuffer + Tile::kKeyBytes + e * 16u);
         X8 v = *at;
-        const bool none = !(good_now >> piece & 1u);
         bool changed = false;
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-          if (none || k0 + k < begin || k0 + k >= end) { v[k] = (T)0.0f; changed = true; }
+          if (k0 + k < begin || k0 + k >= end) { v[k] = (T)0.0f; changed = true; }
         if (changed) *at = v;
         odd = odd || !finite16(v);
       }
@@ -704,7 +825,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attention_tile_kernel(A
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             const uint32_t at = b * 32 + (e >> 3) * 16 + half * 8u + (e & 7), k = base + at;
-            if (k < begin || k >= lim || !(good_now >> (at >> 3) & 1u)) x[b][e] = -INFINITY;
+            if (k < begin || k >= lim) x[b][e] = -INFINITY;
           }
       }
       float top = x[0][0];
@@ -712,10 +833,11 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attention_tile_kernel(A
       for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
         for (int e = 0; e < 16; ++e) top = fmaxf(top, x[b][e]);
-      top = fmaxf(top, __shfl_xor(top, 32)) * scale;
-      // The maximum follows only where it has grown by more than 8 (weights up to 256 are as exact as up to 1): else the
-      // sums need not be scaled.
+      top *= scale;
+      // The maximum follows only where it has grown by more than 8 (weights up to 256 are as exact as up to 1); else the
+      // sums need not be scaled, and the lanes of a row need not hear of each other.
       if (__any(top > m + 8.0f)) {
+        top = fmaxf(top, __shfl_xor(top, 32));
         const float now = fmaxf(m, top), turn = __builtin_amdgcn_exp2f(m - (now == -INFINITY ? 0.0f : now));
         m = now;
         l *= turn;
@@ -816,13 +938,13 @@ __global__ void __launch_bounds__(256) attention_join_kernel(AttentionArgs a) {
   const uint64_t rows = (uint64_t)a.n_tok * a.n_heads;
   uint32_t known = 0;  // the token behind the last one that `s` and `parts` are of
   SequenceSpan s{0u, 0u, 0u, 0u};
-  RowParts of{0u, 0u};
+  RowParts of{0u, 0u, 0u};
   for (uint32_t tok = blockIdx.x * kTokens; tok < blockIdx.x * kTokens + kTokens && tok < a.n_tok; ++tok) {
     if (tok >= known) {
       const uint32_t i = sequence_of(a, tok);
       s = sequence_span(a, i);
       const bool mine = tok >= s.tok0 && tok - s.tok0 < s.n_q;
-      of = mine ? row_parts(a, s.len, shared_of(a, i)) : RowParts{0u, 0u};
+      of = mine ? row_parts(a, s.len, shared_of(a, i)) : RowParts{0u, 0u, 0u};
       known = mine ? s.tok0 + s.n_q : tok + 1u;
     }
     if (of.n_shared == 0u && of.n_own == 1u) {  // (written already)

@@ -295,7 +295,9 @@ void launch_attention(AttentionArgs a, hipStream_t s) {
   }
   if (!tiles || a.n_groups || (uint64_t)a.n * a.max_q != a.n_tok) {
     a.shared_blocks = a.n_groups * heads * a.shared_parts;
-    hipLaunchKernelGGL((attention_stream_kernel<T, C, D>), dim3(a.shared_blocks + a.n * heads * a.own_parts), dim3(256), 0, s, a);
+    const uint32_t items = a.shared_blocks + a.n * heads * a.own_parts;
+    if (a.alone) hipLaunchKernelGGL((attention_stream_kernel<T, C, D, 1>), dim3((items + 3u) / 4u), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((attention_stream_kernel<T, C, D, 4>), dim3(items), dim3(256), 0, s, a);
   }
   if (a.part_o) {
     constexpr uint32_t kHeads = 256 / D;  // of a wave
@@ -410,28 +412,43 @@ int maaso_kv_attention(maaso_instance* inst, const maaso_kv_cache* cache, uint32
   a.n = p->n; a.n_tok = p->n_tok; a.n_heads = p->n_heads; a.n_kv_heads = cache->n_kv_heads; a.group = p->n_heads / cache->n_kv_heads;
   a.n_groups = p->max_shared ? p->n_groups : 0u;
   a.n_pages = pages->n_pages; a.page_log2 = log2_of(pages->page_size); a.n_rows = pages->n_rows; a.width = pages->width;
-  a.max_q = p->max_q; a.max_len = p->max_len; a.max_shared = a.n_groups ? std::min(p->max_shared, p->max_len) : 0u;
+  a.max_q = p->max_q; a.max_len = p->max_len; a.most_shared = a.n_groups ? (uint32_t)std::min<uint64_t>(std::min(p->max_shared, p->max_len), (uint64_t)pages->width * pages->page_size) : 0u;
   a.scale_log2 = (float)((double)p->scale * 1.4426950408889634);
   a.status = inst->status;
   const uint64_t group_rows = (uint64_t)p->n_tok * a.group;
   a.own_tiles = (uint32_t)(group_rows / kTileRows + p->n);
   a.shared_tiles = a.n_groups ? (uint32_t)(group_rows / kTileRows + a.n_groups) : 0u;
   const bool tiles = (uint64_t)p->max_q * a.group > kStreamRows, shared_tiles = group_rows > kStreamRows;
-  // Keys are split until there are some four blocks to a compute unit, or two of the larger ones; and where there are less
-  // than eight of these to a unit, into parts of no more than 2048 keys, so that long rows end when the others do.
-  auto chunk_of = [&](uint64_t keys, uint64_t items, bool large) {
-    const uint64_t cus = (uint64_t)inst->n_cu, want = large ? 2u * cus : 4u * cus, parts = items >= want ? 1u : (want + items - 1u) / items;
+  // How keys are split.  Many rows: until there are two blocks to a compute unit, and where there are less than eight, into
+  // parts of no more than 2048 keys, so that long rows end when the others do.  Few: so that the keys, as far as the lengths'
+  // sum tells, come to even parts for every place that a unit has, but into none below 256 or 128 keys; a row may be longer
+  // than the others and still be cut as finely.
+  const uint64_t cus = (uint64_t)inst->n_cu, heads = a.n_kv_heads, most_len = std::max(1u, p->max_len);
+  auto split = [&](uint64_t keys, uint64_t items) {
+    const uint64_t want = 2u * cus, parts = items >= want ? 1u : (want + items - 1u) / items;
     const uint32_t chunk = std::max(256u, round_up((keys + parts - 1u) / parts, 256u));
-    return large && items < 8u * cus ? std::min(chunk, 2048u) : chunk;
+    return items < 8u * cus ? std::min(chunk, 2048u) : chunk;
   };
-  a.own_chunk = chunk_of(p->max_len, (uint64_t)(tiles ? a.own_tiles : p->n) * a.n_kv_heads, tiles);
-  a.shared_chunk = a.n_groups ? chunk_of(a.max_shared, (uint64_t)(shared_tiles ? a.shared_tiles : a.n_groups) * a.n_kv_heads, shared_tiles) : 256u;
+  a.alone = p->n * heads >= 4096u;
+  const uint64_t places = (a.alone ? 8u : 4u) * cus;
+  auto even = [&](uint64_t keys) { return std::max(a.alone ? 128u : 256u, round_up(keys * heads / places, 64u)); };
+  if (tiles) {
+    a.own_least = split(most_len, (uint64_t)a.own_tiles * heads);
+    a.own_parts = (uint32_t)((most_len + a.own_least - 1u) / a.own_least);
+  } else {
+    const uint64_t total = p->total_len && p->total_len < p->n * most_len ? p->total_len : p->n * most_len;
+    const uint64_t in_common = (uint64_t)p->n * a.most_shared, own = total > in_common ? total - in_common : p->n;
+    a.own_least = a.alone ? 128u : 256u;
+    const uint64_t chunk = even(own), parts = (most_len + chunk - 1u) / chunk;
+    const uint64_t bound = (2u * own / p->n + a.own_least - 1u) / a.own_least + (places + p->n * heads - 1u) / (p->n * heads);
+    a.own_parts = (uint32_t)std::min(parts, bound);
+  }
+  a.shared_chunk = !a.n_groups ? 256u : shared_tiles ? split(a.most_shared, (uint64_t)a.shared_tiles * heads) : even((uint64_t)a.n_groups * a.most_shared);
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
   InstanceCall call(inst, s);
   if (call.rc != MAASO_OK) return call.rc;
   for (;;) {
-    a.own_parts = std::max(1u, (p->max_len + a.own_chunk - 1u) / a.own_chunk);
-    a.shared_parts = (a.max_shared + a.shared_chunk - 1u) / a.shared_chunk;
+    a.shared_parts = (a.most_shared + a.shared_chunk - 1u) / a.shared_chunk;
     if (a.own_parts + a.shared_parts == 1u) break;
     Carve ws{inst->ws, inst->ws_bytes};
     a.part_ml = ws.take<float>(rows * (a.own_parts + a.shared_parts) * 2u);
@@ -439,8 +456,8 @@ int maaso_kv_attention(maaso_instance* inst, const maaso_kv_cache* cache, uint32
     if (ws.fits) break;
     a.part_o = nullptr;
     if (a.own_parts == 1u && a.shared_parts <= 1u) return MAASO_E_WORKSPACE;
-    // parts twice as long, where there are more of them
-    if (a.own_parts >= a.shared_parts) a.own_chunk *= 2u;
+    // half as many parts, where there are more of them
+    if (a.own_parts >= a.shared_parts) a.own_parts = (a.own_parts + 1u) / 2u;
     else a.shared_chunk *= 2u;
   }
   const uint64_t shared_blocks = (uint64_t)(a.shared_tiles + a.n_groups) * a.n_kv_heads * a.shared_parts;
