@@ -300,7 +300,8 @@ struct StreamTile {
     const uint32_t last = (end - 1u) >> a.page_log2, page_at = base >> a.page_log2;
     if (page_at - entry0 >= 63u) {
       entry0 = page_at;
-      entries = entry0 + lane <= last ? list[entry0 + lane] : 0;
+      const uint32_t page = entry0 + lane;  // (a step may begin a page before the item, where held_end() has not looked)
+      entries = page <= last && page >= begin >> a.page_log2 ? list[page] : 0;
     }
     const int32_t at = (int32_t)uniform(page_at - entry0);
     const uint32_t page0 = (uint32_t)__builtin_amdgcn_readlane(entries, at);

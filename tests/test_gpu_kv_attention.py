@@ -360,3 +360,15 @@ def test_groups_that_do_not_hold(inst, over):
         over["max_len"] = 300
     b.run(inst, **over)
     assert I.maaso_instance_status(inst) & I.BAD_BOUND
+
+
+@pytest.mark.parametrize("shared", [16, 48, 80])
+@pytest.mark.parametrize("n", [5, 600])
+def test_a_member_need_not_name_its_groups_pages(inst, shared, n):
+    """Shared keys are read from the first sequence's row: whatever the others' rows hold there is not followed, also where a
+    step of 32 keys begins a page before a sequence's own keys."""
+    b = Batch([shared + i % 70 for i in range(n)], [1] * n, 8, 8, 64, 16, BF16, groups=[(0, n, shared)])
+    for i in range(1, n):
+        b.table[int(b.rows[i]), :shared // 16] = -1 if i % 2 else 2 ** 31 - 1
+    b.run(inst).check()
+    assert I.maaso_instance_status(inst) == 0
