@@ -8,6 +8,7 @@
 #include <cstdint>
 
 #include "../../include/maaso_instance.h"
+#include "lds_barrier.hpp"
 
 namespace maaso {
 
@@ -121,8 +122,8 @@ __device__ inline bool extend_plan(const ExtendArgs& a, uint32_t* part, uint32_t
       }
     found += sum;
   }
-  if (t == 0 && found < need_all) *bad |= MAASO_INST_NO_PAGES;
-  __syncthreads();
+  if (t == 0 && found < need_all) atomicOr(bad, MAASO_INST_NO_PAGES);
+  lds_atomics_barrier();
   if (t == 0 && *bad) raise(a.p.status, *bad);
   return *bad == 0u;
 }
@@ -177,9 +178,20 @@ __device__ inline void extend_apply(const ExtendArgs& a, bool ok, uint32_t t, ui
   }
 }
 
-// Few tokens: all in one block, one launch.
+// Few tokens: all in one block, one launch.  The searches for a page's and a token's row are chains of reads, so what they
+// read lies in shared memory where the rows are no more than the threads.
 __global__ void __launch_bounds__(kPageThreads) extend_kernel(ExtendArgs a) {
   __shared__ uint32_t part[17], bad;
+  __shared__ uint32_t begin[kPageThreads + 1];
+  __shared__ int32_t held[kPageThreads], first[kPageThreads], start[kPageThreads + 1];
+  if (a.n <= kPageThreads) {
+    for (uint32_t i = threadIdx.x; i <= a.n; i += kPageThreads) start[i] = a.q_start[i];
+    a.begin = begin;
+    a.held = held;
+    a.first = first;
+    a.q_start = start;
+  }
+  __syncthreads();
   const bool ok = extend_plan(a, part, &bad);
   __threadfence_block();
   __syncthreads();
@@ -373,16 +385,18 @@ __global__ void __launch_bounds__(256) copy_kernel(CopyArgs a) {
   char* base = (blockIdx.z ? a.v : a.k) + layer * a.layer_stride;
   const uint64_t at = (uint64_t)chunk * kCopyChunk;
   const uint64_t left = a.page_bytes - at;
-  const uint4* src = reinterpret_cast<const uint4*>(base + (uint64_t)from * a.page_stride + at);
-  uint4* dst = reinterpret_cast<uint4*>(base + (uint64_t)to * a.page_stride + at);
-  const uint32_t n = (uint32_t)((left < kCopyChunk ? left : kCopyChunk) / 16u);
-  uint4 r[4];
-#pragma unroll
-  for (uint32_t k = 0; k < 4u; ++k)
-    if (threadIdx.x + k * 256u < n) r[k] = src[threadIdx.x + k * 256u];
-#pragma unroll
-  for (uint32_t k = 0; k < 4u; ++k)
-    if (threadIdx.x + k * 256u < n) dst[threadIdx.x + k * 256u] = r[k];
+  typedef uint32_t piece __attribute__((ext_vector_type(4)));
+  const piece* src = reinterpret_cast<const piece*>(base + (uint64_t)from * a.page_stride + at) + threadIdx.x;
+  piece* dst = reinterpret_cast<piece*>(base + (uint64_t)to * a.page_stride + at) + threadIdx.x;
+  if (left >= kCopyChunk) {
+    const piece r0 = src[0], r1 = src[256], r2 = src[512], r3 = src[768];
+    dst[0] = r0;
+    dst[256] = r1;
+    dst[512] = r2;
+    dst[768] = r3;
+  } else {
+    for (uint32_t e = threadIdx.x; e < (uint32_t)left / 16u; e += 256u, src += 256, dst += 256) *dst = *src;
+  }
 }
 
 }  // namespace maaso

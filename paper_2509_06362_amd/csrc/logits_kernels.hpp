@@ -9,12 +9,28 @@
 #include "../../include/maaso_instance.h"
 #include "element_types.hpp"
 #include "kv_pages_kernels.hpp"
+#include "lds_barrier.hpp"
 
 namespace maaso {
 
-constexpr uint32_t kLogitSlice = 8192;  // tokens of a row that a block takes: their counts fit in 32 KiB of LDS
-constexpr uint32_t kLogitThreads = 512;
+// A block takes a slice of a row, kPieces times eight neighbouring tokens a thread: 4096 tokens where there are rows enough
+// to fill the card (their marks are 16 KiB of LDS, eight blocks to a compute unit), 1024 where there are few.
+constexpr uint32_t kManyThreads = 256, kManyPieces = 2, kFewThreads = 128, kFewPieces = 1;
+constexpr uint32_t kManySlice = 8u * kManyThreads * kManyPieces, kFewSlice = 8u * kFewThreads * kFewPieces;
+constexpr uint32_t kFewRows = 1024;  // rows that the instance keeps a LogitsRow for
+// A token's mark: how often the history has it, and above kCountBits the number of its bias among the row's, from 1 on.  Rows
+// of a longer history or more biases mark a bias by the highest bit alone, and search for it.
+constexpr uint32_t kCountBits = 20, kListed = 512;
 constexpr uint32_t kHasBias = 0x80000000u;
+
+// A row's largest key and how many of its slices are done; zeros between calls.  Rows have cache lines of their own.
+struct __attribute__((aligned(128))) LogitsRow {
+  unsigned long long key;
+  uint32_t done;
+};
+
+// Eight elements at any alignment of an element's: 16-byte accesses all the same.
+template <typename T> struct __attribute__((packed, aligned(2))) Piece { T v[8]; };
 
 struct LogitsArgs {
   const void* logits;
@@ -33,7 +49,8 @@ struct LogitsArgs {
   const int32_t* bias_start;
   const uint32_t* mask;
   const int32_t* mask_row;
-  unsigned long long* best;  // workspace [n][slices]
+  unsigned long long* best;  // workspace [n][slices], many rows
+  LogitsRow* meet;           // [n], few rows
   uint32_t* status;
 };
 
@@ -66,35 +83,55 @@ __device__ inline unsigned long long wave_max(unsigned long long v) {
   return v;
 }
 
-template <typename T, typename O, bool kWide>
-__global__ void __launch_bounds__(kLogitThreads) logits_kernel(LogitsArgs a) {
-  __shared__ uint32_t count[kLogitSlice];
-  __shared__ unsigned long long top[kLogitThreads / 64];
+// y / b rounded once, for eight values, with r = 1 / b rounded once: two corrections of y r by the remainder, which a fused
+// multiply-add gives exactly; the first brings the quotient within one unit of its last place, from where the second rounds
+// it as a division would (Markstein, IBM J. Res. Dev. 34, 1990).  Five operations instead of the division's eleven or so.
+// Magnitudes for which a product or remainder could leave the normal range, zeros, infinities and NaN are divided.
+__device__ inline void divide8(float (&y)[8], float b, float r) {
+  float low = fabsf(y[0]), high = low, sum = y[0];
+#pragma unroll
+  for (int k = 1; k < 8; ++k) {
+    low = fminf(low, fabsf(y[k]));
+    high = fmaxf(high, fabsf(y[k]));
+    sum += y[k];  // (NaN if one is: minimum and maximum pass over it)
+  }
+  if (low >= 0x1p-60f && high <= 0x1p60f && sum == sum) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      float q = y[k] * r;
+      q = fmaf(fmaf(-q, b, y[k]), r, q);
+      y[k] = fmaf(fmaf(-q, b, y[k]), r, q);
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) y[k] = y[k] / b;
+  }
+}
+
+template <typename T, typename O, uint32_t kThreads, uint32_t kPieces>
+__global__ void __launch_bounds__(kThreads) logits_kernel(LogitsArgs a) {
+  constexpr uint32_t kSlice = 8u * kThreads * kPieces;
+  __shared__ __align__(16) uint32_t mark[kSlice];
+  __shared__ float bias[kListed];
+  __shared__ unsigned long long top[kThreads / 64];
   const uint32_t row = blockIdx.x / a.slices, slice = blockIdx.x % a.slices;
-  const uint32_t v0 = slice * kLogitSlice, n = a.vocab - v0 < kLogitSlice ? a.vocab - v0 : kLogitSlice;
+  const uint32_t v0 = slice * kSlice, n = a.vocab - v0 < kSlice ? a.vocab - v0 : kSlice;
+  // The logits are asked for first, and come while the row's history is counted.
+  const T* in = static_cast<const T*>(a.logits) + row * a.stride + v0;
+  Piece<T> raw[kPieces];
+#pragma unroll
+  for (uint32_t p = 0; p < kPieces; ++p) {
+    const uint32_t i0 = (p * kThreads + threadIdx.x) * 8u;
+    if (i0 + 8u <= n) {
+      raw[p] = *reinterpret_cast<const Piece<T>*>(in + i0);
+    } else {
+#pragma unroll
+      for (uint32_t k = 0; k < 8u; ++k) raw[p].v[k] = i0 + k < n ? in[i0 + k] : (T)0.0f;
+    }
+  }
   uint32_t hb, he, bb, be;
   list_part(a.history_start, row, a.n_history, a.status, hb, he);
   list_part(a.bias_start, row, a.n_bias, a.status, bb, be);
-  const bool counts = he > hb || be > bb;
-  if (counts) {
-    for (uint32_t i = threadIdx.x; i < n; i += kLogitThreads) count[i] = 0u;
-    __syncthreads();
-    for (uint32_t i = hb + threadIdx.x; i < he; i += kLogitThreads) {
-      const uint32_t v = (uint32_t)a.history[i];
-      if (v - v0 < n) atomicAdd(&count[v - v0], 1u);
-      else if (v >= a.vocab && slice == 0) raise(a.status, MAASO_INST_BAD_TOKEN);
-    }
-    for (uint32_t i = bb + threadIdx.x; i < be; i += kLogitThreads) {
-      const int32_t v = a.bias_token[i];
-      const bool good = v >= 0 && (uint32_t)v < a.vocab && (i == bb || a.bias_token[i - 1] < v);
-      if (!good) {
-        if (slice == 0) raise(a.status, MAASO_INST_BAD_TOKEN);
-      } else if ((uint32_t)v - v0 < n) {
-        atomicOr(&count[(uint32_t)v - v0], kHasBias);
-      }
-    }
-    __syncthreads();
-  }
   const float rep = a.repetition ? a.repetition[row] : 1.0f, freq = a.frequency ? a.frequency[row] : 0.0f;
   const float pres = a.presence ? a.presence[row] : 0.0f, temp = a.temperature ? a.temperature[row] : 1.0f;
   const uint32_t* bits = nullptr;
@@ -103,69 +140,123 @@ __global__ void __launch_bounds__(kLogitThreads) logits_kernel(LogitsArgs a) {
     if (m >= 0 && (uint32_t)m < a.n_mask) bits = a.mask + (uint64_t)m * a.mask_words;
     else if (m >= 0 && threadIdx.x == 0) raise(a.status, MAASO_INST_BAD_ROW);
   }
-  const T* in = static_cast<const T*>(a.logits) + row * a.stride + v0;
-  O* out = a.out ? static_cast<O*>(a.out) + row * a.out_stride + v0 : nullptr;
-  unsigned long long best = 0ull;
-  for (uint32_t i0 = threadIdx.x * 8u; i0 < n; i0 += kLogitThreads * 8u) {
-    const bool whole = kWide && i0 + 8u <= n;
-    T raw[8];
-    if (whole) {
-      if constexpr (sizeof(T) == 4) {
-        *reinterpret_cast<u32x4*>(raw) = *reinterpret_cast<const u32x4*>(in + i0);
-        *reinterpret_cast<u32x4*>(raw + 4) = *reinterpret_cast<const u32x4*>(in + i0 + 4);
-      } else {
-        *reinterpret_cast<u32x4*>(raw) = *reinterpret_cast<const u32x4*>(in + i0);
+  const bool counts = he > hb || be > bb, listed = he - hb < 1u << kCountBits && be - bb <= kListed;
+  if (counts) {
+#pragma unroll
+    for (uint32_t i = 0; i < kSlice / 4u; i += kThreads) reinterpret_cast<u32x4*>(mark)[i + threadIdx.x] = (u32x4){0u, 0u, 0u, 0u};
+    __syncthreads();
+    for (uint32_t i0 = hb + threadIdx.x; i0 < he; i0 += 4u * kThreads) {  // (he <= 2^31 - 1)
+      uint32_t v[4];
+#pragma unroll
+      for (uint32_t k = 0; k < 4u; ++k) v[k] = i0 + k * kThreads < he ? (uint32_t)a.history[i0 + k * kThreads] : v0;
+#pragma unroll
+      for (uint32_t k = 0; k < 4u; ++k) {
+        if (i0 + k * kThreads >= he) break;
+        if (v[k] - v0 < n) atomicAdd(&mark[v[k] - v0], 1u);
+        else if (v[k] >= a.vocab && slice == 0) raise(a.status, MAASO_INST_BAD_TOKEN);
       }
-    } else {
-      for (uint32_t k = 0; k < 8u; ++k) raw[k] = i0 + k < n ? in[i0 + k] : (T)0.0f;
     }
-    const uint32_t allowed = bits ? bits[(v0 + i0) / 32u] >> (i0 & 31u) : 0xffu;
+    for (uint32_t i = bb + threadIdx.x; i < be; i += kThreads) {
+      const int32_t v = a.bias_token[i];
+      const bool good = v >= 0 && (uint32_t)v < a.vocab && (i == bb || a.bias_token[i - 1] < v);
+      if (listed) bias[i - bb] = a.bias_value[i];
+      if (!good) {
+        if (slice == 0) raise(a.status, MAASO_INST_BAD_TOKEN);
+      } else if ((uint32_t)v - v0 < n) {
+        atomicOr(&mark[(uint32_t)v - v0], listed ? (i - bb + 1u) << kCountBits : kHasBias);
+      }
+    }
+    lds_atomics_barrier();
+  }
+  const bool quick = temp >= 0x1p-30f && temp <= 0x1p30f;
+  const float inverse = 1.0f / temp;
+  O* out = a.out ? static_cast<O*>(a.out) + row * a.out_stride + v0 : nullptr;
+  float best = -INFINITY;
+  uint32_t best_at = 0xffffffffu;  // (none)
+#pragma unroll
+  for (uint32_t p = 0; p < kPieces; ++p) {
+    const uint32_t i0 = (p * kThreads + threadIdx.x) * 8u;
+    if (i0 >= n) break;
     float x[8];
 #pragma unroll
-    for (uint32_t k = 0; k < 8u; ++k) {
-      float y = (float)raw[k];
-      if (counts && i0 + k < n) {
-        const uint32_t c = count[i0 + k];
-        if (c & ~kHasBias) {
-          y = y > 0.0f ? y / rep : y * rep;
-          y = y - (freq * (float)(c & ~kHasBias) + pres);
-        }
-        if (c & kHasBias) {
-          uint32_t lo = bb, hi = be;  // the entry that holds the token (rare: the list is searched)
-          while (hi - lo > 1u) {
-            const uint32_t mid = (lo + hi) >> 1;
-            if (a.bias_token[mid] <= (int32_t)(v0 + i0 + k)) lo = mid; else hi = mid;
+    for (int k = 0; k < 8; ++k) x[k] = (float)raw[p].v[k];
+    if (counts) {
+      const u32x4 c0 = *reinterpret_cast<const u32x4*>(mark + i0), c1 = *reinterpret_cast<const u32x4*>(mark + i0 + 4);
+      if ((c0[0] | c0[1] | c0[2] | c0[3] | c1[0] | c1[1] | c1[2] | c1[3]) != 0u) {
+#pragma unroll
+        for (uint32_t k = 0; k < 8u; ++k) {
+          const uint32_t c = k < 4u ? c0[k & 3u] : c1[k & 3u], times = c & (listed ? (1u << kCountBits) - 1u : ~kHasBias);
+          float y = x[k];
+          if (times) {
+            y = y > 0.0f ? y / rep : y * rep;
+            y = y - (freq * (float)times + pres);
           }
-          if (a.bias_token[lo] == (int32_t)(v0 + i0 + k)) y = y + a.bias_value[lo];
+          if (c != times) {
+            if (listed) {
+              const uint32_t at = c >> kCountBits, most = be - bb;  // (past the last: a token listed twice, out of order)
+              y = y + bias[(at < most ? at : most) - 1u];
+            } else {
+              uint32_t lo = bb, hi = be;  // the entry that holds the token
+              while (hi - lo > 1u) {
+                const uint32_t mid = (lo + hi) >> 1;
+                if (a.bias_token[mid] <= (int32_t)(v0 + i0 + k)) lo = mid; else hi = mid;
+              }
+              if (a.bias_token[lo] == (int32_t)(v0 + i0 + k)) y = y + a.bias_value[lo];
+            }
+          }
+          x[k] = y;
         }
       }
-      y = y / temp;
-      if (!(allowed >> k & 1u)) y = -INFINITY;
-      x[k] = y;
-      if (i0 + k < n && y > -INFINITY) {
-        const unsigned long long key = choice_key(y, v0 + i0 + k);
-        best = key > best ? key : best;
+    }
+    if (quick && temp != 1.0f) {
+      divide8(x, temp, inverse);
+    } else if (temp != 1.0f) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] = x[k] / temp;
+    }
+    const uint32_t allowed = bits ? bits[(v0 + i0) / 32u] >> (i0 & 31u) : 0xffu;
+#pragma unroll
+    for (uint32_t k = 0; k < 8u; ++k) {
+      if (!(allowed >> k & 1u)) x[k] = -INFINITY;
+      if (x[k] > best && i0 + k < n) {  // (ascending tokens: the lowest of equals stays)
+        best = x[k];
+        best_at = v0 + i0 + k;
       }
     }
     if (out) {
-      O o[8];
+      Piece<O> o;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) o[k] = (O)x[k];
-      if (whole) {
-        *reinterpret_cast<u32x4*>(out + i0) = *reinterpret_cast<const u32x4*>(o);
-        if constexpr (sizeof(O) == 4) *reinterpret_cast<u32x4*>(out + i0 + 4) = *reinterpret_cast<const u32x4*>(o + 4);
+      for (int k = 0; k < 8; ++k) o.v[k] = (O)x[k];
+      if (i0 + 8u <= n) {
+        *reinterpret_cast<Piece<O>*>(out + i0) = o;
       } else {
-        for (uint32_t k = 0; k < 8u && i0 + k < n; ++k) out[i0 + k] = o[k];
+#pragma unroll
+        for (uint32_t k = 0; k < 8u; ++k)
+          if (i0 + k < n) out[i0 + k] = o.v[k];
       }
     }
   }
   if (!a.chosen) return;
-  best = wave_max(best);
-  if ((threadIdx.x & 63u) == 0) top[threadIdx.x >> 6] = best;
+  unsigned long long key = wave_max(best_at == 0xffffffffu ? 0ull : choice_key(best, best_at));
+  if ((threadIdx.x & 63u) == 0) top[threadIdx.x >> 6] = key;
   __syncthreads();
-  if (threadIdx.x == 0) {
-    for (uint32_t w = 1; w < kLogitThreads / 64u; ++w) best = top[w] > best ? top[w] : best;
-    a.best[(uint64_t)row * a.slices + slice] = best;
+  if (threadIdx.x != 0) return;
+#pragma unroll
+  for (uint32_t w = 1; w < kThreads / 64u; ++w) key = top[w] > key ? top[w] : key;
+  if (!a.meet) {
+    a.best[(uint64_t)row * a.slices + slice] = key;
+    return;
+  }
+  // The row's last slice writes the choice and leaves zeros.  What is known here of another slice's key is known by atomics
+  // alone: each has had its old value back, so is done, before its block counts itself.
+  LogitsRow* m = a.meet + row;
+  unsigned long long old = atomicMax(&m->key, key);
+  asm volatile("" : "+v"(old)::"memory");
+  __builtin_amdgcn_s_waitcnt(0);
+  if (atomicAdd(&m->done, 1u) == a.slices - 1u) {
+    key = atomicExch(&m->key, 0ull);
+    atomicExch(&m->done, 0u);
+    a.chosen[row] = key ? (int32_t)~(uint32_t)key : -1;
   }
 }
 

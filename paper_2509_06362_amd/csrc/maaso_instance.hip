@@ -20,6 +20,7 @@ struct maaso_instance {
   int device;
   int n_cu;
   uint32_t* status;  // device status word
+  LogitsRow* rows;   // [kFewRows] behind it, zeros between calls
   char* ws;          // device workspace
   size_t ws_bytes;
   // one call at a time, as for maaso_ctx
@@ -63,6 +64,8 @@ struct InstanceCall {
   InstanceCall(const InstanceCall&) = delete;
   InstanceCall& operator=(const InstanceCall&) = delete;
 };
+
+constexpr size_t kOwnBytes = 256u + kFewRows * sizeof(LogitsRow);  // the status word, then the rows
 
 int launched() { return hip_ok(hipGetLastError()) ? MAASO_OK : MAASO_E_HIP; }
 
@@ -133,10 +136,10 @@ int maaso_instance_create(int device, uint64_t workspace_bytes, maaso_instance**
   in->ws_bytes = ((size_t)workspace_bytes + 255) & ~size_t(255);
   int rc = MAASO_OK;
   if (!hip_ok(hipDeviceGetAttribute(&in->n_cu, hipDeviceAttributeMultiprocessorCount, device))) rc = MAASO_E_HIP;
-  if (rc == MAASO_OK && !hip_ok(hipMalloc(reinterpret_cast<void**>(&in->status), 256))) rc = MAASO_E_NOMEM;
+  if (rc == MAASO_OK && !hip_ok(hipMalloc(reinterpret_cast<void**>(&in->status), kOwnBytes))) rc = MAASO_E_NOMEM;
   if (rc == MAASO_OK && !hip_ok(hipMalloc(reinterpret_cast<void**>(&in->ws), in->ws_bytes))) rc = MAASO_E_NOMEM;
   if (rc == MAASO_OK && !hip_ok(hipEventCreateWithFlags(&in->order_ev, hipEventDisableTiming))) rc = MAASO_E_HIP;
-  if (rc == MAASO_OK && (!hip_ok(hipMemset(in->status, 0, 256)) || !hip_ok(hipDeviceSynchronize()))) rc = MAASO_E_HIP;
+  if (rc == MAASO_OK && (!hip_ok(hipMemset(in->status, 0, kOwnBytes)) || !hip_ok(hipDeviceSynchronize()))) rc = MAASO_E_HIP;
   if (rc != MAASO_OK) {
     if (in->order_ev) (void)hipEventDestroy(in->order_ev);
     if (in->ws) (void)hipFree(in->ws);
@@ -145,6 +148,7 @@ int maaso_instance_create(int device, uint64_t workspace_bytes, maaso_instance**
     delete in;
     return rc;
   }
+  in->rows = reinterpret_cast<LogitsRow*>(in->status + 64);
   *out = in;
   return MAASO_OK;
 }
@@ -266,19 +270,16 @@ int maaso_kv_copy(maaso_instance* inst, const maaso_kv_cache* cache, const int32
 namespace {
 
 template <typename T, typename C, int D>
-void launch_append(const AppendArgs& a, uint32_t blocks, bool wide, bool interleaved, hipStream_t s) {
-  const dim3 g(blocks), b(256);
-  if (wide && interleaved) hipLaunchKernelGGL((append_kernel<T, C, D, true, true>), g, b, 0, s, a);
-  else if (wide) hipLaunchKernelGGL((append_kernel<T, C, D, true, false>), g, b, 0, s, a);
-  else if (interleaved) hipLaunchKernelGGL((append_kernel<T, C, D, false, true>), g, b, 0, s, a);
-  else hipLaunchKernelGGL((append_kernel<T, C, D, false, false>), g, b, 0, s, a);
+void launch_append(const AppendArgs& a, uint32_t blocks, bool interleaved, hipStream_t s) {
+  if (interleaved) hipLaunchKernelGGL((append_kernel<T, C, D, true>), dim3(blocks), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((append_kernel<T, C, D, false>), dim3(blocks), dim3(256), 0, s, a);
 }
 
 template <typename T, typename C>
-void launch_append_d(uint32_t d, const AppendArgs& a, uint32_t blocks, bool wide, bool interleaved, hipStream_t s) {
-  if (d == 64u) launch_append<T, C, 64>(a, blocks, wide, interleaved, s);
-  else if (d == 128u) launch_append<T, C, 128>(a, blocks, wide, interleaved, s);
-  else launch_append<T, C, 256>(a, blocks, wide, interleaved, s);
+void launch_append_d(uint32_t d, const AppendArgs& a, uint32_t blocks, bool interleaved, hipStream_t s) {
+  if (d == 64u) launch_append<T, C, 64>(a, blocks, interleaved, s);
+  else if (d == 128u) launch_append<T, C, 128>(a, blocks, interleaved, s);
+  else launch_append<T, C, 256>(a, blocks, interleaved, s);
 }
 
 // Few rows of a sequence or group go through the stream kernel, more through the tile kernel; which, the kernels see
@@ -321,10 +322,10 @@ void launch_attention_d(uint32_t d, const AttentionArgs& a, hipStream_t s) {
 uint32_t round_up(uint64_t x, uint32_t to) { return (uint32_t)((x + to - 1u) / to * to); }
 
 template <typename T, typename O>
-void launch_logits(const LogitsArgs& a, bool wide, hipStream_t s) {
-  const dim3 g(a.n * a.slices), b(kLogitThreads);
-  if (wide) hipLaunchKernelGGL((logits_kernel<T, O, true>), g, b, 0, s, a);
-  else hipLaunchKernelGGL((logits_kernel<T, O, false>), g, b, 0, s, a);
+void launch_logits(const LogitsArgs& a, hipStream_t s) {
+  const dim3 g(a.n * a.slices);
+  if (a.meet) hipLaunchKernelGGL((logits_kernel<T, O, kFewThreads, kFewPieces>), g, dim3(kFewThreads), 0, s, a);
+  else hipLaunchKernelGGL((logits_kernel<T, O, kManyThreads, kManyPieces>), g, dim3(kManyThreads), 0, s, a);
 }
 
 }  // namespace
@@ -349,9 +350,6 @@ int maaso_kv_append(maaso_instance* inst, const maaso_kv_cache* cache, uint32_t 
                         p->k_stride < (uint64_t)cache->n_kv_heads * d || p->v_stride < (uint64_t)cache->n_kv_heads * d))
     return MAASO_E_SHAPE;
   if (p->q == p->q_out && p->n_tok > 1u && p->q_stride != p->q_out_stride) return MAASO_E_INVALID_ARG;
-  const bool wide = aligned(p->q, 16) && aligned(p->k, 16) && aligned(p->v, 16) && aligned(p->q_out, 16) &&
-                    (!p->q_weight || aligned(p->q_weight, 16)) && (!p->k_weight || aligned(p->k_weight, 16)) &&
-                    (p->n_tok == 1u || (p->q_stride % 8u == 0 && p->k_stride % 8u == 0 && p->v_stride % 8u == 0 && p->q_out_stride % 8u == 0));
   const uint64_t size = element_size(cache->type);
   AppendArgs a{};
   a.q = p->q; a.k = p->k; a.v = p->v; a.q_out = p->q_out; a.q_weight = p->q_weight; a.k_weight = p->k_weight;
@@ -366,20 +364,20 @@ int maaso_kv_append(maaso_instance* inst, const maaso_kv_cache* cache, uint32_t 
   a.eps = p->eps;
   a.status = inst->status;
   const bool turned = p->n_tok >= 512u;  // values through shared memory
-  const uint64_t heads = p->n_heads + cache->n_kv_heads * (turned ? 1u : 2u), per = 256u / (d / 8u);
+  const uint64_t heads = p->n_heads + cache->n_kv_heads * (turned ? 1u : 2u), per = 256u / (d / 8u) * kAppendHeads;
   const uint64_t head_blocks = (heads * p->n_tok + per - 1u) / per;
   const uint64_t value_blocks = turned ? (uint64_t)(p->n_tok + kTurnTokens - 1u) / kTurnTokens * cache->n_kv_heads * (d / 64u) : 0u;
   if (head_blocks + value_blocks > 0x7fffffffull) return MAASO_E_SHAPE;
-  a.head_blocks = (uint32_t)head_blocks;
+  a.value_blocks = (uint32_t)value_blocks;
   const uint32_t blocks = (uint32_t)(head_blocks + value_blocks);
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
   InstanceCall call(inst, s);
   if (call.rc != MAASO_OK) return call.rc;
   const bool inter = p->interleaved != 0u;
-  if (p->type == MAASO_BF16 && cache->type == MAASO_BF16) launch_append_d<__bf16, __bf16>(d, a, blocks, wide, inter, s);
-  else if (p->type == MAASO_BF16) launch_append_d<__bf16, E4m3>(d, a, blocks, wide, inter, s);
-  else if (cache->type == MAASO_FP16) launch_append_d<_Float16, _Float16>(d, a, blocks, wide, inter, s);
-  else launch_append_d<_Float16, E4m3>(d, a, blocks, wide, inter, s);
+  if (p->type == MAASO_BF16 && cache->type == MAASO_BF16) launch_append_d<__bf16, __bf16>(d, a, blocks, inter, s);
+  else if (p->type == MAASO_BF16) launch_append_d<__bf16, E4m3>(d, a, blocks, inter, s);
+  else if (cache->type == MAASO_FP16) launch_append_d<_Float16, _Float16>(d, a, blocks, inter, s);
+  else launch_append_d<_Float16, E4m3>(d, a, blocks, inter, s);
   return launched();
 }
 
@@ -484,29 +482,32 @@ int maaso_logits_adjust(maaso_instance* inst, const maaso_logits_args* p, void* 
   if (p->n_history > 0x7fffffffu || p->n_bias > 0x7fffffffu) return MAASO_E_SHAPE;
   LogitsArgs a{};
   a.logits = p->logits; a.out = p->out; a.chosen = p->chosen; a.stride = p->stride; a.out_stride = p->out_stride;
-  a.n = p->n; a.vocab = p->vocab; a.slices = (p->vocab + kLogitSlice - 1u) / kLogitSlice;
+  a.n = p->n; a.vocab = p->vocab; a.slices = (p->vocab + kManySlice - 1u) / kManySlice;
   a.n_history = p->n_history; a.n_bias = p->n_bias; a.n_mask = p->n_mask; a.mask_words = (p->vocab + 31u) / 32u;
   a.repetition = p->repetition; a.frequency = p->frequency; a.presence = p->presence; a.temperature = p->temperature;
   if (p->n_history) { a.history = p->history; a.history_start = p->history_start; }
   if (p->n_bias) { a.bias_token = p->bias_token; a.bias_value = p->bias_value; a.bias_start = p->bias_start; }
   a.mask = p->mask; a.mask_row = p->mask_row;
   a.status = inst->status;
+  // Fewer large slices than eight to a compute unit, which takes as many at once: small ones, whose blocks meet in the
+  // instance's own memory instead of a launch of their own.
+  if (a.n <= kFewRows && (uint64_t)a.n * a.slices < 8u * (uint64_t)inst->n_cu) {
+    a.slices = (p->vocab + kFewSlice - 1u) / kFewSlice;
+    a.meet = inst->rows;
+  }
   if ((uint64_t)a.n * a.slices > 0x7fffffffull) return MAASO_E_SHAPE;
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
   InstanceCall call(inst, s);
   if (call.rc != MAASO_OK) return call.rc;
   Carve ws{inst->ws, inst->ws_bytes};
-  a.best = ws.take<unsigned long long>(a.chosen ? (size_t)a.n * a.slices : 1u);
+  a.best = ws.take<unsigned long long>(a.chosen && !a.meet ? (size_t)a.n * a.slices : 1u);
   if (!ws.fits) return MAASO_E_WORKSPACE;
-  const uint64_t in_size = element_size(p->type), out_size = element_size(p->out_type);
-  const bool wide = aligned(p->logits, 16) && (!p->out || aligned(p->out, 16)) &&
-                    (p->n == 1u || (p->stride * in_size % 16u == 0 && (!p->out || p->out_stride * out_size % 16u == 0)));
-  if (p->type == MAASO_FP32) launch_logits<float, float>(a, wide, s);
-  else if (p->type == MAASO_BF16 && p->out_type == MAASO_FP32) launch_logits<__bf16, float>(a, wide, s);
-  else if (p->type == MAASO_BF16) launch_logits<__bf16, __bf16>(a, wide, s);
-  else if (p->out_type == MAASO_FP32) launch_logits<_Float16, float>(a, wide, s);
-  else launch_logits<_Float16, _Float16>(a, wide, s);
-  if (a.chosen) hipLaunchKernelGGL(choose_kernel, dim3(a.n), dim3(64), 0, s, a.best, a.slices, a.chosen);
+  if (p->type == MAASO_FP32) launch_logits<float, float>(a, s);
+  else if (p->type == MAASO_BF16 && p->out_type == MAASO_FP32) launch_logits<__bf16, float>(a, s);
+  else if (p->type == MAASO_BF16) launch_logits<__bf16, __bf16>(a, s);
+  else if (p->out_type == MAASO_FP32) launch_logits<_Float16, float>(a, s);
+  else launch_logits<_Float16, _Float16>(a, s);
+  if (a.chosen && !a.meet) hipLaunchKernelGGL(choose_kernel, dim3(a.n), dim3(64), 0, s, a.best, a.slices, a.chosen);
   return launched();
 }
 

@@ -198,3 +198,45 @@ def test_a_graph(inst):
         torch.cuda.synchronize()
         assert torch.equal(out, want) and torch.equal(got, which)
         I.maaso_logits_adjust(inst, logits=-x, chosen=got)
+
+
+@pytest.mark.parametrize("biases", [511, 512, 513, 5000])
+def test_many_biases(inst, biases):
+    rng = np.random.default_rng(biases)
+    tokens = np.sort(rng.permutation(20000)[:biases]).astype(np.int32)
+    c = dict(bias_token=tokens, bias_value=rng.normal(size=biases).astype(np.float32), bias_start=np.array([0, biases, biases]),
+             history=np.concatenate([tokens[:100], tokens[:50]]), history_start=np.array([0, 150, 150]), frequency=np.full(2, 0.5, np.float32))
+    check(inst, torch.randn(2, 20000, generator=torch.Generator().manual_seed(2)), {k: v.astype(np.float32 if v.dtype == np.float32 else np.int32) for k, v in c.items()}, torch.float32)
+
+
+def test_a_history_of_more_than_a_million_tokens(inst):
+    history = np.concatenate([np.full(2 ** 20 + 5, 7), np.arange(3000)]).astype(np.int32)
+    c = dict(history=history, history_start=np.array([0, len(history)], np.int32), frequency=np.array([1e-5], np.float32), presence=np.array([0.5], np.float32),
+             bias_token=np.array([3, 7], np.int32), bias_value=np.array([1.5, 100.0], np.float32), bias_start=np.array([0, 2], np.int32))
+    check(inst, torch.randn(1, 5000, generator=torch.Generator().manual_seed(3)), c, torch.float32)
+
+
+def test_biases_out_of_order_by_several(inst):
+    out, tokens = torch.empty(1, 4096, device="cuda"), np.tile([9, 2], 200)
+    for _ in range(2):
+        I.maaso_logits_adjust(inst, logits=torch.ones(1, 4096, device="cuda"), out=out, chosen=i32([0]), bias_token=i32(tokens), bias_value=f32(np.ones(400)), bias_start=i32([0, 400]))
+        assert I.maaso_instance_status(inst) == I.BAD_TOKEN
+        assert out.isfinite().all() and (out[0, 10:] == 1).all()
+
+
+@pytest.mark.parametrize("scale", [1e-38, 1e-30, 1.0, 1e30])
+@pytest.mark.parametrize("temperature", [1e-9, 0.7, 1.0, 3.0, 1e10])
+def test_divisions_over_the_whole_range(inst, scale, temperature):
+    logits = torch.randn(2, 6000, generator=torch.Generator().manual_seed(4)) * scale
+    logits[0, ::7] *= 1e-4
+    logits[1, ::11] = 0
+    check(inst, logits, dict(temperature=np.array([temperature, temperature * 1.1], np.float32)), torch.float32)
+
+
+@pytest.mark.parametrize("n", [1, 3, 900, 1025])
+def test_few_and_many_rows(inst, n):
+    """Rows whose blocks choose together, and rows whose choices are joined by a launch of their own."""
+    rng = np.random.default_rng(n)
+    logits = torch.randint(-3, 4, (n, 9001), generator=torch.Generator().manual_seed(n)).float()
+    for _ in range(2):
+        check(inst, logits, make(rng, n, 9001, 30, 3, 2), torch.float32)
