@@ -6,6 +6,7 @@ arguments only."""
 from __future__ import annotations
 
 import ctypes as C
+from struct import Struct
 
 from .binding import MaasoError, _check, _stream_handle, _t, load_library
 
@@ -58,6 +59,20 @@ class LogitsArgs(C.Structure):
                 ("mask", C.c_void_p), ("mask_row", C.c_void_p), ("n_mask", C.c_uint32)]
 
 
+# The same structures, packed in one go: a ctypes structure of twenty fields takes longer to fill than a kernel to launch.
+_codes = {C.c_uint32: "I", C.c_uint64: "Q", C.c_float: "f", C.c_void_p: "P"}
+
+
+def _packer(structure):
+    s = Struct("@" + "".join(_codes[kind] for _, kind in structure._fields_))
+    if s.size > C.sizeof(structure):
+        raise RuntimeError(f"{structure.__name__} is laid out otherwise than packed")
+    pad = b"\0" * (C.sizeof(structure) - s.size)
+    return (lambda *v: s.pack(*v) + pad) if pad else s.pack
+
+
+_pack_append, _pack_attention, _pack_logits = _packer(AppendArgs), _packer(AttentionArgs), _packer(LogitsArgs)
+
 _lib = None
 
 
@@ -100,29 +115,30 @@ def _type(t) -> int:
         raise AssertionError(f"{t.dtype} is none of the library's types") from None
 
 
-def _ptr(t, dtype, size=None):
-    """Device pointer of a contiguous tensor of this type, with `size` elements where given; None -> NULL."""
+def _ptr(t, dtype, size=0):
+    """Device pointer of a contiguous tensor of this type, with at least `size` elements; None -> 0.  A call has up to a dozen
+    of these, and small calls take no longer than their marshalling: one condition where all is well."""
     if t is None:
-        return None
+        return 0
+    if t.dtype is dtype and t.is_cuda and t.is_contiguous() and t.numel() >= size:
+        return t.data_ptr()
     if not t.is_cuda or not t.is_contiguous():
         raise AssertionError("device buffers must be contiguous GPU tensors")
     if t.dtype != dtype:
         raise AssertionError(f"expected {dtype}, got {t.dtype}")
-    if size is not None and t.numel() < size:
-        raise AssertionError(f"expected {size} elements, got {t.numel()}")
-    return t.data_ptr()
+    raise AssertionError(f"expected {size} elements, got {t.numel()}")
 
 
-def _heads(t, heads, dim, dtype=None):
+def _heads(t, shape, dtype):
     """(pointer, elements between tokens) of [tokens, heads, dim], a token's heads side by side."""
-    if not t.is_cuda or (dtype is not None and t.dtype != dtype):
+    step, heads, side = t.stride() if t.dim() == 3 else (0, 0, 0)
+    if t.dtype is dtype and t.is_cuda and t.shape == shape and side == 1 and (heads == shape[2] or shape[1] == 1):
+        return t.data_ptr(), step
+    if not t.is_cuda or t.dtype != dtype:
         raise AssertionError(f"expected a GPU tensor of {dtype}, got {t.dtype} on {t.device}")
-    shape, stride = t.shape, t.stride()
-    if len(shape) != 3 or shape[2] != dim or (heads is not None and shape[1] != heads):
-        raise AssertionError(f"expected [tokens, {heads}, {dim}], got {tuple(shape)}")
-    if stride[2] != 1 or (shape[1] > 1 and stride[1] != dim):
-        raise AssertionError("a token's heads must lie side by side")
-    return t.data_ptr(), stride[0]
+    if t.shape != shape:
+        raise AssertionError(f"expected {tuple(shape)}, got {tuple(t.shape)}")
+    raise AssertionError("a token's heads must lie side by side")
 
 
 class Instance:
@@ -232,37 +248,38 @@ def maaso_kv_append(inst: Instance, cache: KvCache, *, layer, q, k, v, q_out, sl
                     q_weight=None, k_weight=None, eps=1e-6, interleaved=False, stream=None) -> None:
     """q, q_out [tokens, heads, dim], k, v [tokens, key heads, dim]; cos_sin [positions, rotary] (float32)."""
     torch = _t()
-    dtype, dim, tokens = q.dtype, cache.dim, q.shape[0]
-    qp, qs = _heads(q, None, dim)
-    op, os = _heads(q_out, q.shape[1], dim, dtype)
-    kp, ks = _heads(k, cache.heads, dim, dtype)
-    vp, vs = _heads(v, cache.heads, dim, dtype)
-    if k.shape[0] != tokens or v.shape[0] != tokens or q_out.shape[0] != tokens:
-        raise AssertionError("q, k, v and q_out must have the same tokens")
+    i32, dtype, shape, dim = torch.int32, q.dtype, q.shape, cache.dim
+    if len(shape) != 3 or shape[2] != dim:
+        raise AssertionError(f"expected [tokens, heads, {dim}], got {tuple(shape)}")
+    tokens, heads, _ = shape
+    keys = (tokens, cache.heads, dim)
+    qp, qs = _heads(q, shape, dtype)
+    op, os = _heads(q_out, shape, dtype)
+    kp, ks = _heads(k, keys, dtype)
+    vp, vs = _heads(v, keys, dtype)
     n_pos, rotary = cos_sin.shape if cos_sin is not None else (0, 0)
-    a = AppendArgs(_type(q), tokens, q.shape[1], rotary, int(interleaved), n_pos, float(eps), qp, kp, vp, qs, ks, vs, os,
-                   op, _ptr(q_weight, dtype, dim), _ptr(k_weight, dtype, dim), _ptr(cos_sin, torch.float32),
-                   _ptr(pos, torch.int32, tokens), _ptr(slot, torch.int64, tokens))
-    _check(_library().maaso_kv_append(inst.handle, cache.ref, int(layer), C.byref(a), _stream_handle(stream)),
-           "maaso_kv_append")
+    a = _pack_append(_type(q), tokens, heads, rotary, 1 if interleaved else 0, n_pos, eps, qp, kp, vp, qs, ks, vs, os, op,
+                     _ptr(q_weight, dtype, dim), _ptr(k_weight, dtype, dim), _ptr(cos_sin, torch.float32), _ptr(pos, i32, tokens),
+                     _ptr(slot, torch.int64, tokens))
+    _check(_library().maaso_kv_append(inst.handle, cache.ref, layer, a, _stream_handle(stream)), "maaso_kv_append")
 
 
 def maaso_kv_attention(inst: Instance, cache: KvCache, pages: KvPages, *, layer, q, out, q_start, scale, max_q, max_len,
                        rows=None, group_start=None, shared=None, max_shared=0, total_len=0, lse=None, stream=None) -> None:
     """q, out [tokens, heads, dim]; lse [tokens, heads] (float32)."""
     torch = _t()
-    i32, dim, heads, tokens = torch.int32, cache.dim, q.shape[1], q.shape[0]
+    i32, dtype, shape, dim = torch.int32, q.dtype, q.shape, cache.dim
+    if len(shape) != 3 or shape[2] != dim:
+        raise AssertionError(f"expected [tokens, heads, {dim}], got {tuple(shape)}")
+    tokens, heads, _ = shape
     n = q_start.numel() - 1
     groups = 0 if group_start is None else group_start.numel() - 1
-    qp, qs = _heads(q, None, dim)
-    op, os = _heads(out, heads, dim, q.dtype)
-    if out.shape[0] != tokens:
-        raise AssertionError("q and out must have the same tokens")
-    a = AttentionArgs(_type(q), n, tokens, heads, groups, int(max_q), int(max_len), int(max_shared), int(total_len), float(scale),
-                      qp, op, qs, os, _ptr(lse, torch.float32, tokens * heads), _ptr(q_start, i32), _ptr(rows, i32, n),
-                      _ptr(group_start, i32), _ptr(shared, i32, groups))
-    _check(_library().maaso_kv_attention(inst.handle, cache.ref, int(layer), pages.ref, C.byref(a), _stream_handle(stream)),
-           "maaso_kv_attention")
+    qp, qs = _heads(q, shape, dtype)
+    op, os = _heads(out, shape, dtype)
+    a = _pack_attention(_type(q), n, tokens, heads, groups, int(max_q), int(max_len), int(max_shared), int(total_len), scale, qp, op,
+                        qs, os, _ptr(lse, torch.float32, tokens * heads), _ptr(q_start, i32), _ptr(rows, i32, n),
+                        _ptr(group_start, i32), _ptr(shared, i32, groups))
+    _check(_library().maaso_kv_attention(inst.handle, cache.ref, layer, pages.ref, a, _stream_handle(stream)), "maaso_kv_attention")
 
 
 def maaso_logits_adjust(inst: Instance, *, logits, out=None, chosen=None, repetition=None, frequency=None, presence=None,
@@ -271,18 +288,21 @@ def maaso_logits_adjust(inst: Instance, *, logits, out=None, chosen=None, repeti
     """logits, out [rows, vocabulary], a row's elements side by side; mask [masks, words] (int32)."""
     torch = _t()
     i32, f32 = torch.int32, torch.float32
-    n, vocab = logits.shape
-    if not logits.is_cuda or logits.stride(1) != 1:
+    n, vocab = shape = logits.shape
+    step, side = logits.stride()
+    if side != 1 or not logits.is_cuda:
         raise AssertionError("a row's logits must lie side by side, on the GPU")
-    if out is not None and (not out.is_cuda or tuple(out.shape) != (n, vocab) or out.stride(1) != 1):
-        raise AssertionError("out must have the logits' shape, a row's elements side by side")
+    kind, out_kind, out_step, out_at = _type(logits), MAASO_FP32, 0, 0
+    if out is not None:
+        if not out.is_cuda or out.shape != shape or out.stride(1) != 1:
+            raise AssertionError("out must have the logits' shape, a row's elements side by side")
+        out_kind, out_step, out_at = _type(out), out.stride(0), out.data_ptr()
     if mask is not None and mask.shape[1] != (vocab + 31) // 32:
         raise AssertionError("a mask has a bit for each token")
-    a = LogitsArgs(_type(logits), _type(out) if out is not None else MAASO_FP32, n, vocab, logits.stride(0),
-                   out.stride(0) if out is not None else 0, logits.data_ptr(), out.data_ptr() if out is not None else None,
-                   _ptr(chosen, i32, n), _ptr(repetition, f32, n), _ptr(frequency, f32, n), _ptr(presence, f32, n),
-                   _ptr(temperature, f32, n), _ptr(history, i32), _ptr(history_start, i32, n + 1),
-                   history.numel() if history is not None else 0, bias_token.numel() if bias_token is not None else 0,
-                   _ptr(bias_token, i32), _ptr(bias_value, f32, bias_token.numel() if bias_token is not None else None),
-                   _ptr(bias_start, i32, n + 1), _ptr(mask, i32), _ptr(mask_row, i32, n), mask.shape[0] if mask is not None else 0)
-    _check(_library().maaso_logits_adjust(inst.handle, C.byref(a), _stream_handle(stream)), "maaso_logits_adjust")
+    n_bias = bias_token.numel() if bias_token is not None else 0
+    a = _pack_logits(kind, out_kind, n, vocab, step, out_step, logits.data_ptr(), out_at, _ptr(chosen, i32, n),
+                     _ptr(repetition, f32, n), _ptr(frequency, f32, n), _ptr(presence, f32, n), _ptr(temperature, f32, n),
+                     _ptr(history, i32), _ptr(history_start, i32, n + 1), history.numel() if history is not None else 0, n_bias,
+                     _ptr(bias_token, i32), _ptr(bias_value, f32, n_bias), _ptr(bias_start, i32, n + 1), _ptr(mask, i32),
+                     _ptr(mask_row, i32, n), mask.shape[0] if mask is not None else 0)
+    _check(_library().maaso_logits_adjust(inst.handle, a, _stream_handle(stream)), "maaso_logits_adjust")
