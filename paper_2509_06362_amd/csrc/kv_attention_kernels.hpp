@@ -65,17 +65,19 @@ struct SequenceSpan {
   uint32_t row, tok0, n_q, len;
 };
 
+// (What does not depend on one another is asked for at once, good or not: each load that waits for another is most of a
+// microsecond of a short item.)
 __device__ inline SequenceSpan sequence_span(const AttentionArgs& a, uint32_t i) {
+  const int32_t q0 = a.q_start[i], q1 = a.q_start[i + 1], row = a.rows ? a.rows[i] : (int32_t)i;
+  const bool known = row >= 0 && (uint32_t)row < a.n_rows;
+  const int32_t len = a.length[known ? row : 0];
   SequenceSpan s{0u, 0u, 0u, 0u};
-  const int32_t q0 = a.q_start[i], q1 = a.q_start[i + 1];
   if (q0 < 0 || q1 < q0 || (uint32_t)q1 > a.n_tok) { raise(a.status, MAASO_INST_BAD_BOUND); return s; }
-  const int32_t row = a.rows ? a.rows[i] : (int32_t)i;
   s.tok0 = (uint32_t)q0;
   s.n_q = (uint32_t)(q1 - q0);
   if (s.n_q > a.max_q) { raise(a.status, MAASO_INST_BAD_BOUND); s.n_q = a.max_q; }
-  if (row < 0 || (uint32_t)row >= a.n_rows) { raise(a.status, MAASO_INST_BAD_ROW); return s; }
+  if (!known) { raise(a.status, MAASO_INST_BAD_ROW); return s; }
   s.row = (uint32_t)row;
-  const int32_t len = a.length[row];
   if (len < 0 || (uint64_t)len > (uint64_t)a.width << a.page_log2) { raise(a.status, MAASO_INST_BAD_ROW); return s; }
   s.len = (uint32_t)len;
   if (s.len > a.max_len) { raise(a.status, MAASO_INST_BAD_BOUND); s.len = a.max_len; }
@@ -100,18 +102,21 @@ __device__ inline bool group_good(const AttentionArgs& a, uint32_t g) {
 }
 
 // Tokens that sequence i begins with like its group, as far as the caller's bound and a row's width go; 0 outside every
-// group.  All lanes of the wave have the same i: 64 groups are looked at in one go, for every load in a row of loads that
-// wait for each other is a microsecond of a short item.
-__device__ inline uint32_t shared_of(const AttentionArgs& a, uint32_t i) {
-  const uint32_t lane = threadIdx.x & 63u;
+// group.  All lanes of the wave have the same i: 64 groups are looked at in one go.
+struct GroupLanes {
+  int32_t first, end, shared;
+};
+__device__ inline GroupLanes groups_from(const AttentionArgs& a, uint32_t base) {
+  const uint32_t lane = threadIdx.x & 63u, g = base + lane < a.n_groups ? base + lane : a.n_groups - 1u;
+  return {a.group_start[g], a.group_start[g + 1u], a.shared[g]};
+}
+__device__ inline uint32_t shared_of(const AttentionArgs& a, uint32_t i, GroupLanes at) {
   uint32_t found = 0;
   for (uint32_t base = 0; base < a.n_groups; base += 64u) {
-    const uint32_t g = base + lane < a.n_groups ? base + lane : a.n_groups - 1u;
-    const int32_t f = a.group_start[g], e = a.group_start[g + 1u], v = a.shared[g];
-    const bool in = f >= 0 && f <= (int32_t)i && e > (int32_t)i && (uint32_t)e <= a.n;
-    const uint64_t which = __ballot(in);
+    if (base) at = groups_from(a, base);
+    const uint64_t which = __ballot(at.first >= 0 && at.first <= (int32_t)i && at.end > (int32_t)i && (uint32_t)at.end <= a.n);
     if (which) {
-      const int32_t keys = __shfl(v, __builtin_ctzll(which));
+      const int32_t keys = __shfl(at.shared, __builtin_ctzll(which));
       if (keys < 0 || (uint32_t)keys > a.most_shared) raise(a.status, MAASO_INST_BAD_BOUND);
       found = keys < 0 ? 0u : (uint32_t)keys < a.most_shared ? (uint32_t)keys : a.most_shared;
       break;
@@ -222,13 +227,15 @@ __device__ inline bool item_keys(const AttentionArgs& a, bool is_shared, uint32_
     k.end = k.end < k.begin ? k.begin : k.end;
     return row0 < k.n_rows;
   } else {
+    GroupLanes groups{-1, -1, 0};
+    if (a.n_groups) groups = groups_from(a, 0u);
     const SequenceSpan s = sequence_span(a, which);
     k.tok0 = s.tok0;
     k.n_q = s.n_q;
     k.len = s.len;
     k.n_rows = s.n_q * a.group;
     k.page_row = s.row;
-    const uint32_t shared = shared_of(a, which);
+    const uint32_t shared = shared_of(a, which, groups);
     const RowParts parts = row_parts(a, s.len, shared);
     k.alone = parts.n_shared + parts.n_own <= 1u && parts.n_shared == 0u;
     const uint64_t b = (uint64_t)shared + (uint64_t)part * parts.own_chunk;
@@ -250,14 +257,45 @@ __device__ inline uint32_t row_limit(const AttentionArgs& a, bool is_shared, con
   return seen_keys(s, s.n_q, tok - s.tok0);
 }
 
+// Eight neighbouring elements as they lie in a page: widened to operands; those of [from, to) kept and the others made zeros,
+// whatever they hold (by their bits); whether one is an infinity or NaN.
 template <typename T, typename C> struct KeyLoad;
 template <typename T> struct KeyLoad<T, T> {
   using raw = typename Vec<T>::x8;
+  using bits = u32x4;
   static __device__ inline typename Vec<T>::x8 wide(raw r) { return r; }
+  static __device__ inline bits kept(uint32_t from, uint32_t to) {
+    bits m;
+#pragma unroll
+    for (uint32_t k = 0; k < 4u; ++k)
+      m[k] = (2u * k >= from && 2u * k < to ? 0xffffu : 0u) | (2u * k + 1u >= from && 2u * k + 1u < to ? 0xffff0000u : 0u);
+    return m;
+  }
+  static __device__ inline bool odd(bits b) {
+    constexpr uint32_t kTop = sizeof(T) == 2 && __is_same(T, __bf16) ? 0x7f80u : 0x7c00u;
+    bool odd = false;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) odd = odd || (b[k] & kTop) == kTop || (b[k] >> 16 & kTop) == kTop;
+    return odd;
+  }
 };
 template <typename T> struct KeyLoad<T, E4m3> {
   using raw = u32x2;
+  using bits = u32x2;
   static __device__ inline typename Vec<T>::x8 wide(raw r) { return widen8<T>(r); }
+  static __device__ inline bits kept(uint32_t from, uint32_t to) {
+    bits m;
+#pragma unroll
+    for (uint32_t w = 0; w < 2u; ++w) {
+      m[w] = 0u;
+#pragma unroll
+      for (uint32_t k = 0; k < 4u; ++k)
+        if (w * 4u + k >= from && w * 4u + k < to) m[w] |= 0xffu << (8u * k);
+    }
+    return m;
+  }
+  // (seven ones: the one value that is none)
+  static __device__ inline bool odd(bits b) { return (((b[0] & 0x7f7f7f7fu) + 0x01010101u) | ((b[1] & 0x7f7f7f7fu) + 0x01010101u)) & 0x80808080u; }
 };
 
 template <typename V> __device__ inline bool finite16(V v) {
@@ -268,8 +306,7 @@ template <typename V> __device__ inline bool finite16(V v) {
 }
 
 // One tile of rows against this wave's steps of 32 keys.  First the steps that not all rows see in full, if there are any,
-// then the others, of which the next one's keys and values are asked for before this one's are multiplied: two steps' loads
-// are always under way.
+// then the others, of which with heads of 64 the next one's keys and values are asked for before this one's are multiplied.
 template <typename T, typename C, int D>
 struct StreamTile {
   using X8 = typename Vec<T>::x8;
@@ -384,29 +421,34 @@ struct StreamTile {
     const X8 w = weights(x);
     // Values of keys that no row sees are taken as zeros, whatever their place holds; where one that some rows may see and others
     // not is not finite, row by row.
-    auto value = [&](int d, uint32_t sees) {
-      asm volatile("" : "+v"(s.v[d]));  // (one after the other, and each from anew: registers are few)
-      X8 v = L::wide(s.v[d]);
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (key8 + k < begin || key8 + k >= sees) v[k] = (T)0.0f;
-      return v;
+    auto keep = [&](uint32_t sees) {
+      const uint32_t from = begin < key8 ? 0u : begin - key8, to = sees > key8 ? sees - key8 : 0u;
+      return L::kept(from, to);
     };
+    const typename L::bits held = keep(end);
     bool odd = false;
 #pragma unroll
-    for (int d = 0; d < D / 16; ++d) odd = odd || !finite16(value(d, end));
+    for (int d = 0; d < D / 16; ++d) {
+      const typename L::bits b = __builtin_bit_cast(typename L::bits, s.v[d]) & held;
+      s.v[d] = __builtin_bit_cast(typename L::raw, b);
+      odd = odd || L::odd(b);
+    }
     if (!__any(odd)) {
 #pragma unroll
-      for (int d = 0; d < D / 16; ++d) o[d] = mfma_16x16x32(value(d, end), w, o[d]);
+      for (int d = 0; d < D / 16; ++d) o[d] = mfma_16x16x32(L::wide(s.v[d]), w, o[d]);
       return;
     }
 #pragma unroll 1
     for (int r = 0; r < 16; ++r) {
-      const uint32_t most = __shfl(limit, r), sees = most < end ? most : end;
+      const uint32_t most = __shfl(limit, r);
+      const typename L::bits seen = keep(most < end ? most : end);
 #pragma unroll
       for (int d = 0; d < D / 16; ++d) {
-        const f32x4 t = mfma_16x16x32(value(d, sees), w, o[d]);
+        typename L::bits b = __builtin_bit_cast(typename L::bits, s.v[d]) & seen;
+        asm volatile("" : "+v"(b));  // (one after the other: registers are few)
+        const f32x4 t = mfma_16x16x32(L::wide(__builtin_bit_cast(typename L::raw, b)), w, o[d]);
         if (col == (uint32_t)r) o[d] = t;
+        asm volatile("" : "+v"(o[d]));
       }
     }
   }
@@ -431,7 +473,7 @@ struct StreamTile {
       take_some(s, at);
     }
     uint32_t base = whole0 + wave * 32u;
-    if constexpr (sizeof(Step) > 256u) {  // (two of them are more than the registers hold)
+    if constexpr (D >= 128) {  // (two of them would be a third of the registers, or more)
 #pragma unroll 1
       for (; base < whole1; base += kStride) {
         Step s;
@@ -458,8 +500,11 @@ struct StreamTile {
 
 // Items of few rows.  kSplit 1: a wave takes an item, alone; kSplit 4: the four waves of a block share an item's keys and join
 // in shared memory, for when there are few items and the parts of a row would be many.
+//
+// Blocks to a compute unit, by the registers they need: with heads of 128 three of one step each beat two of two steps (160
+// short sequences behind a shared beginning 110 to 105 us), with heads of 64 two steps have room beside three others.
 template <typename T, typename C, int D, int kSplit>
-__global__ void __launch_bounds__(256, 2) attention_stream_kernel(AttentionArgs a) {
+__global__ void __launch_bounds__(256, D == 256 ? 2 : 3) attention_stream_kernel(AttentionArgs a) {
   using X8 = typename Vec<T>::x8;
   const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6), col = lane & 15u, g = lane >> 4;
   // item -> (part, head, sequence or group)
@@ -943,9 +988,11 @@ __global__ void __launch_bounds__(256) attention_join_kernel(AttentionArgs a) {
   for (uint32_t tok = blockIdx.x * kTokens; tok < blockIdx.x * kTokens + kTokens && tok < a.n_tok; ++tok) {
     if (tok >= known) {
       const uint32_t i = sequence_of(a, tok);
+      GroupLanes groups{-1, -1, 0};
+      if (a.n_groups) groups = groups_from(a, 0u);
       s = sequence_span(a, i);
       const bool mine = tok >= s.tok0 && tok - s.tok0 < s.n_q;
-      of = mine ? row_parts(a, s.len, shared_of(a, i)) : RowParts{0u, 0u, 0u};
+      of = mine ? row_parts(a, s.len, shared_of(a, i, groups)) : RowParts{0u, 0u, 0u};
       known = mine ? s.tok0 + s.n_q : tok + 1u;
     }
     if (of.n_shared == 0u && of.n_own == 1u) {  // (written already)
