@@ -1,15 +1,18 @@
-"""Builds libmaaso.so in-tree with hipcc for gfx950.  `python -m paper_2509_06362_amd.build`."""
+"""Builds libmaaso.so (hipcc, gfx950) and the marshalling module _marshal.so (host code, against the installed
+torch) in-tree.  `python -m paper_2509_06362_amd.build`."""
 from __future__ import annotations
 
 import os
 import subprocess
 import sys
+import sysconfig
 from pathlib import Path
 
 PKG = Path(__file__).resolve().parent
 ROOT = PKG.parent
 CSRC = PKG / "csrc"
 LIB = PKG / "libmaaso.so"
+MARSHAL = PKG / "_marshal.so"
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
@@ -23,6 +26,28 @@ HIPCC_FLAGS = [
 
 def sources():
     return sorted(CSRC.glob("*.hip"))
+
+
+def build_marshal(verbose: bool = False) -> Path:
+    import torch
+    from torch.utils import cpp_extension
+    tmp = MARSHAL.with_suffix(f".so.tmp{os.getpid()}")
+    include = [*cpp_extension.include_paths(), os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "include"),
+               sysconfig.get_paths()["include"]]
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *(f"-isystem{p}" for p in include),
+           "-Wall", "-Wextra", str(CSRC / "instance_marshal.cpp"), *(f"-L{p}" for p in cpp_extension.library_paths()),
+           "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_python", "-o", str(tmp)]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        tmp.unlink(missing_ok=True)
+        raise RuntimeError(f"{cmd[0]} failed ({res.returncode}):\n{res.stderr}")
+    if verbose and res.stderr.strip():
+        print(res.stderr, file=sys.stderr)
+    os.replace(tmp, MARSHAL)
+    return MARSHAL
 
 
 def build_library(verbose: bool = False) -> Path:
@@ -40,6 +65,7 @@ def build_library(verbose: bool = False) -> Path:
     if verbose and err.strip():
         print(err, file=sys.stderr)
     os.replace(tmp, LIB)
+    build_marshal(verbose)
     return LIB
 
 
