@@ -229,7 +229,7 @@ def test_calls_look_at_tensors(lib):
     inst, view = I.Instance(0, 0), type("View", (), {"at": C.addressof(I.CacheArgs(n_kv_heads=1, head_dim=64))})()
     rows, heads = torch.zeros(2, dtype=i32), torch.zeros(2, 1, 64, dtype=bf16)
     calls = [lambda x: I.maaso_kv_extend(inst, view, rows=x, q_start=x, slot=x, copies=x), lambda x: I.maaso_kv_fork(inst, view, parents=x, children=x),
-             lambda x: I.maaso_kv_trim(inst, view, rows=x, keep=x), lambda x: I.maaso_kv_copy(inst, view, pairs=x),
+             lambda x: I.maaso_kv_trim(inst, view, rows=x, keep=x), lambda x: I.maaso_kv_copy(inst, view, pairs=rows if x is None else x),
              lambda x: I.maaso_kv_append(inst, view, layer=0, q=x, k=x, v=x, q_out=x, slot=rows),
              lambda x: I.maaso_kv_attention(inst, view, view, layer=0, q=x, out=x, q_start=rows, scale=1.0, max_q=1, max_len=1),
              lambda x: I.maaso_logits_adjust(inst, logits=x, chosen=rows)]
