@@ -48,7 +48,8 @@ struct AttentionArgs {
   uint32_t own_least, shared_chunk;    // keys of an own part at least, of a shared one; multiples of 64
   uint32_t own_parts, shared_parts;    // most parts of a row
   uint32_t own_tiles, shared_tiles;    // most tiles of kTileRows rows
-  uint32_t shared_blocks;              // of the launch: blocks that take shared parts; those behind them take own ones
+  uint32_t tile_blocks, stream_blocks; // of the launch of tiles
+  uint32_t tile_shared, stream_shared; // blocks, items that take shared parts; those behind them take own ones
   bool alone;                          // items of few rows: a wave each, not a block
   float scale_log2;
   // workspace, where a row has several parts
@@ -500,17 +501,19 @@ struct StreamTile {
 
 // Items of few rows.  kSplit 1: a wave takes an item, alone; kSplit 4: the four waves of a block share an item's keys and join
 // in shared memory, for when there are few items and the parts of a row would be many.
-//
-// Blocks to a compute unit, by the registers they need: with heads of 128 three of one step each beat two of two steps (160
-// short sequences behind a shared beginning 110 to 105 us), with heads of 64 two steps have room beside three others.
+template <typename T, int D> struct StreamJoin {
+  float o[4][16][D + 4];
+  float m[4][16], l[4][16];
+};
+
 template <typename T, typename C, int D, int kSplit>
-__global__ void __launch_bounds__(256, D == 256 ? 2 : 3) attention_stream_kernel(AttentionArgs a) {
+__device__ inline void stream_block(const AttentionArgs& a, uint32_t block, StreamJoin<T, D>* meet) {
   using X8 = typename Vec<T>::x8;
   const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6), col = lane & 15u, g = lane >> 4;
   // item -> (part, head, sequence or group)
-  uint32_t id = kSplit == 1 ? blockIdx.x * 4u + wave : blockIdx.x;
-  const bool is_shared = id < a.shared_blocks;
-  if (!is_shared) id -= a.shared_blocks;
+  uint32_t id = kSplit == 1 ? block * 4u + wave : block;
+  const bool is_shared = id < a.stream_shared;
+  if (!is_shared) id -= a.stream_shared;
   const uint32_t head = id % a.n_kv_heads;
   id /= a.n_kv_heads;
   const uint32_t count = is_shared ? a.n_groups : a.n, which = id % count, part = id / count;
@@ -570,8 +573,8 @@ __global__ void __launch_bounds__(256, D == 256 ? 2 : 3) attention_stream_kernel
     }
   } else {
     // join the waves
-    __shared__ float so[4][16][D + 4];
-    __shared__ float sm[4][16], sl[4][16];
+    auto &so = meet->o;
+    auto &sm = meet->m, &sl = meet->l;
     if (g == 0) { sm[wave][col] = st.m; sl[wave][col] = l; }
     __syncthreads();
     float top = -INFINITY;
@@ -605,6 +608,19 @@ __global__ void __launch_bounds__(256, D == 256 ? 2 : 3) attention_stream_kernel
       for (int k = 0; k < D / 16; ++k) a.part_o[(slot0 + row) * D + at + k] = acc[k];
       if (at == 0) *reinterpret_cast<f32x2*>(a.part_ml + (slot0 + row) * 2) = (f32x2){mm, ll};
     }
+  }
+}
+
+//
+// Blocks to a compute unit, by the registers they need: with heads of 128 three of one step each beat two of two steps (160
+// short sequences behind a shared beginning 110 to 105 us), with heads of 64 two steps have room beside three others.
+template <typename T, typename C, int D, int kSplit>
+__global__ void __launch_bounds__(256, D == 256 ? 2 : 3) attention_stream_kernel(AttentionArgs a) {
+  if constexpr (kSplit == 1) {
+    stream_block<T, C, D, 1>(a, blockIdx.x, nullptr);
+  } else {
+    __shared__ StreamJoin<T, D> meet;
+    stream_block<T, C, D, kSplit>(a, blockIdx.x, &meet);
   }
 }
 
@@ -726,14 +742,13 @@ __device__ inline void feed() {
 }
 
 template <typename T, typename C, int D, int kKeys>
-__global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attention_tile_kernel(AttentionArgs a) {
+__device__ inline void tile_block(const AttentionArgs& a, uint32_t block, char* lds, uint32_t* lowest_of) {
   using X8 = typename Vec<T>::x8;
   using Tile = RowTile<T, C, D, kKeys>;
   constexpr int kBlocks = kKeys / 32, kSteps = kKeys / 16;
-  __shared__ __align__(128) char lds[2 * Tile::kBuffer];
   const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31u, half = lane >> 5;
-  const bool is_shared = blockIdx.x < a.shared_blocks;
-  uint32_t id = is_shared ? blockIdx.x : blockIdx.x - a.shared_blocks;
+  const bool is_shared = block < a.tile_shared;
+  uint32_t id = is_shared ? block : block - a.tile_shared;
   const uint32_t head = id % a.n_kv_heads;
   id /= a.n_kv_heads;
   const uint32_t tiles = is_shared ? a.shared_tiles : a.own_tiles;
@@ -754,7 +769,6 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attention_tile_kernel(A
     lowest = x < lowest ? x : lowest;
     highest = y > highest ? y : highest;
   }
-  __shared__ uint32_t lowest_of[4];
   if (lane == 0) lowest_of[wave] = lowest;
   __syncthreads();
   const uint32_t low2 = lowest_of[0] < lowest_of[1] ? lowest_of[0] : lowest_of[1], low3 = lowest_of[2] < lowest_of[3] ? lowest_of[2] : lowest_of[3];
@@ -969,6 +983,20 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attention_tile_kernel(A
         *reinterpret_cast<f32x4*>(a.part_o + slot * D + d * 32 + j * 8 + half * 4u) = (f32x4){o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]};
     if (half == 0u) { a.part_ml[slot * 2] = m; a.part_ml[slot * 2 + 1] = l; }
   }
+}
+
+// Tiles, and behind them in the same launch what there is of few rows: its blocks come in as the tiles run out, and are bound
+// by the pages' bytes where those are by the matrix units and shared memory.  Against a launch of their own: 160 sequences
+// behind 6144 shared tokens 104 to 101 us, 20 behind five beginnings of 3372 tokens 41 to 32 us, three prompts of up to 990
+// tokens (heads of 256) 32 to 23 us.  By turns with the tiles from the start, eight and eight, the first takes 119 us.
+template <typename T, typename C, int D, int kKeys>
+__global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attention_tile_kernel(AttentionArgs a) {
+  constexpr uint32_t kTile = 2 * RowTile<T, C, D, kKeys>::kBuffer, kMeet = sizeof(StreamJoin<T, D>);
+  __shared__ __align__(128) char lds[kTile > kMeet ? kTile : kMeet];
+  __shared__ uint32_t lowest_of[4];
+  if (blockIdx.x < a.tile_blocks) tile_block<T, C, D, kKeys>(a, blockIdx.x, lds, lowest_of);
+  else if (a.alone) stream_block<T, C, D, 1>(a, blockIdx.x - a.tile_blocks, nullptr);
+  else stream_block<T, C, D, 4>(a, blockIdx.x - a.tile_blocks, reinterpret_cast<StreamJoin<T, D>*>(lds));
 }
 
 // Joins rows' parts.  A block takes kTokens tokens and some heads; 256 / D heads share a wave, a lane has four neighbouring

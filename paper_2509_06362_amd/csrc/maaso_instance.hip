@@ -288,17 +288,18 @@ template <typename T, typename C, int D>
 void launch_attention(AttentionArgs a, hipStream_t s) {
   const uint32_t heads = a.n_kv_heads;
   const bool tiles = a.max_q * a.group > kStreamRows, shared_tiles = a.shared_parts && (uint64_t)a.n_tok * a.group > kStreamRows;
+  const bool few = !tiles || a.n_groups || (uint64_t)a.n * a.max_q != a.n_tok;
+  a.stream_shared = a.n_groups * heads * a.shared_parts;
+  const uint32_t items = a.stream_shared + a.n * heads * a.own_parts;
+  a.stream_blocks = !few ? 0u : a.alone ? (items + 3u) / 4u : items;
   if (tiles || shared_tiles) {
-    AttentionArgs t = a;
-    t.shared_blocks = shared_tiles ? a.shared_tiles * heads * a.shared_parts : 0u;
-    const uint32_t blocks = t.shared_blocks + (tiles ? a.own_tiles * heads * a.own_parts : 0u);
-    hipLaunchKernelGGL((attention_tile_kernel<T, C, D, D == 256 ? 32 : 64>), dim3(blocks), dim3(256), 0, s, t);
-  }
-  if (!tiles || a.n_groups || (uint64_t)a.n * a.max_q != a.n_tok) {
-    a.shared_blocks = a.n_groups * heads * a.shared_parts;
-    const uint32_t items = a.shared_blocks + a.n * heads * a.own_parts;
-    if (a.alone) hipLaunchKernelGGL((attention_stream_kernel<T, C, D, 1>), dim3((items + 3u) / 4u), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((attention_stream_kernel<T, C, D, 4>), dim3(items), dim3(256), 0, s, a);
+    a.tile_shared = shared_tiles ? a.shared_tiles * heads * a.shared_parts : 0u;
+    a.tile_blocks = a.tile_shared + (tiles ? a.own_tiles * heads * a.own_parts : 0u);
+    hipLaunchKernelGGL((attention_tile_kernel<T, C, D, D == 256 ? 32 : 64>), dim3(a.tile_blocks + a.stream_blocks), dim3(256), 0, s, a);
+  } else if (a.alone) {
+    hipLaunchKernelGGL((attention_stream_kernel<T, C, D, 1>), dim3(a.stream_blocks), dim3(256), 0, s, a);
+  } else {
+    hipLaunchKernelGGL((attention_stream_kernel<T, C, D, 4>), dim3(a.stream_blocks), dim3(256), 0, s, a);
   }
   if (a.part_o) {
     constexpr uint32_t kHeads = 256 / D;  // of a wave
