@@ -347,7 +347,7 @@ struct StreamTile {
     const uint32_t kpage = col >> 3 ? page1 : page0, vpage = g >> 1 ? page1 : page0;
     const uint32_t row = (base + 8u * (col >> 2) + (col & 3u)) & (per - 1u);
     const C* kr = kp + (uint64_t)kpage * a.page_stride + row * (uint32_t)D + g * 8u;
-    const C* vr = vp + (uint64_t)vpage * a.page_stride + ((base + 8u * g) & (per - 1u)) + (col << a.page_log2);
+    const __attribute__((address_space(1))) C* vr = (const __attribute__((address_space(1))) C*)vp + (uint64_t)vpage * a.page_stride + ((base + 8u * g) & (per - 1u)) + (col << a.page_log2);
 #pragma unroll
     for (int t = 0; t < D / 32; ++t) {
       s.k0[t] = *reinterpret_cast<const typename L::raw*>(kr + t * 32);
@@ -355,9 +355,9 @@ struct StreamTile {
     }
 #pragma unroll
     for (int d = 0; d < D / 16; ++d) {
-      s.v[d] = *reinterpret_cast<const typename L::raw*>(vr);
+      s.v[d] = *reinterpret_cast<const __attribute__((address_space(1))) typename L::raw*>(vr);
       vr += 16u << a.page_log2;
-      asm volatile("" : "+v"(vr));  // (one address, moved on)
+      asm volatile("" : "+v"(vr));  // (one address, moved on; it is named global, which the compiler cannot see behind this)
     }
     __builtin_amdgcn_sched_barrier(0);
   }
@@ -797,9 +797,6 @@ __device__ inline void tile_block(const AttentionArgs& a, uint32_t block, char* 
       }
     }
   }
-  // (the queries have come: a wait for them inside the loop would wait for the step's loads as well)
-#pragma unroll
-  for (int s = 0; s < D / 16; ++s) asm volatile("" : "+v"(q[s]));
   f32x16 o[D / 32];
 #pragma unroll
   for (int d = 0; d < D / 32; ++d)
@@ -821,9 +818,9 @@ __device__ inline void tile_block(const AttentionArgs& a, uint32_t block, char* 
   tile.kp = reinterpret_cast<const C*>(a.k_pages) + ((uint64_t)head << a.page_log2) * D;
   tile.vp = reinterpret_cast<const C*>(a.v_pages) + ((uint64_t)head << a.page_log2) * D;
   const int32_t* list = a.table + (uint64_t)keys.page_row * a.width;
+  int32_t held = 0;
   if (begin < end) {
-    int32_t unused;
-    end = uniform(held_end(a, list, begin, end, unused));
+    end = uniform(held_end(a, list, begin, end, held));
   }
   // The table's entry for keys at + 8 (lane % (kKeys / 8)), 0 outside the item.
   auto entry_at = [&](uint32_t at) {
@@ -834,10 +831,16 @@ __device__ inline void tile_block(const AttentionArgs& a, uint32_t block, char* 
   uint32_t buffer = 0;
   int32_t entry = 0;
   if (begin < end) {
-    tile.bring(0, first, entry_at(first));
+    // (the first step's pages are among those that held_end() has looked at: five at most)
+    const uint32_t key8 = first + 8u * (lane % (kKeys / 8)), nth = (key8 >> a.page_log2) - (begin >> a.page_log2);
+    const int32_t page = __shfl(held, (int)(nth & 63u));
+    tile.bring(0, first, key8 < end && (key8 | 15u) >= begin ? page : 0);
     tile.settle(0);
     entry = entry_at(first + kKeys);
   }
+  // (the queries have come, behind the first step's loads: a wait for them inside the loop would wait for the step's as well)
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) asm volatile("" : "+v"(q[s]));
   for (uint32_t base = first; begin < end && base < end; base += kKeys) {
     // This step's keys and values, and the next one's entries, have come; everybody is done with the other buffer.
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");

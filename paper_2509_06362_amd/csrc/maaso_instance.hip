@@ -306,7 +306,7 @@ void launch_attention(AttentionArgs a, hipStream_t s) {
     const uint32_t groups = (a.n_heads + kHeads - 1u) / kHeads;
     if ((uint64_t)a.n_tok * groups < 1024u)
       hipLaunchKernelGGL((attention_join_kernel<T, C, D, 4, 1>), dim3(a.n_tok, groups), dim3(256), 0, s, a);
-    else if (a.n_tok < 1024u)
+    else if ((uint64_t)a.n_tok * groups < 32768u)
       hipLaunchKernelGGL((attention_join_kernel<T, C, D, 1, 1>), dim3(a.n_tok, (groups + 3u) / 4u), dim3(256), 0, s, a);
     else
       hipLaunchKernelGGL((attention_join_kernel<T, C, D, 1, 8>), dim3((a.n_tok + 7u) / 8u, (groups + 3u) / 4u), dim3(256), 0, s, a);
