@@ -28,7 +28,6 @@ namespace maaso {
 
 constexpr float kLn2 = 0.693147180559945309f;
 constexpr uint32_t kStreamRows = 16;  // most rows of an item that one wave's registers take; more are taken in tiles
-constexpr uint32_t kStreamKeys = 32;  // keys of a wave's step
 
 struct AttentionArgs {
   const void* q;

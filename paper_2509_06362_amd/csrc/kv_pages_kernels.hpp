@@ -66,6 +66,15 @@ struct ExtendArgs {
 // extend_kernel; 48 prompts' 1500 pages of 65,536: 5.8 to plan, 4.7 to write).
 __device__ inline bool extend_plan(const ExtendArgs& a, uint32_t* part, uint32_t* bad) {
   const uint32_t t = threadIdx.x, per = 1u << a.p.page_log2;
+  // (which of four pages are free; the first step's are asked for before the rows are looked at)
+  auto free_of = [&](uint32_t p0) {
+    uint32_t free4 = 0;
+#pragma unroll
+    for (uint32_t k = 0; k < 4u; ++k)
+      if (p0 + k < a.p.n_pages && a.p.refs[p0 + k] == 0) free4 |= 1u << k;
+    return free4;
+  };
+  uint32_t free4 = free_of(t * 4u);
   if (t == 0) *bad = 0u;
   __syncthreads();
   uint32_t need_all = 0;
@@ -110,14 +119,12 @@ __device__ inline bool extend_plan(const ExtendArgs& a, uint32_t* part, uint32_t
   // The first need_all free pages, 4 per thread and step.
   uint32_t found = 0;
   for (uint32_t base = 0; base < a.p.n_pages && found < need_all; base += blockDim.x * 4u) {
-    uint32_t free4 = 0;
-    const uint32_t p0 = base + t * 4u;
-    for (uint32_t k = 0; k < 4u; ++k)
-      if (p0 + k < a.p.n_pages && a.p.refs[p0 + k] == 0) free4 |= 1u << k;
+    const uint32_t p0 = base + t * 4u, now = free4;
+    free4 = free_of(p0 + blockDim.x * 4u);  // (the next step's, while this one's are summed; pages are below 2^24)
     uint32_t sum;
-    uint32_t at = found + block_scan(__popc(free4), part, sum);
+    uint32_t at = found + block_scan(__popc(now), part, sum);
     for (uint32_t k = 0; k < 4u; ++k)
-      if (free4 >> k & 1u) {
+      if (now >> k & 1u) {
         if (at < need_all) a.ids[at] = (int32_t)(p0 + k);
         ++at;
       }
@@ -265,8 +272,10 @@ __global__ void __launch_bounds__(256) trim_kernel(PageArgs p, const int32_t* ro
 // ------------------------------------------------------------------------------------------------ compact
 // Held pages below p, `live(p)`, give every page's place: n_live is live(n_pages); a free page p < n_live is hole
 // number p - live(p), a held page p >= n_live takes hole number live(p) - live(n_live).  Three launches: held pages
-// of each chunk; live() of every page and the holes; the new numbers.
-constexpr uint32_t kCompactChunk = 4096;
+// of each chunk; live() of every page and the holes; the new numbers.  A pool of one chunk with a table that a block is
+// through with at once, up to 32 entries a thread, takes one launch (3000 pages, 96 rows of 12, with the copy: 28 us, with one
+// launch 21).
+constexpr uint32_t kCompactChunk = 4096, kCompactEntries = 32 * kPageThreads;
 
 struct CompactArgs {
   PageArgs p;
@@ -291,10 +300,9 @@ __global__ void __launch_bounds__(kPageThreads) compact_count_kernel(CompactArgs
   if (threadIdx.x == 0) a.held[blockIdx.x] = sum;
 }
 
-__global__ void __launch_bounds__(kPageThreads) compact_rank_kernel(CompactArgs a) {
-  __shared__ uint32_t part[17];
+__device__ inline void compact_rank(const CompactArgs& a, uint32_t* part) {
   uint32_t before = 0, n_live = 0;
-  for (uint32_t base = 0; base < a.chunks; base += blockDim.x) {
+  for (uint32_t base = 0; a.chunks > 1u && base < a.chunks; base += blockDim.x) {
     const uint32_t c = base + threadIdx.x;
     const uint32_t v = c < a.chunks ? a.held[c] : 0u;
     uint32_t sum;
@@ -311,6 +319,7 @@ __global__ void __launch_bounds__(kPageThreads) compact_rank_kernel(CompactArgs 
     else mine[k] |= 0x80000000u;
   }
   const uint32_t at = before + block_scan(live, part, sum);
+  if (a.chunks == 1u) n_live = sum;
   for (uint32_t k = 0; k < 4u; ++k) {
     const uint32_t p = p0 + k, r = at + (mine[k] & 0x7fffffffu);
     if (p < a.p.n_pages) {
@@ -324,7 +333,7 @@ __global__ void __launch_bounds__(kPageThreads) compact_rank_kernel(CompactArgs 
   }
 }
 
-__global__ void __launch_bounds__(256) compact_apply_kernel(CompactArgs a) {
+__device__ inline void compact_apply(const CompactArgs& a) {
   const uint32_t n = a.p.n_pages, n_live = a.below[n], low = a.below[n_live], threads = gridDim.x * blockDim.x;
   const uint32_t t = blockIdx.x * blockDim.x + threadIdx.x;
   const uint32_t moved = n_live - low;
@@ -360,6 +369,23 @@ __global__ void __launch_bounds__(256) compact_apply_kernel(CompactArgs a) {
     }
     a.table_out[e] = p;
   }
+}
+
+__global__ void __launch_bounds__(kPageThreads) compact_rank_kernel(CompactArgs a) {
+  __shared__ uint32_t part[17];
+  compact_rank(a, part);
+}
+
+__global__ void __launch_bounds__(256) compact_apply_kernel(CompactArgs a) { compact_apply(a); }
+
+__global__ void __launch_bounds__(kPageThreads) compact_kernel(CompactArgs a) {
+  __shared__ uint32_t part[17], below[kCompactChunk + 1];
+  __shared__ int32_t holes[kCompactChunk];
+  a.below = below;
+  a.holes = holes;
+  compact_rank(a, part);
+  __syncthreads();
+  compact_apply(a);
 }
 
 // ------------------------------------------------------------------------------------------------ copy

@@ -242,7 +242,11 @@ int maaso_kv_compact(maaso_instance* inst, const maaso_kv_pages* pages, int32_t*
                 ws.take<uint32_t>(pages->n_pages + 1u), ws.take<int32_t>(pages->n_pages)};
   if (!ws.fits) return MAASO_E_WORKSPACE;
   const uint64_t entries = std::max<uint64_t>((uint64_t)pages->n_rows * pages->width, pages->n_pages);
-  hipLaunchKernelGGL(compact_count_kernel, dim3(chunks), dim3(kPageThreads), 0, s, a);
+  if (chunks == 1u && entries <= kCompactEntries) {
+    hipLaunchKernelGGL(compact_kernel, dim3(1), dim3(kPageThreads), 0, s, a);
+    return launched();
+  }
+  if (chunks > 1u) hipLaunchKernelGGL(compact_count_kernel, dim3(chunks), dim3(kPageThreads), 0, s, a);
   hipLaunchKernelGGL(compact_rank_kernel, dim3(chunks), dim3(kPageThreads), 0, s, a);
   hipLaunchKernelGGL(compact_apply_kernel, dim3((uint32_t)std::min<uint64_t>(2048u, (entries + 255u) / 256u)), dim3(256), 0, s, a);
   return launched();

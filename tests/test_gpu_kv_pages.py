@@ -322,3 +322,23 @@ def test_captured_calls_replay(inst):
         b.extend([2], [17])
         b.trim([2], [0])
     assert I.maaso_instance_status(inst) == 0
+
+
+@pytest.mark.parametrize("n_pages, rows, width", [(4096, 3, 1000), (4096, 64, 512), (4095, 64, 513), (4097, 5, 700), (100, 2000, 17)])
+def test_compact_pools_of_one_chunk_and_of_two(inst, n_pages, rows, width):
+    """Pools and tables on both sides of what one block takes in one launch."""
+    rng = np.random.default_rng(n_pages + rows)
+    b = Both(inst, n_pages, 16, rows, width)
+    live = np.sort(rng.permutation(n_pages)[:n_pages * 2 // 3])
+    of = rng.integers(0, rows, len(live))
+    for r in range(rows):
+        mine = rng.permutation(live[of == r])[:width]
+        b.m.table[r, :len(mine)] = mine
+        b.m.length[r] = 16 * len(mine)
+        b.m.refs[mine] = 1
+    b.refs.copy_(dev(b.m.refs))
+    b.table.copy_(dev(b.m.table))
+    b.length.copy_(dev(b.m.length))
+    b.compact(in_place=False)
+    b.compact(in_place=True)
+    assert I.maaso_instance_status(inst) == 0
