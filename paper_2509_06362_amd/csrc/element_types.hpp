@@ -18,6 +18,10 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
+// Before and after the stores of a branch that go past the caches: the compiler would make one of the two branches' stores,
+// and forget which kind they are.
+__device__ inline void keep_apart() { asm volatile("" ::: "memory"); }
+
 struct E4m3 { uint8_t bits; };  // the 8-bit type of a cache, as a template's argument
 
 template <typename T> struct Vec;

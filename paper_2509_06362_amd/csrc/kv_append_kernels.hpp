@@ -1,6 +1,7 @@
 // New tokens' queries, keys and values: norm of each head, position rotation, and the write into the cache's
 // pages, in one pass over the data.  Bound by memory (2 bytes in and 2 out per element, some 7 operations): 7000 tokens of 32
-// and 8 heads of 128 in 28 us, 3.9 TB/s, of which a copy reaches 4.8; 64 tokens in 5 us, a launch's time.
+// and 8 heads of 128 in 23 us, 4.7 TB/s, of which a copy reaches 4.8 (29 us before queries of more than the L2s hold, 32 MiB,
+// were written past them); 64 tokens in 5 us, a launch's time.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -32,6 +33,7 @@ struct AppendArgs {
   uint32_t n_tok, n_heads, n_kv_heads, rotary, n_pos, page_log2;
   uint32_t value_blocks;  // blocks that take values, the longer work, before those that take heads; 0: with the heads
   float eps;
+  bool past;  // queries are written past the caches
   uint32_t* status;
 };
 
@@ -41,7 +43,16 @@ template <typename T> struct Eight {
   struct __attribute__((packed, aligned(2))) at { x8 v; };
 };
 template <typename T> __device__ inline typename Vec<T>::x8 load8(const T* p) { return reinterpret_cast<const typename Eight<T>::at*>(p)->v; }
-template <typename T> __device__ inline void store8(T* p, typename Vec<T>::x8 v) { reinterpret_cast<typename Eight<T>::at*>(p)->v = v; }
+template <typename T> __device__ inline void store8(T* p, typename Vec<T>::x8 v, bool past) {
+  typedef uint32_t sixteen __attribute__((ext_vector_type(4), aligned(2)));
+  if (past) {
+    keep_apart();
+    __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), reinterpret_cast<sixteen*>(p));
+    keep_apart();
+  } else {
+    reinterpret_cast<typename Eight<T>::at*>(p)->v = v;
+  }
+}
 
 // One element of a page, in the cache's type.
 template <typename T, typename C>
@@ -138,7 +149,7 @@ __device__ inline void append_heads(const AppendArgs& a, uint32_t block, bool va
     }
     if (!inside[u]) continue;
     if (is_q) {
-      store8<T>(static_cast<T*>(a.q_out) + tok * a.q_out_stride + (uint64_t)h * D + lane * 8u, narrow8<T>(x));
+      store8<T>(static_cast<T*>(a.q_out) + tok * a.q_out_stride + (uint64_t)h * D + lane * 8u, narrow8<T>(x), a.past);
       continue;
     }
     const int64_t slot = a.slot[tok];

@@ -1,7 +1,7 @@
 // Logits as the next token is chosen from: penalties for what has been said, biases, temperature, a grammar's mask,
 // and the token of the largest value, in one pass over the logits.  Bound by memory, the row in, the row out, and by the
 // instructions of tokens that the history or a bias marks: 192 rows of 131,072 (16 bits in, 32 out, half of them masked) in
-// 49 us, 3.1 TB/s; one row of 50,257 in 7.
+// 43 us, 3.6 TB/s; one row of 50,257 in 7.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -21,6 +21,9 @@ namespace maaso {
 // row in 1024 a block without the second launch 10.3 for 13.0.
 constexpr uint32_t kManyThreads = 256, kManyPieces = 2, kFewThreads = 128, kFewPieces = 1;
 constexpr uint32_t kManySlice = 8u * kManyThreads * kManyPieces, kFewSlice = 8u * kFewThreads * kFewPieces;
+// Outputs of more than 8 MiB whose rows begin at multiples of 16 bytes are written past the caches: the 192 rows 50 to 43 us, 18 rows
+// of 131,072 10.2 to 9.6; 5 rows 7.1 to 7.3, and 126 rows of 100,003 16-bit logits, whose pieces lie across lines, 21.5 to 23.5.
+constexpr uint64_t kLogitPast = 8u << 20;
 constexpr uint32_t kFewRows = 1024;  // rows that the instance keeps a LogitsRow for
 // A token's mark: how often the history has it, and above kCountBits the number of its bias among the row's, from 1 on.  Rows
 // of a longer history or more biases mark a bias by the highest bit alone, and search for it.
@@ -53,6 +56,7 @@ struct LogitsArgs {
   const int32_t* bias_start;
   const uint32_t* mask;
   const int32_t* mask_row;
+  bool past;                 // what is written goes past the caches
   unsigned long long* best;  // workspace [n][slices], many rows
   LogitsRow* meet;           // [n], few rows
   uint32_t* status;
@@ -232,7 +236,16 @@ __global__ void __launch_bounds__(kThreads) logits_kernel(LogitsArgs a) {
 #pragma unroll
       for (int k = 0; k < 8; ++k) o.v[k] = (O)x[k];
       if (i0 + 8u <= n) {
-        *reinterpret_cast<Piece<O>*>(out + i0) = o;
+        if (a.past) {
+          typedef uint32_t sixteen __attribute__((ext_vector_type(4), aligned(2)));
+          keep_apart();
+#pragma unroll
+          for (uint32_t w = 0; w < sizeof(O) / 2u; ++w)
+            __builtin_nontemporal_store(reinterpret_cast<const sixteen*>(&o)[w], reinterpret_cast<sixteen*>(out + i0) + w);
+          keep_apart();
+        } else {
+          *reinterpret_cast<Piece<O>*>(out + i0) = o;
+        }
       } else {
 #pragma unroll
         for (uint32_t k = 0; k < 8u; ++k)

@@ -264,7 +264,7 @@ int maaso_kv_copy(maaso_instance* inst, const maaso_kv_cache* cache, const int32
   InstanceCall call(inst, s);
   if (call.rc != MAASO_OK) return call.rc;
   CopyArgs a{pairs, n, cache->n_pages, (uint32_t)chunks, cache->n_layers, bytes, cache->page_stride * size, cache->layer_stride * size,
-             static_cast<char*>(cache->k), static_cast<char*>(cache->v), inst->status};
+             static_cast<char*>(cache->k), static_cast<char*>(cache->v), bytes * n * cache->n_layers * 2u > kCopyPast, inst->status};
   hipLaunchKernelGGL(copy_kernel, dim3((uint32_t)(chunks * n), cache->n_layers, 2), dim3(256), 0, s, a);
   return launched();
 }
@@ -367,6 +367,7 @@ int maaso_kv_append(maaso_instance* inst, const maaso_kv_cache* cache, uint32_t 
   a.n_slots = (uint64_t)cache->n_pages << a.page_log2;
   a.n_tok = p->n_tok; a.n_heads = p->n_heads; a.n_kv_heads = cache->n_kv_heads; a.rotary = p->rotary; a.n_pos = p->n_pos;
   a.eps = p->eps;
+  a.past = (uint64_t)p->n_tok * p->n_heads * d * 2u > kCopyPast;
   a.status = inst->status;
   const bool turned = p->n_tok >= 512u;  // values through shared memory
   const uint64_t heads = p->n_heads + cache->n_kv_heads * (turned ? 1u : 2u), per = 256u / (d / 8u) * kAppendHeads;
@@ -501,6 +502,8 @@ int maaso_logits_adjust(maaso_instance* inst, const maaso_logits_args* p, void* 
     a.meet = inst->rows;
   }
   if ((uint64_t)a.n * a.slices > 0x7fffffffull) return MAASO_E_SHAPE;
+  const uint64_t out_size = element_size(p->out_type);
+  a.past = p->out && (uint64_t)p->n * p->vocab * out_size > kLogitPast && aligned(p->out, 16) && (p->n == 1u || p->out_stride * out_size % 16u == 0u);
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
   InstanceCall call(inst, s);
   if (call.rc != MAASO_OK) return call.rc;
