@@ -23,6 +23,7 @@
 #include "../../include/maaso_instance.h"
 #include "element_types.hpp"
 #include "kv_pages_kernels.hpp"
+#include "page_walk.hpp"
 
 namespace maaso {
 
@@ -180,17 +181,16 @@ struct ItemKeys {
 
 // The end of an item's keys [begin, end), begin < end, as far as its page list holds pages: a bad entry is not followed, what
 // lies behind it in the item is left out.  All lanes of the wave have the same item; `entries` becomes the list's first 64
-// entries from begin's page on, a lane each.
+// entries from begin's page on, a lane each, from a bad one on 0.
 __device__ inline uint32_t held_end(const AttentionArgs& a, const int32_t* list, uint32_t begin, uint32_t end, int32_t& entries) {
   const uint32_t first = begin >> a.page_log2, last = (end - 1u) >> a.page_log2, lane = threadIdx.x & 63u;
   for (uint32_t page0 = first; page0 <= last; page0 += 64u) {
     const int32_t page = page0 + lane <= last ? list[page0 + lane] : 0;
-    if (page0 == first) entries = page;
     const uint64_t bad = __ballot(page < 0 || (uint32_t)page >= a.n_pages);
+    if (page0 == first) entries = kept_entry(page, bad, lane);
     if (bad) {
       raise(a.status, MAASO_INST_BAD_PAGE);
-      const uint32_t stop = (page0 + (uint32_t)__builtin_ctzll(bad)) << a.page_log2;
-      return stop < begin ? begin : stop;
+      return end_before(page0, (uint32_t)__builtin_ctzll(bad), a.page_log2, begin);
     }
   }
   return end;
@@ -338,15 +338,15 @@ struct StreamTile {
   // The keys from `base` on, a multiple of 32: two pages at most.
   __device__ inline void ask(const AttentionArgs& a, Step& s, uint32_t base) {
     const uint32_t lane = threadIdx.x & 63u, col = lane & 15u, g = lane >> 4, per = 1u << a.page_log2;
-    const uint32_t last = (end - 1u) >> a.page_log2, page_at = base >> a.page_log2;
-    if (page_at - entry0 >= 63u) {
+    const uint32_t page_at = base >> a.page_log2;
+    if (beyond_entries(page_at, entry0)) {
       entry0 = page_at;
       const uint32_t page = entry0 + lane;  // (a step may begin a page before the item, where held_end() has not looked)
-      entries = page <= last && page >= begin >> a.page_log2 ? list[page] : 0;
+      entries = page_of_item(page, begin, end, a.page_log2) ? list[page] : 0;
     }
-    const int32_t at = (int32_t)uniform(page_at - entry0);
-    const uint32_t page0 = (uint32_t)__builtin_amdgcn_readlane(entries, at);
-    const uint32_t page1 = (uint32_t)__builtin_amdgcn_readlane(entries, per < 32u ? at + 1 : at);
+    const uint32_t at = uniform(page_at - entry0);
+    const uint32_t page0 = (uint32_t)__builtin_amdgcn_readlane(entries, (int)at);
+    const uint32_t page1 = (uint32_t)__builtin_amdgcn_readlane(entries, (int)second_entry(at, a.page_log2));
     const uint32_t kpage = col >> 3 ? page1 : page0, vpage = g >> 1 ? page1 : page0;
     const uint32_t row = (base + 8u * (col >> 2) + (col & 3u)) & (per - 1u);
     const C* kr = kp + (uint64_t)kpage * a.page_stride + row * (uint32_t)D + g * 8u;
@@ -832,7 +832,7 @@ __device__ inline void tile_block(const AttentionArgs& a, uint32_t block, char* 
   // The table's entry for keys at + 8 (lane % (kKeys / 8)), 0 outside the item.
   auto entry_at = [&](uint32_t at) {
     const uint32_t key8 = at + 8u * (lane % (kKeys / 8));
-    return key8 < end && (key8 | 15u) >= begin ? list[key8 >> a.page_log2] : 0;  // (a wave's key rows go by the page of the first of sixteen)
+    return eight_of_item(key8, begin, end) ? list[key8 >> a.page_log2] : 0;
   };
   const uint32_t first = begin & ~(uint32_t)(kKeys - 1);
   uint32_t buffer = 0;
@@ -841,7 +841,7 @@ __device__ inline void tile_block(const AttentionArgs& a, uint32_t block, char* 
     // (the first step's pages are among those that held_end() has looked at: five at most)
     const uint32_t key8 = first + 8u * (lane % (kKeys / 8)), nth = (key8 >> a.page_log2) - (begin >> a.page_log2);
     const int32_t page = __shfl(held, (int)(nth & 63u));
-    tile.bring(0, first, key8 < end && (key8 | 15u) >= begin ? page : 0);
+    tile.bring(0, first, eight_of_item(key8, begin, end) ? page : 0);
     tile.settle(0);
     entry = entry_at(first + kKeys);
   }
