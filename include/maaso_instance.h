@@ -164,7 +164,8 @@ int maaso_kv_append(maaso_instance* inst, const maaso_kv_cache* cache, uint32_t 
 /* Attention of n sequences' newest tokens to all that their rows hold.  Sequence i is row rows[i] of the
  * pages (rows NULL: row i) and has the queries q_start[i] .. q_start[i + 1] - 1, which are the last tokens of
  * the row: query j of n_q sees the keys before position length - n_q + j + 1.  Query head h reads key head
- * h / (n_heads / n_kv_heads).
+ * h / (n_heads / n_kv_heads).  The sequences need not fill n_tok, and may have no queries (idle places of a captured
+ * step): queries before q_start[0] or from q_start[n] on are of no sequence, and their out and lse are left as they are.
  *   out = sum_t softmax_t(scale * q . k_t) v_t,   lse = log sum_t exp(scale * q . k_t)
  * A query that sees no key gets out = 0, lse = -infinity.  What lies behind the keys that a query sees
  * has no part in its result, whatever it holds, infinities and NaN included.

@@ -130,9 +130,10 @@ __device__ inline uint32_t shared_of(const AttentionArgs& a, uint32_t i, GroupLa
   return found;
 }
 
-// The sequence of token t: the last one that begins at t or before.
+// The sequence of token t: the last one that begins at t or before (t may lie behind its end, or before the first: then it is of
+// none).  Where each sequence may have its one token it is looked for at its own place first.
 __device__ inline uint32_t sequence_of(const AttentionArgs& a, uint32_t t) {
-  if (a.max_q == 1u && a.n_tok == a.n) return t;
+  if (a.max_q == 1u && a.n_tok == a.n && a.q_start[t] == (int32_t)t && a.q_start[t + 1u] == (int32_t)t + 1) return t;
   uint32_t lo = 0, hi = a.n;
   while (hi - lo > 1u) {
     const uint32_t mid = (lo + hi) >> 1;
@@ -1030,7 +1031,7 @@ __global__ void __launch_bounds__(256) attention_join_kernel(AttentionArgs a) {
       if (a.n_groups) groups = groups_from(a, 0u);
       s = sequence_span(a, i);
       const bool mine = tok >= s.tok0 && tok - s.tok0 < s.n_q;
-      of = mine ? row_parts(a, s.len, shared_of(a, i, groups)) : RowParts{0u, 0u, 0u};
+      of = mine ? row_parts(a, s.len, shared_of(a, i, groups)) : RowParts{0u, 1u, 0u};  // (of no sequence: left alone)
       known = mine ? s.tok0 + s.n_q : tok + 1u;
     }
     if (of.n_shared == 0u && of.n_own == 1u) {  // (written already)

@@ -287,15 +287,15 @@ void launch_append_d(uint32_t d, const AppendArgs& a, uint32_t blocks, bool inte
 }
 
 // Few rows of a sequence or group go through the stream kernel, more through the tile kernel; which, the kernels see
-// from the device's arrays, the host leaves out a launch that would have nothing.
+// from the device's arrays.  The bounds tell the host whether there can be tiles, but not that there is nothing of few rows:
+// n * max_q == n_tok does not say that every sequence has max_q queries, for they need not fill n_tok.
 template <typename T, typename C, int D>
 void launch_attention(AttentionArgs a, hipStream_t s) {
   const uint32_t heads = a.n_kv_heads;
   const bool tiles = a.max_q * a.group > kStreamRows, shared_tiles = a.shared_parts && (uint64_t)a.n_tok * a.group > kStreamRows;
-  const bool few = !tiles || a.n_groups || (uint64_t)a.n * a.max_q != a.n_tok;
   a.stream_shared = a.n_groups * heads * a.shared_parts;
   const uint32_t items = a.stream_shared + a.n * heads * a.own_parts;
-  a.stream_blocks = !few ? 0u : a.alone ? (items + 3u) / 4u : items;
+  a.stream_blocks = a.alone ? (items + 3u) / 4u : items;
   if (tiles || shared_tiles) {
     a.tile_shared = shared_tiles ? a.shared_tiles * heads * a.shared_parts : 0u;
     a.tile_blocks = a.tile_shared + (tiles ? a.own_tiles * heads * a.own_parts : 0u);
