@@ -130,16 +130,21 @@ __device__ inline uint32_t shared_of(const AttentionArgs& a, uint32_t i, GroupLa
   return found;
 }
 
-// The sequence of token t: the last one that begins at t or before (t may lie behind its end, or before the first: then it is of
-// none).  Where each sequence may have its one token it is looked for at its own place first.
-__device__ inline uint32_t sequence_of(const AttentionArgs& a, uint32_t t) {
-  if (a.max_q == 1u && a.n_tok == a.n && a.q_start[t] == (int32_t)t && a.q_start[t + 1u] == (int32_t)t + 1) return t;
+// The sequence i of token t: the last one that begins at t or before (t may lie behind its end, or before the first: then it
+// is of none).  Where each sequence may have its one token, the span at its own place is looked at first.
+__device__ inline SequenceSpan sequence_of(const AttentionArgs& a, uint32_t t, uint32_t& i) {
+  if (a.max_q == 1u && a.n_tok == a.n) {
+    i = t;
+    const SequenceSpan s = sequence_span(a, i);
+    if (t - s.tok0 < s.n_q) return s;
+  }
   uint32_t lo = 0, hi = a.n;
   while (hi - lo > 1u) {
     const uint32_t mid = (lo + hi) >> 1;
     if ((uint32_t)a.q_start[mid] <= t) lo = mid; else hi = mid;
   }
-  return lo;
+  i = lo;
+  return sequence_span(a, i);
 }
 
 // Tile `tile` of `rows` rows, counted through the sequences (or groups) with more than kStreamRows rows: which one, and
@@ -258,7 +263,8 @@ __device__ inline bool item_keys(const AttentionArgs& a, bool is_shared, uint32_
 // Keys that token tok of the item sees.
 __device__ inline uint32_t row_limit(const AttentionArgs& a, bool is_shared, const ItemKeys& k, uint32_t tok) {
   if (!is_shared) return seen_keys({k.page_row, k.tok0, k.n_q, k.len}, k.n_q, tok - k.tok0);
-  const SequenceSpan s = sequence_span(a, sequence_of(a, tok));
+  uint32_t i;
+  const SequenceSpan s = sequence_of(a, tok, i);
   return seen_keys(s, s.n_q, tok - s.tok0);
 }
 
@@ -1026,10 +1032,10 @@ __global__ void __launch_bounds__(256) attention_join_kernel(AttentionArgs a) {
   RowParts of{0u, 0u, 0u};
   for (uint32_t tok = blockIdx.x * kTokens; tok < blockIdx.x * kTokens + kTokens && tok < a.n_tok; ++tok) {
     if (tok >= known) {
-      const uint32_t i = sequence_of(a, tok);
+      uint32_t i;
       GroupLanes groups{-1, -1, 0};
       if (a.n_groups) groups = groups_from(a, 0u);
-      s = sequence_span(a, i);
+      s = sequence_of(a, tok, i);
       const bool mine = tok >= s.tok0 && tok - s.tok0 < s.n_q;
       of = mine ? row_parts(a, s.len, shared_of(a, i, groups)) : RowParts{0u, 1u, 0u};  // (of no sequence: left alone)
       known = mine ? s.tok0 + s.n_q : tok + 1u;
