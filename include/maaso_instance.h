@@ -13,8 +13,9 @@
  * host synchronisation and can be captured into a graph.  An instance serves one call at a time: calls on
  * one stream are ordered by it, a call on another stream than the previous one is ordered behind it with
  * an event, a second thread meanwhile gets MAASO_E_BUSY.  A call that is being captured is not ordered
- * with earlier ones, and a graph's replays share the instance's workspace with other calls: the caller
- * orders both.
+ * with earlier ones, a call on another stream is not ordered behind a previous call whose stream is being
+ * captured by then, and a graph's replays share the instance's workspace with other calls: the caller
+ * orders all three (by the event or synchronisation with which it begins the capture, for the first two).
  *
  * What the host cannot see (page numbers, rows, lengths, tokens) the kernels check: an entry out of its
  * range is never followed, and raises a bit that maaso_instance_status returns.

@@ -32,7 +32,9 @@ struct maaso_instance {
 
 namespace {
 
-// Exclusive use by one call, and order behind the previous call's stream (calls that are captured are left to the caller).
+// Exclusive use by one call, and order behind the previous call's stream (calls that are captured are left to the caller, and
+// so is the order behind a stream that is being captured by now: an event recorded there would be a node of its graph, and the
+// wait for it would draw this call's stream into the capture).
 struct InstanceCall {
   maaso_instance* inst;
   DeviceGuard device;
@@ -47,7 +49,7 @@ struct InstanceCall {
     if (!device.ok) { rc = MAASO_E_HIP; return; }
     if (inst->has_last && inst->last_stream == s) return;
     if (is_captured(s)) return;
-    if (inst->has_last) {
+    if (inst->has_last && !is_captured(inst->last_stream)) {
       const bool ordered = hipEventRecord(inst->order_ev, inst->last_stream) == hipSuccess &&
                            hipStreamWaitEvent(s, inst->order_ev, 0) == hipSuccess;
       if (!ordered) {

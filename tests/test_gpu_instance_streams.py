@@ -1,0 +1,44 @@
+"""The instance's calls on several streams, captures among them."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+from paper_2509_06362_amd import instance as I  # noqa: E402
+from tests.test_gpu_kv_attention import BF16, Batch, i32, inst  # noqa: E402, F401
+
+
+def attend(inst, b, rows, stream):  # noqa: F811
+    I.maaso_kv_attention(inst, b.view, b.pages, layer=0, q=b.q, out=b.out, lse=b.lse, q_start=b.q_start, rows=rows, scale=b.scale, max_q=max(b.new),
+                         max_len=max(b.total), total_len=sum(b.total), stream=stream)
+
+
+def test_a_call_elsewhere_while_the_previous_calls_stream_is_captured(inst):  # noqa: F811
+    """It runs, and is no part of the capture; the graph replays."""
+    one, two = Batch([3000, 40], [1, 2], 4, 2, 64, 16, BF16), Batch([2000, 70, 9], [1, 1, 1], 8, 2, 128, 32, BF16, seed=1)
+    rows = [i32(b.rows) for b in (one, two)]
+    here, there = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    attend(inst, one, rows[0], here)
+    torch.cuda.synchronize()
+    one.check()
+    two.out.fill_(9.0)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=here):
+        attend(inst, one, rows[0], here)
+        attend(inst, two, rows[1], there)
+    torch.cuda.synchronize()
+    two.check()
+    for _ in range(3):
+        one.out.fill_(9.0)
+        two.out.fill_(9.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        one.check()
+        assert (two.out == 9).all()
+        attend(inst, two, rows[1], there)
+        attend(inst, two, rows[1], here)
+        torch.cuda.synchronize()
+        two.check()
