@@ -61,7 +61,8 @@ typedef struct maaso_instance maaso_instance; /* opaque: a device, a workspace, 
 int maaso_instance_create(int device, uint64_t workspace_bytes, maaso_instance** out);
 void maaso_instance_destroy(maaso_instance* inst);
 /* Synchronises the device, returns the MAASO_INST_* bits raised since the last call in *bits (may be NULL)
- * and clears them.  MAASO_E_INVALID_ARG if there are any, else MAASO_OK. */
+ * and clears them.  MAASO_E_INVALID_ARG if there are any, else MAASO_OK.  Errors: INVALID_ARG (no instance),
+ * BUSY, HIP; *bits is 0 then. */
 int maaso_instance_status(maaso_instance* inst, uint32_t* bits);
 
 /* The pages of a cache: a pool of n_pages pages of page_size tokens, and rows of up to `width` pages.

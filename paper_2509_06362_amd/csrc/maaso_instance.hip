@@ -19,7 +19,7 @@ using namespace maaso;
 struct maaso_instance {
   int device;
   int n_cu;
-  uint32_t* status;  // device status word
+  uint32_t* status;  // device status word, and behind it the one that maaso_instance_status reads
   LogitsRow* rows;   // [kFewRows] behind it, zeros between calls
   char* ws;          // device workspace
   size_t ws_bytes;
@@ -67,6 +67,11 @@ struct InstanceCall {
   InstanceCall& operator=(const InstanceCall&) = delete;
 };
 
+// Takes the status bits and leaves none, in one step: a copy and a clear of their own would lose what is raised between them.
+__global__ void __launch_bounds__(64) take_status_kernel(uint32_t* status) {
+  if (threadIdx.x == 0) status[1] = atomicExch(status, 0u);
+}
+
 constexpr size_t kOwnBytes = 256u + kFewRows * sizeof(LogitsRow);  // the status word, then the rows
 
 int launched() { return hip_ok(hipGetLastError()) ? MAASO_OK : MAASO_E_HIP; }
@@ -85,6 +90,20 @@ struct Carve {
     return p;
   }
 };
+
+// The copy is behind the kernel on the null stream and has come when it returns: nothing is under way then that later calls,
+// on streams that do not wait for the null stream, could run beside.
+int take_status(maaso_instance* in, uint32_t* bits) {
+  DeviceGuard guard(in->device);
+  if (!guard.ok) return MAASO_E_HIP;
+  uint32_t v = 0;
+  if (!hip_ok(hipDeviceSynchronize())) return MAASO_E_HIP;
+  hipLaunchKernelGGL(take_status_kernel, dim3(1), dim3(64), 0, nullptr, in->status);
+  if (!hip_ok(hipGetLastError())) return MAASO_E_HIP;
+  if (!hip_ok(hipMemcpy(&v, in->status + 1, 4, hipMemcpyDeviceToHost))) return MAASO_E_HIP;
+  if (bits) *bits = v;
+  return v ? MAASO_E_INVALID_ARG : MAASO_OK;
+}
 
 bool page_size_ok(uint32_t s) { return s == 16u || s == 32u || s == 64u || s == 128u; }
 uint32_t log2_of(uint32_t x) { return 31u - (uint32_t)__builtin_clz(x); }
@@ -169,14 +188,11 @@ void maaso_instance_destroy(maaso_instance* in) {
 int maaso_instance_status(maaso_instance* in, uint32_t* bits) {
   if (bits) *bits = 0;
   if (!in) return MAASO_E_INVALID_ARG;
-  DeviceGuard guard(in->device);
-  if (!guard.ok) return MAASO_E_HIP;
-  uint32_t v = 0;
-  if (!hip_ok(hipDeviceSynchronize())) return MAASO_E_HIP;
-  if (!hip_ok(hipMemcpy(&v, in->status, 4, hipMemcpyDeviceToHost))) return MAASO_E_HIP;
-  if (v != 0 && !hip_ok(hipMemset(in->status, 0, 4))) return MAASO_E_HIP;
-  if (bits) *bits = v;
-  return v ? MAASO_E_INVALID_ARG : MAASO_OK;
+  int idle = 0;
+  if (!in->in_call.compare_exchange_strong(idle, 1, std::memory_order_acquire)) return MAASO_E_BUSY;
+  const int rc = take_status(in, bits);
+  in->in_call.store(0, std::memory_order_release);
+  return rc;
 }
 
 int maaso_kv_extend(maaso_instance* inst, const maaso_kv_pages* pages, const int32_t* rows, uint32_t n, const int32_t* q_start,

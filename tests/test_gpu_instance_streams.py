@@ -42,3 +42,15 @@ def test_a_call_elsewhere_while_the_previous_calls_stream_is_captured(inst):  # 
         attend(inst, two, rows[1], here)
         torch.cuda.synchronize()
         two.check()
+
+
+def test_a_bit_raised_behind_the_status_call_is_kept(inst):  # noqa: F811
+    """The clear has been made when the call returns, also for streams that do not wait for the null stream."""
+    vocab, streams = 100, [torch.cuda.Stream() for _ in range(3)]
+    logits, chosen, start = torch.zeros(1, vocab, device="cuda"), i32([0]), i32([0, 1])
+    bad, good = i32([vocab]), i32([5])
+    torch.cuda.synchronize()
+    for k in range(60):
+        for history, want in ((bad, I.BAD_TOKEN), (bad, I.BAD_TOKEN), (good, 0)):
+            I.maaso_logits_adjust(inst, logits=logits, chosen=chosen, history=history, history_start=start, stream=streams[k % 3])
+            assert I.maaso_instance_status(inst) == want
