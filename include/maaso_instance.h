@@ -16,6 +16,8 @@
  * with earlier ones, a call on another stream is not ordered behind a previous call whose stream is being
  * captured by then, and a graph's replays share the instance's workspace with other calls: the caller
  * orders all three (by the event or synchronisation with which it begins the capture, for the first two).
+ * Calls that ran at once all the same may have given wrong results; once none runs, maaso_instance_status
+ * puts the instance in order again.
  *
  * What the host cannot see (page numbers, rows, lengths, tokens) the kernels check: an entry out of its
  * range is never followed, and raises a bit that maaso_instance_status returns.

@@ -20,7 +20,7 @@ struct maaso_instance {
   int device;
   int n_cu;
   uint32_t* status;  // device status word, and behind it the one that maaso_instance_status reads
-  LogitsRow* rows;   // [kFewRows] behind it, zeros between calls
+  LogitsRow* rows;   // [kFewRows] behind it, zeros between calls (made so again by maaso_instance_status)
   char* ws;          // device workspace
   size_t ws_bytes;
   // one call at a time, as for maaso_ctx
@@ -68,9 +68,15 @@ struct InstanceCall {
 };
 
 // Takes the status bits and leaves none, in one step: a copy and a clear of their own would lose what is raised between them.
-__global__ void __launch_bounds__(64) take_status_kernel(uint32_t* status) {
-  if (threadIdx.x == 0) status[1] = atomicExch(status, 0u);
+// The rows are made zeros, as calls leave them: two few-row calls that have run at once, which the caller has to order, may
+// have left counts behind that every later call would go wrong by.
+__global__ void __launch_bounds__(256) take_status_kernel(uint32_t* status, LogitsRow* rows) {
+  const uint32_t i = blockIdx.x * 256u + threadIdx.x;
+  rows[i].key = 0ull;
+  rows[i].done = 0u;
+  if (i == 0u) status[1] = atomicExch(status, 0u);
 }
+static_assert(kFewRows % 256u == 0u, "a thread to a row");
 
 constexpr size_t kOwnBytes = 256u + kFewRows * sizeof(LogitsRow);  // the status word, then the rows
 
@@ -98,7 +104,7 @@ int take_status(maaso_instance* in, uint32_t* bits) {
   if (!guard.ok) return MAASO_E_HIP;
   uint32_t v = 0;
   if (!hip_ok(hipDeviceSynchronize())) return MAASO_E_HIP;
-  hipLaunchKernelGGL(take_status_kernel, dim3(1), dim3(64), 0, nullptr, in->status);
+  hipLaunchKernelGGL(take_status_kernel, dim3(kFewRows / 256u), dim3(256), 0, nullptr, in->status, in->rows);
   if (!hip_ok(hipGetLastError())) return MAASO_E_HIP;
   if (!hip_ok(hipMemcpy(&v, in->status + 1, 4, hipMemcpyDeviceToHost))) return MAASO_E_HIP;
   if (bits) *bits = v;

@@ -1,4 +1,6 @@
 """The instance's calls on several streams, captures among them."""
+import ctypes as C
+
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -54,3 +56,21 @@ def test_a_bit_raised_behind_the_status_call_is_kept(inst):  # noqa: F811
         for history, want in ((bad, I.BAD_TOKEN), (bad, I.BAD_TOKEN), (good, 0)):
             I.maaso_logits_adjust(inst, logits=logits, chosen=chosen, history=history, history_start=start, stream=streams[k % 3])
             assert I.maaso_instance_status(inst) == want
+
+
+def test_the_status_call_puts_the_instance_in_order(inst):  # noqa: F811
+    """What calls of few rows of logits keep between their blocks, as calls that ran at once may leave it, is cleared."""
+    lib, vocab = I._library(), 50257
+    logits = torch.randn(3, vocab, generator=torch.Generator().manual_seed(1)).cuda()
+    chosen = torch.empty(3, dtype=torch.int32, device="cuda")
+    with I.maaso_instance_create() as spoilt:
+        assert C.c_int32.from_address(spoilt.handle + 4).value == torch.cuda.get_device_properties(0).multi_processor_count
+        status = C.c_void_p.from_address(spoilt.handle + 8).value  # the rows lie 256 bytes behind it, 128 bytes each
+        torch.cuda.synchronize()
+        assert lib.hipMemset(C.c_void_p(status + 256), 1, C.c_size_t(1024 * 128)) == 0
+        torch.cuda.synchronize()
+        assert I.maaso_instance_status(spoilt) == 0
+        for _ in range(3):
+            chosen.fill_(-7)
+            I.maaso_logits_adjust(spoilt, logits=logits, chosen=chosen)
+            assert torch.equal(chosen.long(), logits.argmax(1))
