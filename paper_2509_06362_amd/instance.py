@@ -201,7 +201,7 @@ def maaso_instance_status(inst: Instance) -> int:
     """Synchronises; returns and clears the MAASO_INST_* bits."""
     bits = C.c_uint32(0)
     rc = _library().maaso_instance_status(inst.handle, C.byref(bits))
-    if rc not in (0, -1):
+    if rc not in (0, -1) or (rc == -1 and not bits.value):  # (INVALID_ARG with bits is what they are read by)
         raise MaasoError(rc, "maaso_instance_status")
     return int(bits.value)
 
