@@ -56,6 +56,12 @@ float real(PyObject* o) {
   return (float)v;
 }
 
+bool truth(PyObject* o) {
+  const int v = PyObject_IsTrue(o);
+  if (v < 0) throw Refused{};
+  return v != 0;
+}
+
 template <typename T> T* address(PyObject* o) { return reinterpret_cast<T*>((uintptr_t)whole(o)); }
 
 uint32_t type_of(const at::Tensor& t) {
@@ -218,7 +224,7 @@ PyObject* append(PyObject*, Args a, Py_ssize_t n) {
     p.q_weight = buffer(a[10], type, dim);
     p.k_weight = buffer(a[11], type, dim);
     p.eps = real(a[12]);
-    p.interleaved = PyObject_IsTrue(a[13]) == 1;
+    p.interleaved = truth(a[13]);
     void* s = stream(a[14]);
     return [=] { return call_append(inst, cache, layer, &p, s); };
   });
