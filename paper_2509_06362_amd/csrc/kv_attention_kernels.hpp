@@ -677,10 +677,14 @@ struct RowTile {
   static __device__ inline uint32_t fv(uint32_t row) { return by_lane(row, kKeys / 8); }
 
   // 16 bytes a lane from the pages to 1024 bytes of shared memory from `to` on.  Written out, because the compiler would
-  // have every later read of shared memory wait for it; the loop waits itself, once a step.
+  // have every later read of shared memory wait for it; the loop waits itself, once a step.  (m0 is named as changed, so that
+  // none of the compiler's own uses of it, from its setting on, has this between; that it warns of, as of any reserved register.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
   __device__ inline void async16(const void* from, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_base + to), "v"(from) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_base + to), "v"(from) : "memory", "m0");
   }
+#pragma clang diagnostic pop
 
   // Brings keys and values from `base` on; ids: lane c < kKeys / 8 (and every kKeys / 8 after it) holds the page of keys base + 8 c.
   __device__ inline void bring(uint32_t buffer, uint32_t base, int32_t ids) {
