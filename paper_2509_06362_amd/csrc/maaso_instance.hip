@@ -457,15 +457,20 @@ int maaso_kv_attention(maaso_instance* inst, const maaso_kv_cache* cache, uint32
     const uint32_t chunk = std::max(256u, round_up((keys + parts - 1u) / parts, 256u));
     return items < 8u * cus ? std::min(chunk, 2048u) : chunk;
   };
-  a.alone = p->n * heads >= 4096u;
+  const uint64_t total = p->total_len && p->total_len < p->n * most_len ? p->total_len : p->n * most_len;
+  const uint64_t in_common = (uint64_t)p->n * a.most_shared, own = total > in_common ? total - in_common : p->n;
+  // Items to a wave each, where there are many of few keys: four waves that share one have little to do and wait for each other
+  // twice.  512 to 1024 sequences of 8 key heads (heads of 256: 1024 of 4), a block to an item against a wave, us: heads of 64
+  // in 16 bits, 64 keys 25 : 16, 300 keys 68 : 66, 500 keys 97 : 105; in 8 bits, 300 keys 41 : 34, 1000 keys 96 : 100; heads of 256, 200
+  // keys 212 : 164, 1000 keys 726 : 724; heads of 128 in 8 bits, 200 keys 60 : 58, 300 keys 74 : 78; in 16 bits, 40 keys 42 : 30,
+  // 100 keys 58 : 61, 300 keys 126 : 143.
+  a.alone = p->n * heads >= 4096u && own <= p->n * (d == 128u && size == 2u ? 64u : 256u);
   const uint64_t places = (a.alone ? 8u : 4u) * cus;
   auto even = [&](uint64_t keys) { return std::max(a.alone ? 128u : 256u, round_up(keys * heads / places, 64u)); };
   if (tiles) {
     a.own_least = split(most_len, (uint64_t)a.own_tiles * heads);
     a.own_parts = (uint32_t)((most_len + a.own_least - 1u) / a.own_least);
   } else {
-    const uint64_t total = p->total_len && p->total_len < p->n * most_len ? p->total_len : p->n * most_len;
-    const uint64_t in_common = (uint64_t)p->n * a.most_shared, own = total > in_common ? total - in_common : p->n;
     a.own_least = a.alone ? 128u : 256u;
     const uint64_t chunk = even(own), parts = (most_len + chunk - 1u) / chunk;
     const uint64_t bound = (2u * own / p->n + a.own_least - 1u) / a.own_least + (places + p->n * heads - 1u) / (p->n * heads);
