@@ -54,10 +54,10 @@ template <typename T> __device__ inline void store8(T* p, typename Vec<T>::x8 v,
   }
 }
 
-// One element of a page, in the cache's type.
+// One element of a page, in the cache's type; scale: what 8 bits are multiplied by.
 template <typename T, typename C>
-__device__ inline void store_one(C* p, T x, float inv) {
-  if constexpr (sizeof(C) == 1) p->bits = (uint8_t)e4m3_pack4((float)x / inv, 0.0f, 0.0f, 0.0f);
+__device__ inline void store_one(C* p, T x, float scale) {
+  if constexpr (sizeof(C) == 1) p->bits = (uint8_t)e4m3_pack4((float)x / scale, 0.0f, 0.0f, 0.0f);
   else *p = x;
 }
 

@@ -621,7 +621,6 @@ __device__ inline void stream_block(const AttentionArgs& a, uint32_t block, Stre
   }
 }
 
-//
 // Blocks to a compute unit, by the registers they need: with heads of 128 three of one step each beat two of two steps (160
 // short sequences behind a shared beginning 110 to 105 us), with heads of 64 two steps have room beside three others.
 template <typename T, typename C, int D, int kSplit>
