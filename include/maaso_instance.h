@@ -180,8 +180,10 @@ int maaso_kv_append(maaso_instance* inst, const maaso_kv_cache* cache, uint32_t 
  * Sequences outside every group share nothing.
  *
  * max_q, max_len and max_shared bound the queries of a sequence, the length of a row and the tokens
- * shared; what lies beyond is left out and raises MAASO_INST_BAD_BOUND.  total_len is the sum of the rows'
- * lengths or an estimate of it (0: unknown); only the division of the work depends on it.
+ * shared; what lies beyond is left out and raises MAASO_INST_BAD_BOUND: queries from max_q on are left as
+ * they are, keys from max_len on are seen by nobody, and the others' results are as without them.
+ * total_len is the sum of the rows' lengths or an estimate of it (0: unknown); only the division of the
+ * work depends on it.
  * Errors: INVALID_ARG, SHAPE, WORKSPACE (parts of long or shared rows do not fit), BUSY, HIP. */
 typedef struct {
   uint32_t type;                 /* of q and out: BF16 or FP16; the cache has the same, or E4M3  */

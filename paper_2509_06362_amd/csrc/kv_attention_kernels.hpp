@@ -68,6 +68,7 @@ __device__ inline uint32_t uniform(uint32_t x) { return (uint32_t)__builtin_amdg
 // What a sequence or a group has of rows and keys, from the device's arrays; everything within its bounds.
 struct SequenceSpan {
   uint32_t row, tok0, n_q, len;
+  int32_t before;  // tokens that its row held before its queries, all of them (negative: it holds fewer than they are)
 };
 
 // (What does not depend on one another is asked for at once, good or not: each load that waits for another is most of a
@@ -76,7 +77,7 @@ __device__ inline SequenceSpan sequence_span(const AttentionArgs& a, uint32_t i)
   const int32_t q0 = a.q_start[i], q1 = a.q_start[i + 1], row = a.rows ? a.rows[i] : (int32_t)i;
   const bool known = row >= 0 && (uint32_t)row < a.n_rows;
   const int32_t len = a.length[known ? row : 0];
-  SequenceSpan s{0u, 0u, 0u, 0u};
+  SequenceSpan s{0u, 0u, 0u, 0u, 0};
   if (q0 < 0 || q1 < q0 || (uint32_t)q1 > a.n_tok) { raise(a.status, MAASO_INST_BAD_BOUND); return s; }
   s.tok0 = (uint32_t)q0;
   s.n_q = (uint32_t)(q1 - q0);
@@ -85,14 +86,15 @@ __device__ inline SequenceSpan sequence_span(const AttentionArgs& a, uint32_t i)
   s.row = (uint32_t)row;
   if (len < 0 || (uint64_t)len > (uint64_t)a.width << a.page_log2) { raise(a.status, MAASO_INST_BAD_ROW); return s; }
   s.len = (uint32_t)len;
+  s.before = len - (q1 - q0);
   if (s.len > a.max_len) { raise(a.status, MAASO_INST_BAD_BOUND); s.len = a.max_len; }
   return s;
 }
 
-// Keys that query j of the span sees.
-__device__ inline uint32_t seen_keys(const SequenceSpan& s, uint32_t q_all, uint32_t j) {
-  const int64_t limit = (int64_t)s.len - q_all + j + 1;
-  return limit < 0 ? 0u : (uint32_t)limit;
+// Keys that query j of a span sees, by the sequence's own length and queries, also where a bound leaves some of them out.
+__device__ inline uint32_t seen_keys(int32_t before, uint32_t len, uint32_t j) {
+  const uint32_t limit = (uint32_t)before + j + 1u;
+  return (int32_t)limit < 0 ? 0u : limit < len ? limit : len;
 }
 
 // Whether group g's sequences, and their queries, are a range.
@@ -181,7 +183,8 @@ __device__ inline bool find_tile(const AttentionArgs& a, bool groups, uint32_t r
 
 // An item's rows and keys.
 struct ItemKeys {
-  uint32_t tok0, n_rows, begin, end, page_row, n_q, len;
+  uint32_t tok0, n_rows, begin, end, page_row, len;
+  int32_t before;
   bool alone;  // its rows have no other part: their results are written as they are, not joined
 };
 
@@ -241,7 +244,7 @@ __device__ inline bool item_keys(const AttentionArgs& a, bool is_shared, uint32_
     if (a.n_groups) groups = groups_from(a, 0u);
     const SequenceSpan s = sequence_span(a, which);
     k.tok0 = s.tok0;
-    k.n_q = s.n_q;
+    k.before = s.before;
     k.len = s.len;
     k.n_rows = s.n_q * a.group;
     k.page_row = s.row;
@@ -262,10 +265,10 @@ __device__ inline bool item_keys(const AttentionArgs& a, bool is_shared, uint32_
 
 // Keys that token tok of the item sees.
 __device__ inline uint32_t row_limit(const AttentionArgs& a, bool is_shared, const ItemKeys& k, uint32_t tok) {
-  if (!is_shared) return seen_keys({k.page_row, k.tok0, k.n_q, k.len}, k.n_q, tok - k.tok0);
+  if (!is_shared) return seen_keys(k.before, k.len, tok - k.tok0);
   uint32_t i;
   const SequenceSpan s = sequence_of(a, tok, i);
-  return seen_keys(s, s.n_q, tok - s.tok0);
+  return seen_keys(s.before, s.len, tok - s.tok0);
 }
 
 // Eight neighbouring elements as they lie in a page: widened to operands; those of [from, to) kept and the others made zeros,
@@ -1031,7 +1034,7 @@ __global__ void __launch_bounds__(256) attention_join_kernel(AttentionArgs a) {
   const uint32_t h = (kSplit == 4 ? blockIdx.y : blockIdx.y * 4u + wave) * kHeads + lane / kLanes, at = lane % kLanes * 4u;
   const uint64_t rows = (uint64_t)a.n_tok * a.n_heads;
   uint32_t known = 0;  // the token behind the last one that `s` and `parts` are of
-  SequenceSpan s{0u, 0u, 0u, 0u};
+  SequenceSpan s{0u, 0u, 0u, 0u, 0};
   RowParts of{0u, 0u, 0u};
   for (uint32_t tok = blockIdx.x * kTokens; tok < blockIdx.x * kTokens + kTokens && tok < a.n_tok; ++tok) {
     if (tok >= known) {

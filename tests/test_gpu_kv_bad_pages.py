@@ -13,8 +13,8 @@ from tests.test_gpu_kv_attention import BF16, E4M3, FP16, Batch, inst  # noqa: E
 
 
 def check_seen(b, i, sees):
-    """Sequence i's results where its queries see the keys of `sees` [new, held + new]."""
-    half, group, at, w = torch.finfo(b.dtype).eps / 2, b.heads // b.kv, sum(b.new[:i]), b.new[i]
+    """Sequence i's results where its first queries see the keys of `sees` [queries, held + new]."""
+    half, group, at, w = torch.finfo(b.dtype).eps / 2, b.heads // b.kv, sum(b.new[:i]), len(sees)
     q, out, lse = b.q_host[at:at + w].double().cuda(), b.out[at:at + w].double(), b.lse[at:at + w].double()
     K = (b.K[i].float() * b.ks[:, None]).double().cuda().repeat_interleave(group, 1)
     V = (b.V[i].float() * b.vs[:, None]).double().cuda().repeat_interleave(group, 1)
