@@ -171,7 +171,9 @@ __global__ void __launch_bounds__(kThreads) logits_kernel(LogitsArgs a) {
       if (!good) {
         if (slice == 0) raise(a.status, MAASO_INST_BAD_TOKEN);
       } else if ((uint32_t)v - v0 < n) {
-        atomicOr(&mark[(uint32_t)v - v0], listed ? (i - bb + 1u) << kCountBits : kHasBias);
+        // (a token listed twice, out of order, is marked by ones: a number that no bias has)
+        const uint32_t old = atomicOr(&mark[(uint32_t)v - v0], listed ? (i - bb + 1u) << kCountBits : kHasBias);
+        if (listed && old >> kCountBits) atomicOr(&mark[(uint32_t)v - v0], ~0u << kCountBits);
       }
     }
     lds_atomics_barrier();
@@ -201,8 +203,8 @@ __global__ void __launch_bounds__(kThreads) logits_kernel(LogitsArgs a) {
           }
           if (c != times) {
             if (listed) {
-              const uint32_t at = c >> kCountBits, most = be - bb;  // (past the last: a token listed twice, out of order)
-              y = y + bias[(at < most ? at : most) - 1u];
+              const uint32_t at = c >> kCountBits;
+              if (at <= kListed) y = y + bias[at - 1u];
             } else {
               uint32_t lo = bb, hi = be;  // the entry that holds the token
               while (hi - lo > 1u) {
