@@ -23,8 +23,9 @@
  * range is never followed, and raises a bit that maaso_instance_status returns.
  *
  * Sums, softmax statistics and norms are binary32; a result is rounded once to its output's type, and
- * attention's weights (between 0 and 1) to 16 bits for the matrix units.  Results do not depend on the
- * order in which blocks run: a call repeated on the same inputs gives the same bits. */
+ * attention's weights to the queries' 16-bit type for the matrix units: half a step of it, relative to each
+ * weight (they are 2^(score - m), m a maximum so far that may lag, so at most 2^8).  Results do not depend on
+ * the order in which blocks run: a call repeated on the same inputs gives the same bits. */
 #ifndef MAASO_INSTANCE_H
 #define MAASO_INSTANCE_H
 

@@ -16,9 +16,9 @@
 namespace maaso {
 
 // A block takes a slice of a row, kPieces times eight neighbouring tokens a thread: 4096 tokens where there are rows enough
-// to fill the card (their marks are 16 KiB of LDS, eight blocks to a compute unit), 1024 where there are few.  The 192 rows with
-// 8192 tokens a block of 512 threads 60 us, of 256 threads 67, with 2048 tokens 66, against 56 before biases were listed; one
-// row in 1024 a block without the second launch 10.3 for 13.0.
+// to fill the card (their marks are 16 KiB of LDS, eight blocks to a compute unit), 1024 where there are few.  The 192 rows 43.1 us;
+// with 8192 tokens a block of 512 threads 43.1, of 256 threads 48.0, with 2048 tokens 43.7.  One row of 50,257 in 1024 a block,
+// without the second launch, 7.0 for 9.0.
 constexpr uint32_t kManyThreads = 256, kManyPieces = 2, kFewThreads = 128, kFewPieces = 1;
 constexpr uint32_t kManySlice = 8u * kManyThreads * kManyPieces, kFewSlice = 8u * kFewThreads * kFewPieces;
 // Outputs of more than 8 MiB whose rows begin at multiples of 16 bytes are written past the caches: the 192 rows 50 to 43 us, 18 rows
