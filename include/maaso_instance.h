@@ -1,6 +1,7 @@
-/* maaso_instance.h - C ABI of what a model instance does between its matrix products: the pages of its
- * key/value cache, the write of new keys and values, attention over the pages, and the adjustment of the
- * logits that a token is chosen from.
+/* maaso_instance.h - C ABI of what a model instance does between its plain matrix products: the pages of its
+ * key/value cache, the write of new keys and values, attention over the pages, the adjustment of the
+ * logits that a token is chosen from, rows brought to 8-bit integers and their products, and experts: the
+ * routing of tokens, the products over each expert's tokens, the joining of their outputs.
  *
  * The placer and the distributor (maaso.h) decide from a profile: seconds per decode step against the
  * instance's load, and prefill seconds against the prompt's length.  The entry points here are the parts of
@@ -39,13 +40,14 @@ typedef enum {
   MAASO_BF16 = 0,
   MAASO_FP16 = 1,
   MAASO_FP32 = 2,
-  MAASO_E4M3 = 3 /* 8 bits, 4 of them exponent, no infinity, largest value 448 */
+  MAASO_E4M3 = 3, /* 8 bits, 4 of them exponent, no infinity, largest value 448 */
+  MAASO_INT8 = 4  /* whole numbers of 8 bits */
 } maaso_type;
 
 /* bits of maaso_instance_status */
 #define MAASO_INST_BAD_PAGE 1u  /* a page number outside the pool, or one given back that nobody held       */
 #define MAASO_INST_BAD_ROW 2u   /* a row outside the table, a length outside the row, a fork into a row that
-                                   holds tokens                                                              */
+                                   holds tokens; a row outside an operand of a product or of a joining       */
 #define MAASO_INST_NO_PAGES 4u  /* maaso_kv_extend found too few free pages, or a row too narrow: it did
                                    nothing                                                                   */
 #define MAASO_INST_BAD_BOUND 8u /* q_start, group_start, or a start of a list runs backwards or past its end,
@@ -56,6 +58,9 @@ typedef enum {
 #define MAASO_INSTANCE_WORKSPACE_BYTES (256u << 20) /* what workspace_bytes = 0 selects */
 #define MAASO_KV_MAX_ROWS 65536u                    /* rows of one call                 */
 #define MAASO_KV_MAX_PAGES 16777216u                /* pages of a pool                  */
+#define MAASO_PRODUCT_MAX_IN 131071u                /* n_in of a product: what 8-bit integers' sums in 32 bits hold */
+#define MAASO_EXPERT_MAX 1024u                      /* experts                          */
+#define MAASO_EXPERT_MAX_CHOSEN 32u                 /* experts of a token               */
 
 typedef struct maaso_instance maaso_instance; /* opaque: a device, a workspace, a status word */
 
@@ -234,6 +239,112 @@ typedef struct {
   uint32_t n_mask;
 } maaso_logits_args;
 int maaso_logits_adjust(maaso_instance* inst, const maaso_logits_args* a, void* hip_stream);
+
+/* Rows of activations as 8-bit integers, with a scale for each row.  Of row t of x, y is
+ *   MAASO_ROWS_PLAIN:  x
+ *   MAASO_ROWS_NORM:   x / sqrt(mean(x^2) + eps) * weight           (weight NULL: 1)
+ *   MAASO_ROWS_GATED:  silu(x[i]) * x[width + i], silu(x) = x / (1 + exp(-x)); x has 2 * width elements
+ * and with m = max |y|:   scale[t] = m / 127,   q[t][i] = y * (127 / m), rounded to the nearest, ties to even.
+ * A row of zeros has q = 0, scale = 0.  A row that holds a NaN or an infinity in y, or whose sum of squares passes
+ * binary32, has q = 0, scale = NaN: products of it are NaN and nothing else is.  All DEVICE.
+ * Errors: INVALID_ARG, SHAPE, BUSY, HIP. */
+typedef enum { MAASO_ROWS_PLAIN = 0, MAASO_ROWS_NORM = 1, MAASO_ROWS_GATED = 2 } maaso_rows_form;
+typedef struct {
+  uint32_t type;               /* of x and weight: BF16, FP16 or FP32                             */
+  uint32_t form;               /* maaso_rows_form                                                 */
+  uint32_t n, width;
+  float eps;
+  uint64_t x_stride, q_stride; /* elements between rows; of q a multiple of 16                    */
+  const void* x;               /* [n][width], MAASO_ROWS_GATED: [n][2 * width]                    */
+  const void* weight;          /* [width] or NULL, MAASO_ROWS_NORM only                           */
+  int8_t* q;                   /* [n][width], aligned to 16 bytes                                 */
+  float* scale;                /* [n]                                                             */
+} maaso_rows_quantize_args;
+int maaso_rows_quantize(maaso_instance* inst, const maaso_rows_quantize_args* a, void* hip_stream);
+
+/* Product of rows with weights, row c of w holding what channel c multiplies:
+ *   y[t][c] = a_scale[t] * w_scale[c] * sum_i a[t][i] w[c][i] + bias[c]
+ * and, where `gated` is not 0, w has 2 * n_out rows and out[t][c] = silu(y[t][c]) * y[t][n_out + c], else out = y.
+ * Sums of 8-bit integers are exact, those of 16-bit types binary32.  What lies between a row's n_in elements and the next
+ * row has no part in it, whatever it holds.  No rows may be 0: nothing is done then. */
+typedef struct {
+  uint32_t type;     /* of a and w: INT8, or, of experts, BF16 or FP16                              */
+  uint32_t out_type; /* FP32 or, of INT8, BF16 or FP16, of these the same                           */
+  uint32_t n_a;      /* rows of a                                                                   */
+  uint32_t n_in;     /* 1 .. MAASO_PRODUCT_MAX_IN                                                   */
+  uint32_t n_out, gated;
+  uint64_t a_stride, w_stride; /* elements between rows; multiples of 16 bytes, as the pointers are */
+  uint64_t out_stride;         /* any                                                               */
+  const void* a;
+  const void* w;
+  const float* a_scale; /* [n_a], INT8 only, NULL for 1                                             */
+  const float* w_scale; /* [n_out], gated [2 * n_out]; INT8 only, NULL for 1                        */
+  const float* bias;    /* [n_out], gated [2 * n_out]; NULL for 0                                   */
+  void* out;            /* aligned to an element                                                    */
+} maaso_product;
+
+/* Every row of a (type INT8): out [n_a][n_out].  Errors: INVALID_ARG, SHAPE, BUSY, HIP. */
+int maaso_scaled_product(maaso_instance* inst, const maaso_product* p, void* hip_stream);
+
+/* The experts that each token goes to, and the order of the tokens by expert.  Of token t
+ *   softmax:  p[e] = exp(x[e]) / sum exp(x),     the score that experts are chosen by is x[e]
+ *   sigmoid:  p[e] = 1 / (1 + exp(-x[e])),       the score is x[e], or with a bias p[e] + bias[e] in 64 bits
+ * The k largest scores are chosen, the lowest expert of equals first: expert[t][j], and weight[t][j] =
+ * scale * p[expert[t][j]], divided by the sum of the chosen p where `renorm` is not 0 (0 where that sum is 0).  An expert
+ * whose logit or score is NaN or -infinity is not chosen and has p = 0 (a logit of +infinity is the largest finite one); where fewer than k are left,
+ * the rest of the row has expert = -1, weight = 0.
+ * token holds the tokens of expert 0 in ascending order, then those of expert 1, ...: expert e's are
+ * token[start[e]] .. token[start[e + 1] - 1], and place[t][j] is where choice j of token t stands (-1 where
+ * there is none).  token is -1 behind start[n_experts].  All DEVICE.
+ * Errors: INVALID_ARG, SHAPE, WORKSPACE, BUSY, HIP. */
+typedef struct {
+  uint32_t type;             /* of the logits: BF16, FP16 or FP32                          */
+  uint32_t n, n_experts, k;  /* k <= n_experts, MAASO_EXPERT_MAX_CHOSEN                    */
+  uint32_t sigmoid, renorm;
+  float scale;
+  uint64_t stride;           /* elements between the tokens' logits                        */
+  const void* logits;        /* [n][n_experts]                                             */
+  const float* bias;         /* [n_experts] or NULL; sigmoid only                          */
+  int32_t* expert;           /* [n][k]                                                     */
+  float* weight;             /* [n][k]                                                     */
+  int32_t* start;            /* [n_experts + 1]; these three or none of them               */
+  int32_t* token;            /* [n * k]                                                    */
+  int32_t* place;            /* [n * k]                                                    */
+} maaso_expert_route_args;
+int maaso_expert_route(maaso_instance* inst, const maaso_expert_route_args* a, void* hip_stream);
+
+/* The product of each expert's rows with its weights: row r of out, start[e] <= r < start[e + 1], is row token[r] of a
+ * (token NULL: row r) with w + e * expert_stride, w_scale + e * channels and bias + e * channels, channels being
+ * n_out, or 2 * n_out where gated.  Rows of out before start[0] or from start[n_experts] on are left as they are.
+ * A start below 0, past n_rows or below an earlier one is taken as the nearest that is not, and raises
+ * MAASO_INST_BAD_BOUND; a row whose token is outside a is left as it is, and raises MAASO_INST_BAD_ROW.
+ * Errors: INVALID_ARG, SHAPE, BUSY, HIP. */
+typedef struct {
+  maaso_product product;
+  uint32_t n_rows;        /* rows of out                                             */
+  uint32_t n_experts;     /* at most MAASO_EXPERT_MAX                                */
+  uint64_t expert_stride; /* elements between experts' weights, a multiple of 16 bytes */
+  const int32_t* start;   /* [n_experts + 1], DEVICE as all                          */
+  const int32_t* token;   /* [n_rows] or NULL                                        */
+} maaso_expert_product_args;
+int maaso_expert_product(maaso_instance* inst, const maaso_expert_product_args* a, void* hip_stream);
+
+/* The experts' outputs back to their tokens:
+ *   out[t] = residual[t] + sum_j weight[t][j] * y[place[t][j]]
+ * A negative place adds nothing, whatever its weight; one outside y neither, and raises MAASO_INST_BAD_ROW.  All DEVICE.
+ * Errors: INVALID_ARG, SHAPE, BUSY, HIP. */
+typedef struct {
+  uint32_t type;                                /* of y, residual and out: BF16, FP16 or FP32             */
+  uint32_t n, k, width;                         /* k <= MAASO_EXPERT_MAX_CHOSEN                           */
+  uint32_t n_rows;                              /* of y                                                   */
+  uint64_t y_stride, residual_stride, out_stride; /* elements                                             */
+  const void* y;                                /* [n_rows][width]                                        */
+  const void* residual;                         /* [n][width] or NULL                                     */
+  void* out;                                    /* [n][width]; may be residual, with the same stride      */
+  const int32_t* place;                         /* [n][k]                                                 */
+  const float* weight;                          /* [n][k] or NULL for 1                                   */
+} maaso_expert_combine_args;
+int maaso_expert_combine(maaso_instance* inst, const maaso_expert_combine_args* a, void* hip_stream);
 
 #ifdef __cplusplus
 }

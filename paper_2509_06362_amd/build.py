@@ -6,6 +6,8 @@ import os
 import subprocess
 import sys
 import sysconfig
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 from pathlib import Path
 
 PKG = Path(__file__).resolve().parent
@@ -15,7 +17,7 @@ LIB = PKG / "libmaaso.so"
 MARSHAL = PKG / "_marshal.so"
 
 HIPCC_FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     # one IEEE operation per source operation: no contraction, correctly rounded division
     "-ffp-contract=off", "-fhip-fp32-correctly-rounded-divide-sqrt",
     # packed fp32 instructions stay off
@@ -51,20 +53,30 @@ def build_marshal(verbose: bool = False) -> Path:
 
 
 def build_library(verbose: bool = False) -> Path:
+    """Every source compiled, side by side, and linked."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    tmp = LIB.with_suffix(f".so.tmp{os.getpid()}")
-    cmd = [hipcc, *HIPCC_FLAGS, f"-I{ROOT / 'include'}", *map(str, sources()), "-o", str(tmp)]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    res = subprocess.run(cmd, capture_output=True, text=True)
     noise = "is not a recognized feature for this target"
-    err = "\n".join(l for l in res.stderr.splitlines() if noise not in l)
-    if res.returncode != 0:
-        tmp.unlink(missing_ok=True)
-        raise RuntimeError(f"hipcc failed ({res.returncode}):\n{err}")
-    if verbose and err.strip():
-        print(err, file=sys.stderr)
-    os.replace(tmp, LIB)
+
+    def run(cmd):
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        res = subprocess.run(cmd, capture_output=True, text=True)
+        err = "\n".join(l for l in res.stderr.splitlines() if noise not in l)
+        if res.returncode != 0:
+            raise RuntimeError(f"hipcc failed ({res.returncode}):\n{err}")
+        if verbose and err.strip():
+            print(err, file=sys.stderr)
+
+    with tempfile.TemporaryDirectory(prefix="maaso_build") as tmp:
+        objects = [str(Path(tmp) / f"{s.stem}.o") for s in sources()]
+        with ThreadPoolExecutor(len(objects)) as pool:
+            list(pool.map(run, [[hipcc, *HIPCC_FLAGS, f"-I{ROOT / 'include'}", "-c", str(s), "-o", o] for s, o in zip(sources(), objects)]))
+        linked = LIB.with_suffix(f".so.tmp{os.getpid()}")
+        try:
+            run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", *objects, "-o", str(linked)])
+            os.replace(linked, LIB)
+        finally:
+            linked.unlink(missing_ok=True)
     build_marshal(verbose)
     return LIB
 

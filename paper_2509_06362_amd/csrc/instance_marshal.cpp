@@ -22,6 +22,11 @@ decltype(&maaso_kv_copy) call_copy;
 decltype(&maaso_kv_append) call_append;
 decltype(&maaso_kv_attention) call_attention;
 decltype(&maaso_logits_adjust) call_logits;
+decltype(&maaso_rows_quantize) call_quantize;
+decltype(&maaso_scaled_product) call_product;
+decltype(&maaso_expert_route) call_route;
+decltype(&maaso_expert_product) call_experts;
+decltype(&maaso_expert_combine) call_combine;
 
 struct Refused {};  // the Python error is set
 
@@ -70,6 +75,7 @@ uint32_t type_of(const at::Tensor& t) {
     case Type::Half: return MAASO_FP16;
     case Type::Float: return MAASO_FP32;
     case Type::Float8_e4m3fn: return MAASO_E4M3;
+    case Type::Char: return MAASO_INT8;
     default: refuse(std::string(c10::toString(t.scalar_type())) + " is none of the library's types");
   }
 }
@@ -97,6 +103,23 @@ void* heads(PyObject* o, Type type, int64_t n_tok, int64_t n_heads, int64_t dim,
   if (t.stride(2) != 1 || (n_heads > 1 && t.stride(1) != dim)) refuse("a token's heads must lie side by side");
   stride = (uint64_t)t.stride(0);
   return t.data_ptr();
+}
+
+// [rows, width], a row's elements side by side; the elements between rows go to `stride`.
+void* rows_of(PyObject* o, Type type, int64_t n, int64_t width, uint64_t& stride) {
+  const at::Tensor& t = tensor(o);
+  if (!t.is_cuda() || t.scalar_type() != type)
+    refuse(std::string("expected a GPU tensor of ") + c10::toString(type) + ", got " + c10::toString(t.scalar_type()) + " on " + t.device().str());
+  if (t.dim() != 2 || t.size(0) != n || t.size(1) != width)
+    refuse("expected [" + std::to_string(n) + ", " + std::to_string(width) + "]");
+  if (t.stride(1) != 1 && width > 1) refuse("a row's elements must lie side by side");
+  stride = (uint64_t)t.stride(0);
+  return t.data_ptr();
+}
+const at::Tensor& matrix(PyObject* o, int64_t dims, const char* what) {
+  const at::Tensor& t = tensor(o);
+  if (t.dim() != dims) refuse(std::string("expected ") + what);
+  return t;
 }
 
 void* stream(PyObject* o) {
@@ -312,9 +335,135 @@ PyObject* logits(PyObject*, Args a, Py_ssize_t n) {
   });
 }
 
+// (inst, x, q, scale, weight, norm, gated, eps, stream)
+PyObject* quantize(PyObject*, Args a, Py_ssize_t n) {
+  return entry(n, 9, [=] {
+    maaso_instance* inst = instance_of(a[0]);
+    const at::Tensor &x = matrix(a[1], 2, "x as [rows, width]"), &q = matrix(a[2], 2, "q as [rows, width]");
+    maaso_rows_quantize_args p{};
+    const bool norm = truth(a[5]), gated = truth(a[6]);
+    if (norm && gated) refuse("rows are either normed or gated");
+    const int64_t rows = x.size(0), width = q.size(1);
+    p.type = type_of(x);
+    p.form = norm ? MAASO_ROWS_NORM : gated ? MAASO_ROWS_GATED : MAASO_ROWS_PLAIN;
+    p.n = whole32(rows);
+    p.width = whole32(width);
+    p.eps = real(a[7]);
+    p.x = rows_of(a[1], x.scalar_type(), rows, gated ? 2 * width : width, p.x_stride);
+    p.q = static_cast<int8_t*>(rows_of(a[2], Type::Char, rows, width, p.q_stride));
+    p.scale = floats(a[3], rows);
+    p.weight = buffer(a[4], x.scalar_type(), width);
+    void* s = stream(a[8]);
+    return [=] { return call_quantize(inst, &p, s); };
+  });
+}
+
+// What both products have in common: a [rows, in], out [out rows, channels]; w's last two dimensions are looked at by the caller.
+maaso_product product_of(PyObject* a, PyObject* a_scale, const at::Tensor& w, PyObject* w_scale, PyObject* out, PyObject* bias, PyObject* gated, int64_t experts) {
+  maaso_product p{};
+  const at::Tensor &x = matrix(a, 2, "a as [rows, in]"), &y = matrix(out, 2, "out as [rows, channels]");
+  const int64_t rows = x.size(0), in = x.size(1), channels = w.size(-2);
+  p.type = type_of(x);
+  p.out_type = type_of(y);
+  p.gated = truth(gated) ? 1u : 0u;
+  if (!w.is_cuda() || w.scalar_type() != x.scalar_type()) refuse("w must be a GPU tensor of a's type");
+  if (w.size(-1) != in || channels != y.size(1) * (p.gated ? 2 : 1)) refuse("w must have a row of a's width for each channel, twice as many where gated");
+  if (w.stride(-1) != 1 && in > 1) refuse("a row's elements must lie side by side");
+  p.n_a = whole32(rows);
+  p.n_in = whole32(in);
+  p.n_out = whole32(y.size(1));
+  p.a = rows_of(a, x.scalar_type(), rows, in, p.a_stride);
+  p.out = rows_of(out, y.scalar_type(), y.size(0), y.size(1), p.out_stride);
+  p.w = w.data_ptr();
+  p.w_stride = (uint64_t)w.stride(-2);
+  p.a_scale = floats(a_scale, rows);
+  p.w_scale = floats(w_scale, experts * channels);
+  p.bias = floats(bias, experts * channels);
+  return p;
+}
+
+// (inst, a, a_scale, w, w_scale, out, bias, gated, stream)
+PyObject* scaled_product(PyObject*, Args a, Py_ssize_t n) {
+  return entry(n, 9, [=] {
+    maaso_instance* inst = instance_of(a[0]);
+    const at::Tensor& w = matrix(a[3], 2, "w as [channels, in]");
+    const maaso_product p = product_of(a[1], a[2], w, a[4], a[5], a[6], a[7], 1);
+    if (tensor(a[5]).size(0) != tensor(a[1]).size(0)) refuse("out must have a's rows");
+    void* s = stream(a[8]);
+    return [=] { return call_product(inst, &p, s); };
+  });
+}
+
+// (inst, a, a_scale, w, w_scale, out, start, token, bias, gated, stream)
+PyObject* expert_product(PyObject*, Args a, Py_ssize_t n) {
+  return entry(n, 11, [=] {
+    maaso_instance* inst = instance_of(a[0]);
+    const at::Tensor& w = matrix(a[3], 3, "w as [experts, channels, in]");
+    maaso_expert_product_args p{};
+    p.product = product_of(a[1], a[2], w, a[4], a[5], a[8], a[9], w.size(0));
+    p.n_rows = whole32(tensor(a[5]).size(0));
+    p.n_experts = whole32(w.size(0));
+    p.expert_stride = (uint64_t)w.stride(0);
+    p.start = ints(a[6], w.size(0) + 1);
+    p.token = ints(a[7], p.n_rows);
+    void* s = stream(a[10]);
+    return [=] { return call_experts(inst, &p, s); };
+  });
+}
+
+// (inst, logits, bias, expert, weight, start, token, place, sigmoid, renorm, scale, stream)
+PyObject* route(PyObject*, Args a, Py_ssize_t n) {
+  return entry(n, 12, [=] {
+    maaso_instance* inst = instance_of(a[0]);
+    const at::Tensor &x = matrix(a[1], 2, "logits as [tokens, experts]"), &e = matrix(a[3], 2, "expert as [tokens, chosen]");
+    maaso_expert_route_args p{};
+    const int64_t tokens = x.size(0), k = e.size(1);
+    if (e.size(0) != tokens) refuse("expert must have a row for each token");
+    p.type = type_of(x);
+    p.n = whole32(tokens);
+    p.n_experts = whole32(x.size(1));
+    p.k = whole32(k);
+    p.logits = rows_of(a[1], x.scalar_type(), tokens, x.size(1), p.stride);
+    p.bias = floats(a[2], p.n_experts);
+    p.expert = ints(a[3]);
+    p.weight = floats(a[4], tokens * k);
+    p.start = ints(a[5], x.size(1) + 1);
+    p.token = ints(a[6], tokens * k);
+    p.place = ints(a[7], tokens * k);
+    p.sigmoid = truth(a[8]) ? 1u : 0u;
+    p.renorm = truth(a[9]) ? 1u : 0u;
+    p.scale = real(a[10]);
+    void* s = stream(a[11]);
+    return [=] { return call_route(inst, &p, s); };
+  });
+}
+
+// (inst, y, place, weight, out, residual, stream)
+PyObject* combine(PyObject*, Args a, Py_ssize_t n) {
+  return entry(n, 7, [=] {
+    maaso_instance* inst = instance_of(a[0]);
+    const at::Tensor &y = matrix(a[1], 2, "y as [rows, width]"), &place = matrix(a[2], 2, "place as [tokens, chosen]");
+    maaso_expert_combine_args p{};
+    const Type type = y.scalar_type();
+    const int64_t tokens = place.size(0), width = y.size(1);
+    p.type = type_of(y);
+    p.n = whole32(tokens);
+    p.k = whole32(place.size(1));
+    p.width = whole32(width);
+    p.n_rows = whole32(y.size(0));
+    p.y = rows_of(a[1], type, y.size(0), width, p.y_stride);
+    p.out = rows_of(a[4], type, tokens, width, p.out_stride);
+    if (a[5] != Py_None) p.residual = rows_of(a[5], type, tokens, width, p.residual_stride);
+    p.place = ints(a[2]);
+    p.weight = floats(a[3], tokens * place.size(1));
+    void* s = stream(a[6]);
+    return [=] { return call_combine(inst, &p, s); };
+  });
+}
+
 // The library's entry points, as addresses, in the order of the declarations above.
 PyObject* bind(PyObject*, Args a, Py_ssize_t n) {
-  return entry(n, 8, [=] {
+  return entry(n, 13, [=] {
     auto at = [&](int k) { return (uintptr_t)whole(a[k]); };
     call_extend = reinterpret_cast<decltype(call_extend)>(at(0));
     call_fork = reinterpret_cast<decltype(call_fork)>(at(1));
@@ -324,6 +473,11 @@ PyObject* bind(PyObject*, Args a, Py_ssize_t n) {
     call_append = reinterpret_cast<decltype(call_append)>(at(5));
     call_attention = reinterpret_cast<decltype(call_attention)>(at(6));
     call_logits = reinterpret_cast<decltype(call_logits)>(at(7));
+    call_quantize = reinterpret_cast<decltype(call_quantize)>(at(8));
+    call_product = reinterpret_cast<decltype(call_product)>(at(9));
+    call_route = reinterpret_cast<decltype(call_route)>(at(10));
+    call_experts = reinterpret_cast<decltype(call_experts)>(at(11));
+    call_combine = reinterpret_cast<decltype(call_combine)>(at(12));
     return [] { return 0; };
   });
 }
@@ -335,7 +489,9 @@ PyMethodDef method(const char* name) {
 
 PyMethodDef methods[] = {method<bind>("bind"), method<extend>("extend"), method<fork_rows>("fork"), method<trim>("trim"),
                          method<compact>("compact"), method<copy_pages>("copy"), method<append>("append"),
-                         method<attention>("attention"), method<logits>("logits"), {nullptr, nullptr, 0, nullptr}};
+                         method<attention>("attention"), method<logits>("logits"), method<quantize>("quantize"),
+                         method<scaled_product>("scaled_product"), method<expert_product>("expert_product"), method<route>("route"),
+                         method<combine>("combine"), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,238 @@
+// Host side of the products, the experts and the rows in 8 bits (include/maaso_instance.h): argument validation, launch shapes.
+#include "../../include/maaso_instance.h"
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "instance_host.hpp"
+#include "product_kernels.hpp"
+#include "route_kernels.hpp"
+#include "rows_kernels.hpp"
+
+using namespace maaso;
+
+namespace {
+
+bool whole16(uint64_t elements, uint64_t size) { return elements % (16u / size) == 0; }
+
+template <typename T, int Form>
+void launch_quantize_form(const QuantizeArgs& a, hipStream_t s) {
+  if (a.width <= 2048u && a.n >= 1024u)
+    hipLaunchKernelGGL((quantize_kernel<T, Form, 64, 4>), dim3((a.n + 3u) / 4u), dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL((quantize_kernel<T, Form, 256, 4>), dim3(a.n), dim3(256), 0, s, a);
+}
+
+template <typename T>
+void launch_quantize(uint32_t form, const QuantizeArgs& a, hipStream_t s) {
+  if (form == MAASO_ROWS_PLAIN) launch_quantize_form<T, MAASO_ROWS_PLAIN>(a, s);
+  else if (form == MAASO_ROWS_NORM) launch_quantize_form<T, MAASO_ROWS_NORM>(a, s);
+  else launch_quantize_form<T, MAASO_ROWS_GATED>(a, s);
+}
+
+// What a product's arguments have to be, of one matrix and of experts alike.
+int check_product(const maaso_product* p) {
+  if (p->type != MAASO_INT8 && p->type != MAASO_BF16 && p->type != MAASO_FP16) return MAASO_E_INVALID_ARG;
+  if (p->out_type > MAASO_FP32 || (p->type != MAASO_INT8 && p->out_type != MAASO_FP32 && p->out_type != p->type)) return MAASO_E_INVALID_ARG;
+  if (p->type != MAASO_INT8 && (p->a_scale || p->w_scale)) return MAASO_E_INVALID_ARG;
+  if (p->n_in == 0 || p->n_in > MAASO_PRODUCT_MAX_IN || p->n_out == 0 || p->n_out > 0x3fffffffu) return MAASO_E_SHAPE;
+  const uint64_t size = element_size(p->type), channels = (uint64_t)p->n_out * (p->gated ? 2u : 1u);
+  if (p->n_a > 1u && (!whole16(p->a_stride, size) || p->a_stride < p->n_in)) return MAASO_E_SHAPE;
+  if (channels > 1u && (!whole16(p->w_stride, size) || p->w_stride < p->n_in)) return MAASO_E_SHAPE;
+  if (!aligned(p->a, 16) || !aligned(p->w, 16) || !aligned(p->out, element_size(p->out_type))) return MAASO_E_SHAPE;
+  return MAASO_OK;
+}
+
+ProductArgs product_args(const maaso_instance* inst, const maaso_product* p, uint32_t n_rows) {
+  const uint64_t size = element_size(p->type), out_size = element_size(p->out_type);
+  ProductArgs a{};
+  a.a = static_cast<const char*>(p->a); a.w = static_cast<const char*>(p->w); a.out = p->out;
+  a.a_scale = p->a_scale; a.w_scale = p->w_scale; a.bias = p->bias;
+  a.a_stride = p->a_stride * size; a.w_stride = p->w_stride * size; a.out_stride = p->out_stride;
+  a.n_a = p->n_a; a.n_rows = n_rows; a.n_experts = 1u;
+  a.in_bytes = p->n_in * (uint32_t)size; a.n_out = p->n_out; a.channels = p->n_out * (p->gated ? 2u : 1u);
+  a.out_type = p->out_type;
+  a.wide = aligned(p->out, 16) && (n_rows <= 1u || p->out_stride * out_size % 16u == 0u);
+  a.status = inst->status;
+  return a;
+}
+
+// Row tiles of `rows` rows that there can be.
+uint64_t most_tiles(const ProductArgs& a, uint32_t rows) {
+  return a.start ? a.n_rows / rows + std::min(a.n_experts, a.n_rows) : (a.n_rows + rows - 1u) / rows;
+}
+
+template <typename T, int MT, int NT, bool Gated>
+int launch_stream(ProductArgs& a, hipStream_t s) {
+  const uint32_t cols = 16u * (Gated ? NT / 2 : NT);
+  const uint64_t down = most_tiles(a, 16u * MT);
+  if (down > 65535u) return MAASO_E_SHAPE;
+  hipLaunchKernelGGL((product_stream_kernel<T, MT, NT, Gated, 4>), dim3((a.n_out + cols - 1u) / cols, (uint32_t)down), dim3(256), 0, s, a);
+  return launched();
+}
+
+template <typename T, int WM, int WN, int MI, int NI, bool Gated>
+int launch_tiles(ProductArgs& a, hipStream_t s) {
+  const uint32_t cols = WN * NI * 16u / (Gated ? 2u : 1u);
+  a.col_tiles = (a.n_out + cols - 1u) / cols;
+  const uint64_t blocks = (most_tiles(a, WM * MI * 16u) * a.col_tiles + 7u) / 8u * 8u;
+  if (blocks > 0x7fffffffull) return MAASO_E_SHAPE;
+  hipLaunchKernelGGL((product_tile_kernel<T, WM, WN, MI, NI, Gated>), dim3((uint32_t)blocks), dim3(64 * WM * WN), 0, s, a);
+  return launched();
+}
+
+template <typename T, bool Gated>
+int launch_product(ProductArgs& a, uint32_t n_cu, hipStream_t s) {
+  const uint64_t rows = (a.n_rows + a.n_experts - 1u) / a.n_experts;  // of an expert, on the average
+  if (rows <= 16u) return launch_stream<T, 1, 2, Gated>(a, s);
+  if (rows <= 64u) return launch_stream<T, 2, 2, Gated>(a, s);
+  const uint64_t large = most_tiles(a, 256u) * ((a.channels + 255u) / 256u);
+  if (large >= n_cu) return launch_tiles<T, 2, 4, 8, 4, Gated>(a, s);
+  return launch_tiles<T, 2, 2, 4, 4, Gated>(a, s);
+}
+
+template <typename T>
+int launch_product(ProductArgs& a, bool gated, uint32_t n_cu, hipStream_t s) {
+  return gated ? launch_product<T, true>(a, n_cu, s) : launch_product<T, false>(a, n_cu, s);
+}
+
+int launch_product(uint32_t type, ProductArgs& a, bool gated, uint32_t n_cu, hipStream_t s) {
+  if (type == MAASO_INT8) return launch_product<Int8>(a, gated, n_cu, s);
+  if (type == MAASO_BF16) return launch_product<__bf16>(a, gated, n_cu, s);
+  return launch_product<_Float16>(a, gated, n_cu, s);
+}
+
+template <typename T, int Per>
+void launch_choose(const RouteArgs& a, hipStream_t s) {
+  const dim3 g((a.n + 3u) / 4u);
+  if (a.bias) hipLaunchKernelGGL((route_choose_kernel<T, Per, true>), g, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((route_choose_kernel<T, Per, false>), g, dim3(256), 0, s, a);
+}
+
+template <typename T>
+void launch_choose(const RouteArgs& a, hipStream_t s) {
+  if (a.n_experts <= 64u) launch_choose<T, 1>(a, s);
+  else if (a.n_experts <= 128u) launch_choose<T, 2>(a, s);
+  else if (a.n_experts <= 256u) launch_choose<T, 4>(a, s);
+  else if (a.n_experts <= 512u) launch_choose<T, 8>(a, s);
+  else launch_choose<T, 16>(a, s);
+}
+
+}  // namespace
+
+extern "C" {
+
+int maaso_rows_quantize(maaso_instance* inst, const maaso_rows_quantize_args* p, void* hip_stream) {
+  if (!inst || !p) return MAASO_E_INVALID_ARG;
+  if (p->type > MAASO_FP32 || p->form > MAASO_ROWS_GATED || (p->weight && p->form != MAASO_ROWS_NORM)) return MAASO_E_INVALID_ARG;
+  if (p->width == 0 || p->width > 0x3fffffffu) return MAASO_E_SHAPE;
+  if (p->n == 0) return MAASO_OK;
+  if (p->n > 0x7fffffffu) return MAASO_E_SHAPE;
+  if (!p->x || !p->q || !p->scale) return MAASO_E_INVALID_ARG;
+  if (p->form == MAASO_ROWS_NORM && (!(p->eps >= 0.0f) || !std::isfinite(p->eps))) return MAASO_E_INVALID_ARG;
+  const uint64_t size = element_size(p->type), elements = (uint64_t)p->width * (p->form == MAASO_ROWS_GATED ? 2u : 1u);
+  if (!aligned(p->x, size) || !aligned(p->q, 16) || !aligned(p->weight, size)) return MAASO_E_SHAPE;
+  if (p->n > 1u && (p->q_stride % 16u || p->x_stride < elements || p->q_stride < p->width)) return MAASO_E_SHAPE;
+  const QuantizeArgs a{p->x, p->weight, p->q, p->scale, p->x_stride, p->q_stride, p->n, p->width, p->eps};
+  const hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  InstanceCall call(inst, s);
+  if (call.rc != MAASO_OK) return call.rc;
+  if (p->type == MAASO_BF16) launch_quantize<__bf16>(p->form, a, s);
+  else if (p->type == MAASO_FP16) launch_quantize<_Float16>(p->form, a, s);
+  else launch_quantize<float>(p->form, a, s);
+  return launched();
+}
+
+int maaso_scaled_product(maaso_instance* inst, const maaso_product* p, void* hip_stream) {
+  if (!inst || !p) return MAASO_E_INVALID_ARG;
+  if (p->type != MAASO_INT8) return MAASO_E_INVALID_ARG;
+  if (const int rc = check_product(p)) return rc;
+  if (p->n_a == 0) return MAASO_OK;
+  if (!p->a || !p->w || !p->out) return MAASO_E_INVALID_ARG;
+  if (p->n_a > 0x7fffffffu || (p->n_a > 1u && p->out_stride < p->n_out)) return MAASO_E_SHAPE;
+  ProductArgs a = product_args(inst, p, p->n_a);
+  const hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  InstanceCall call(inst, s);
+  if (call.rc != MAASO_OK) return call.rc;
+  return launch_product(p->type, a, p->gated != 0u, (uint32_t)inst->n_cu, s);
+}
+
+int maaso_expert_product(maaso_instance* inst, const maaso_expert_product_args* p, void* hip_stream) {
+  if (!inst || !p) return MAASO_E_INVALID_ARG;
+  if (const int rc = check_product(&p->product)) return rc;
+  if (p->n_experts == 0 || p->n_experts > MAASO_EXPERT_MAX) return MAASO_E_SHAPE;
+  if (p->n_rows == 0) return MAASO_OK;
+  if (!p->product.a || !p->product.w || !p->product.out || !p->start || p->product.n_a == 0) return MAASO_E_INVALID_ARG;
+  if (p->n_rows > 0x7fffffffu || p->product.n_a > 0x7fffffffu || (p->n_rows > 1u && p->product.out_stride < p->product.n_out)) return MAASO_E_SHAPE;
+  const uint64_t size = element_size(p->product.type), channels = (uint64_t)p->product.n_out * (p->product.gated ? 2u : 1u);
+  if (p->n_experts > 1u && (!whole16(p->expert_stride, size) || p->expert_stride < (channels - 1u) * p->product.w_stride + p->product.n_in)) return MAASO_E_SHAPE;
+  ProductArgs a = product_args(inst, &p->product, p->n_rows);
+  a.start = p->start; a.token = p->token; a.n_experts = p->n_experts; a.expert_stride = p->expert_stride * size;
+  const hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  InstanceCall call(inst, s);
+  if (call.rc != MAASO_OK) return call.rc;
+  return launch_product(p->product.type, a, p->product.gated != 0u, (uint32_t)inst->n_cu, s);
+}
+
+int maaso_expert_route(maaso_instance* inst, const maaso_expert_route_args* p, void* hip_stream) {
+  if (!inst || !p) return MAASO_E_INVALID_ARG;
+  if (p->type > MAASO_FP32 || (p->bias && !p->sigmoid) || !std::isfinite(p->scale)) return MAASO_E_INVALID_ARG;
+  if (p->n_experts == 0 || p->n_experts > MAASO_EXPERT_MAX || p->k == 0 || p->k > p->n_experts || p->k > MAASO_EXPERT_MAX_CHOSEN) return MAASO_E_SHAPE;
+  const bool order = p->start || p->token || p->place;
+  if (order && !(p->start && p->token && p->place) && p->n) return MAASO_E_INVALID_ARG;
+  if (p->n && (!p->logits || !p->expert || !p->weight)) return MAASO_E_INVALID_ARG;
+  if ((uint64_t)p->n * p->k > 0x7fffffffull || (p->n > 1u && p->stride < p->n_experts)) return MAASO_E_SHAPE;
+  if (p->n == 0 && !p->start) return MAASO_OK;
+  RouteArgs a{p->logits, p->bias, p->expert, p->weight, p->start, p->token, p->place, p->stride, p->n, p->n_experts, p->k,
+              p->sigmoid != 0u, p->renorm != 0u, p->scale, (p->n + kChunk - 1u) / kChunk, nullptr};
+  const hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  InstanceCall call(inst, s);
+  if (call.rc != MAASO_OK) return call.rc;
+  if (order && a.n > kOneBlock) {
+    Carve ws{inst->ws, inst->ws_bytes};
+    a.counts = ws.take<uint32_t>((size_t)a.chunks * a.n_experts);
+    if (!ws.fits) return MAASO_E_WORKSPACE;
+  }
+  if (a.n) {
+    if (p->type == MAASO_BF16) launch_choose<__bf16>(a, s);
+    else if (p->type == MAASO_FP16) launch_choose<_Float16>(a, s);
+    else launch_choose<float>(a, s);
+  }
+  if (!order) return launched();
+  if (a.n <= kOneBlock) {
+    const uint32_t words = (a.n + 31u) / 32u;
+    hipLaunchKernelGGL(route_order_kernel, dim3(1), dim3(1024), a.n_experts * (words + 1u) * 4u, s, a);
+    return launched();
+  }
+  const uint32_t room = a.n_experts * (kChunk / 32u) * 4u;
+  hipLaunchKernelGGL(route_count_kernel, dim3(a.chunks), dim3(256), room, s, a);
+  hipLaunchKernelGGL(route_starts_kernel, dim3(1), dim3(1024), 0, s, a);
+  hipLaunchKernelGGL(route_place_kernel, dim3(a.chunks), dim3(256), room, s, a);
+  return launched();
+}
+
+int maaso_expert_combine(maaso_instance* inst, const maaso_expert_combine_args* p, void* hip_stream) {
+  if (!inst || !p) return MAASO_E_INVALID_ARG;
+  if (p->type > MAASO_FP32) return MAASO_E_INVALID_ARG;
+  if (p->width == 0 || p->width > 0x3fffffffu || p->k == 0 || p->k > MAASO_EXPERT_MAX_CHOSEN) return MAASO_E_SHAPE;
+  if (p->n == 0) return MAASO_OK;
+  if (!p->out || !p->place || (!p->y && p->n_rows)) return MAASO_E_INVALID_ARG;
+  const uint64_t size = element_size(p->type), blocks = ((uint64_t)p->n * ((p->width + 7u) / 8u) + 255u) / 256u;
+  if (p->n > 0x7fffffffu || p->n_rows > 0x7fffffffu || blocks > 0x7fffffffull) return MAASO_E_SHAPE;
+  if (!aligned(p->y, size) || !aligned(p->residual, size) || !aligned(p->out, size)) return MAASO_E_SHAPE;
+  auto rows_ok = [&](uint32_t rows, uint64_t stride) { return rows <= 1u || stride >= p->width; };
+  if (!rows_ok(p->n_rows, p->y_stride) || !rows_ok(p->n, p->out_stride) || (p->residual && !rows_ok(p->n, p->residual_stride))) return MAASO_E_SHAPE;
+  if (p->residual == p->out && p->n > 1u && p->residual_stride != p->out_stride) return MAASO_E_INVALID_ARG;
+  const CombineArgs a{p->y, p->residual, p->out, p->place, p->weight, p->y_stride, p->residual_stride, p->out_stride, p->n, p->k, p->width, p->n_rows, inst->status};
+  const hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  InstanceCall call(inst, s);
+  if (call.rc != MAASO_OK) return call.rc;
+  if (p->type == MAASO_BF16) hipLaunchKernelGGL(combine_kernel<__bf16>, dim3((uint32_t)blocks), dim3(256), 0, s, a);
+  else if (p->type == MAASO_FP16) hipLaunchKernelGGL(combine_kernel<_Float16>, dim3((uint32_t)blocks), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL(combine_kernel<float>, dim3((uint32_t)blocks), dim3(256), 0, s, a);
+  return launched();
+}
+
+}  // extern "C"

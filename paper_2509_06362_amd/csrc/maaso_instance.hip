@@ -4,11 +4,10 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <atomic>
 #include <cmath>
 #include <new>
 
-#include "host_common.hpp"
+#include "instance_host.hpp"
 #include "kv_append_kernels.hpp"
 #include "kv_attention_kernels.hpp"
 #include "kv_pages_kernels.hpp"
@@ -16,56 +15,7 @@
 
 using namespace maaso;
 
-struct maaso_instance {
-  int device;
-  int n_cu;
-  uint32_t* status;  // device status word, and behind it the one that maaso_instance_status reads
-  LogitsRow* rows;   // [kFewRows] behind it, zeros between calls (made so again by maaso_instance_status)
-  char* ws;          // device workspace
-  size_t ws_bytes;
-  // one call at a time, as for maaso_ctx
-  std::atomic<int> in_call;
-  hipEvent_t order_ev;
-  hipStream_t last_stream;
-  bool has_last;
-};
-
 namespace {
-
-// Exclusive use by one call, and order behind the previous call's stream (calls that are captured are left to the caller, and
-// so is the order behind a stream that is being captured by now: an event recorded there would be a node of its graph, and the
-// wait for it would draw this call's stream into the capture).
-struct InstanceCall {
-  maaso_instance* inst;
-  DeviceGuard device;
-  int rc;
-  InstanceCall(maaso_instance* in, hipStream_t s) : inst(in), device(in->device), rc(MAASO_OK) {
-    int idle = 0;
-    if (!inst->in_call.compare_exchange_strong(idle, 1, std::memory_order_acquire)) {
-      inst = nullptr;
-      rc = MAASO_E_BUSY;
-      return;
-    }
-    if (!device.ok) { rc = MAASO_E_HIP; return; }
-    if (inst->has_last && inst->last_stream == s) return;
-    if (is_captured(s)) return;
-    if (inst->has_last && !is_captured(inst->last_stream)) {
-      const bool ordered = hipEventRecord(inst->order_ev, inst->last_stream) == hipSuccess &&
-                           hipStreamWaitEvent(s, inst->order_ev, 0) == hipSuccess;
-      if (!ordered) {
-        (void)hipGetLastError();
-        if (!hip_ok(hipDeviceSynchronize())) rc = MAASO_E_HIP;
-      }
-    }
-    inst->last_stream = s;
-    inst->has_last = true;
-  }
-  ~InstanceCall() {
-    if (inst) inst->in_call.store(0, std::memory_order_release);
-  }
-  InstanceCall(const InstanceCall&) = delete;
-  InstanceCall& operator=(const InstanceCall&) = delete;
-};
 
 // Takes the status bits and leaves none, in one step: a copy and a clear of their own would lose what is raised between them.
 // The rows are made zeros, as calls leave them: two few-row calls that have run at once, which the caller has to order, may
@@ -79,23 +29,6 @@ __global__ void __launch_bounds__(256) take_status_kernel(uint32_t* status, Logi
 static_assert(kFewRows % 256u == 0u, "a thread to a row");
 
 constexpr size_t kOwnBytes = 256u + kFewRows * sizeof(LogitsRow);  // the status word, then the rows
-
-int launched() { return hip_ok(hipGetLastError()) ? MAASO_OK : MAASO_E_HIP; }
-
-// Parts of the workspace, 256 bytes apart.
-struct Carve {
-  char* at;
-  size_t left;
-  bool fits = true;
-  template <typename T> T* take(size_t n) {
-    const size_t bytes = (n * sizeof(T) + 255) & ~size_t(255);
-    if (bytes > left) { fits = false; return nullptr; }
-    T* p = reinterpret_cast<T*>(at);
-    at += bytes;
-    left -= bytes;
-    return p;
-  }
-};
 
 // The copy is behind the kernel on the null stream and has come when it returns: nothing is under way then that later calls,
 // on streams that do not wait for the null stream, could run beside.
@@ -113,7 +46,6 @@ int take_status(maaso_instance* in, uint32_t* bits) {
 
 bool page_size_ok(uint32_t s) { return s == 16u || s == 32u || s == 64u || s == 128u; }
 uint32_t log2_of(uint32_t x) { return 31u - (uint32_t)__builtin_clz(x); }
-bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
 int check_pages(const maaso_kv_pages* p) {
   if (!p || !p->refs || !p->table || !p->length) return MAASO_E_INVALID_ARG;
@@ -126,8 +58,6 @@ int check_pages(const maaso_kv_pages* p) {
 PageArgs page_args(const maaso_instance* inst, const maaso_kv_pages* p) {
   return {p->n_pages, log2_of(p->page_size), p->n_rows, p->width, p->refs, p->table, p->length, inst->status};
 }
-
-uint64_t element_size(uint32_t type) { return type == MAASO_E4M3 ? 1u : type == MAASO_FP32 ? 4u : 2u; }
 
 int check_cache(const maaso_kv_cache* c) {
   if (!c || !c->k || !c->v) return MAASO_E_INVALID_ARG;

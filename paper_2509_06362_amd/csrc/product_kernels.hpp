@@ -1,0 +1,453 @@
+// Products of rows with weights whose rows are channels, for one matrix (8-bit integers with scales) or for many, each with
+// its own ragged group of rows (experts), with the gate in the epilogue.
+//
+// Both operands hold what is summed over along a row, so that a lane's 16 bytes of a row are an operand of the matrix units as
+// they are, 8 elements of 16 bits or 16 of 8: every type goes through the same addresses, in bytes.  Which bytes of a row
+// meet in which instruction does not matter as long as both operands agree.  The weights are the instructions' first operand:
+// a lane then ends with four neighbouring channels of one row.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "../../include/maaso_instance.h"
+#include "element_types.hpp"
+#include "gate.hpp"
+
+namespace maaso {
+
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+
+struct Int8 { int8_t bits; };  // the 8-bit integers, as a template's argument
+
+template <typename T> struct Operand;
+template <> struct Operand<__bf16> {
+  using Sum = f32x4;
+  static __device__ inline f32x4 mfma(u32x4 w, u32x4 a, f32x4 c) {
+    return mfma_16x16x32(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, a), c);
+  }
+};
+template <> struct Operand<_Float16> {
+  using Sum = f32x4;
+  static __device__ inline f32x4 mfma(u32x4 w, u32x4 a, f32x4 c) {
+    return mfma_16x16x32(__builtin_bit_cast(f16x8, w), __builtin_bit_cast(f16x8, a), c);
+  }
+};
+template <> struct Operand<Int8> {
+  using Sum = i32x4;
+  static __device__ inline i32x4 mfma(u32x4 w, u32x4 a, i32x4 c) {
+    return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, w), __builtin_bit_cast(i32x4, a), c, 0, 0, 0);
+  }
+};
+
+struct ProductArgs {
+  const char* a;
+  const char* w;
+  void* out;
+  const float* a_scale;
+  const float* w_scale;
+  const float* bias;
+  const int32_t* start;    // NULL: one group of all rows
+  const int32_t* token;
+  uint64_t a_stride, w_stride, expert_stride;  // bytes
+  uint64_t out_stride;                         // elements
+  uint32_t n_a, n_rows, n_experts, in_bytes, n_out, channels;  // channels: rows of an expert's weights
+  uint32_t out_type;
+  uint32_t col_tiles;
+  bool wide;  // rows of out begin at multiples of 16 bytes
+  uint32_t* status;
+};
+
+// The rows of one tile: `rows` rows of out from `begin` on (0: there is no such tile), of this expert.
+struct RowTile {
+  uint32_t expert, begin, rows;
+};
+
+__device__ inline uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
+
+// Inclusive sum / maximum over the lanes below.
+__device__ inline uint32_t lanes_sum(uint32_t v) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const uint32_t o = (uint32_t)__shfl_up((int)v, d);
+    v += (int)(threadIdx.x & 63u) >= d ? o : 0u;
+  }
+  return v;
+}
+__device__ inline uint32_t lanes_max(uint32_t v) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const uint32_t o = (uint32_t)__shfl_up((int)v, d);
+    v = max(v, (int)(threadIdx.x & 63u) >= d ? o : 0u);
+  }
+  return v;
+}
+
+// 64 experts at a time, one to a lane: their rows [lo, hi) and the tiles of `Rows` rows up to and with each of them.
+// A start out of order is taken as the nearest that is not.
+template <uint32_t Rows> struct Groups {
+  uint32_t base = 0, seen = 0, last = 0, lo = 0, hi = 0, upto = 0;
+  bool bad = false;
+  __device__ inline void look(const ProductArgs& a) {
+    const uint32_t e = base + (threadIdx.x & 63u);
+    const bool in = e < a.n_experts;
+    const int32_t s0 = in ? a.start[e] : 0, s1 = in ? a.start[e + 1u] : 0;
+    lo = (uint32_t)min(max(s0, 0), (int32_t)a.n_rows);
+    hi = (uint32_t)min(max(s1, 0), (int32_t)a.n_rows);
+    const bool off = in && (hi < lo || lo != (uint32_t)s0 || hi != (uint32_t)s1 || lo < last);
+    if (__ballot(off)) {
+      bad = true;
+      lo = lanes_max(max(lo, last));
+      hi = lanes_max(max(lo, hi));
+    }
+    last = (uint32_t)__builtin_amdgcn_readlane((int)hi, (int)min(63u, a.n_experts - 1u - base));
+    if (!in) lo = hi = 0u;
+    upto = seen + lanes_sum((hi - lo + Rows - 1u) / Rows);
+    seen = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+  }
+  // The tile among the experts looked at; it is there: `tile` is below `seen`, and was not below what was seen before.
+  __device__ inline RowTile take(uint32_t tile) const {
+    const int l = (int)__builtin_ctzll(__ballot(tile < upto));
+    const uint32_t first = (uint32_t)__builtin_amdgcn_readlane((int)lo, l), end = (uint32_t)__builtin_amdgcn_readlane((int)hi, l);
+    const uint32_t tiles = (end - first + Rows - 1u) / Rows, to = (uint32_t)__builtin_amdgcn_readlane((int)upto, l);
+    const uint32_t begin = first + (tile - (to - tiles)) * Rows;
+    return {base + (uint32_t)l, begin, min(Rows, end - begin)};
+  }
+};
+
+template <uint32_t Rows> __device__ inline RowTile row_tile(const ProductArgs& a, uint32_t tile) {
+  if (!a.start) return {0u, tile * Rows, tile * Rows < a.n_rows ? min(Rows, a.n_rows - tile * Rows) : 0u};
+  Groups<Rows> g;
+  for (; g.base < a.n_experts; g.base += 64u) {
+    g.look(a);
+    if (tile < g.seen) return g.take(tile);
+  }
+  return {0u, 0u, 0u};
+}
+
+// Whoever is first: starts out of order are told once, and by a block that would look at them all the same.
+__device__ inline void check_starts(const ProductArgs& a) {
+  if (!a.start) return;
+  Groups<16u> g;
+  for (; g.base < a.n_experts; g.base += 64u) g.look(a);
+  if (g.bad && (threadIdx.x & 63u) == 0u) atomicOr(a.status, MAASO_INST_BAD_BOUND);
+}
+
+// The row of a that row `r` of out is made of; `ok`: there is one.
+__device__ inline uint32_t source_row(const ProductArgs& a, uint32_t r, bool& ok) {
+  const uint32_t t = a.token ? (uint32_t)a.token[r] : r;
+  ok = t < a.n_a;
+  return ok ? t : 0u;
+}
+
+// The first `left` of 16 bytes, the others zeros.
+__device__ inline u32x4 first_bytes(u32x4 v, int left) {
+#pragma unroll
+  for (int d = 0; d < 4; ++d) {
+    const int keep = left - 4 * d;
+    v[d] = keep >= 4 ? v[d] : keep <= 0 ? 0u : v[d] & ((1u << (8 * keep)) - 1u);
+  }
+  return v;
+}
+
+// 16 bytes from byte `at` of a row on, zeros from the row's end on.  (Rows begin at multiples of 16 bytes: what is read beside
+// a row's last byte lies in the same 16.)
+__device__ inline u32x4 row_bytes(const char* row, uint32_t at, uint32_t in_bytes) {
+  const u32x4 v = *reinterpret_cast<const u32x4*>(row + (at < in_bytes ? at : 0u));
+  return first_bytes(v, (int)in_bytes - (int)at);
+}
+
+// N neighbouring channels of one row: scales, bias, gate, the one rounding.
+template <typename T, int N, bool Gated>
+__device__ inline void finish(const ProductArgs& a, uint32_t expert, uint32_t row, uint32_t source, uint32_t col, float (&y)[N], float (&up)[N]) {
+  const uint64_t at = (uint64_t)expert * a.channels + col;
+  if constexpr (sizeof(T) == 1) {
+    const float s = a.a_scale ? a.a_scale[source] : 1.0f;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      if (col + (uint32_t)k >= a.n_out) break;
+      y[k] = y[k] * s * (a.w_scale ? a.w_scale[at + k] : 1.0f);
+      if constexpr (Gated) up[k] = up[k] * s * (a.w_scale ? a.w_scale[at + a.n_out + k] : 1.0f);
+    }
+  }
+  if (a.bias) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      if (col + (uint32_t)k >= a.n_out) break;
+      y[k] += a.bias[at + k];
+      if constexpr (Gated) up[k] += a.bias[at + a.n_out + k];
+    }
+  }
+  if constexpr (Gated) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) y[k] = silu(y[k]) * up[k];
+  }
+  const uint64_t to = (uint64_t)row * a.out_stride + col;
+  const bool whole = a.wide && col + (uint32_t)N <= a.n_out;
+  if (a.out_type == MAASO_FP32) {
+    float* p = static_cast<float*>(a.out) + to;
+    if (whole) {
+#pragma unroll
+      for (int k = 0; k < N; k += 4) *reinterpret_cast<f32x4*>(p + k) = (f32x4){y[k], y[k + 1], y[k + 2], y[k + 3]};
+    } else {
+#pragma unroll
+      for (int k = 0; k < N; ++k)
+        if (col + (uint32_t)k < a.n_out) p[k] = y[k];
+    }
+    return;
+  }
+  uint32_t pair[N / 2];
+  if (a.out_type == MAASO_BF16) {
+#pragma unroll
+    for (int k = 0; k < N / 2; ++k) pair[k] = __builtin_bit_cast(uint32_t, narrow2<__bf16>(y[2 * k], y[2 * k + 1]));
+  } else {
+#pragma unroll
+    for (int k = 0; k < N / 2; ++k) pair[k] = __builtin_bit_cast(uint32_t, narrow2<_Float16>(y[2 * k], y[2 * k + 1]));
+  }
+  uint16_t* p = static_cast<uint16_t*>(a.out) + to;
+  if (whole) {
+    if constexpr (N % 8 == 0) {
+#pragma unroll
+      for (int k = 0; k < N / 2; k += 4) *reinterpret_cast<u32x4*>(p + 2 * k) = (u32x4){pair[k], pair[k + 1], pair[k + 2], pair[k + 3]};
+    } else {
+#pragma unroll
+      for (int k = 0; k < N / 2; k += 2) *reinterpret_cast<u32x2*>(p + 2 * k) = (u32x2){pair[k], pair[k + 1]};
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      if (col + (uint32_t)k < a.n_out) p[k] = (uint16_t)(pair[k / 2] >> (16 * (k & 1)));
+  }
+}
+
+// Few rows: the weights are read once, straight into registers, and what bounds it is that reading.  A block is 16 rows by
+// MT and 16 channels by NT (gated: NT / 2 of the gate and as many beside them); its waves share what is summed over, 128
+// bytes of a row in turn, and their sums meet in shared memory, in the order of the waves.
+template <typename T, int MT, int NT, bool Gated, int Waves>
+__global__ void __launch_bounds__(64 * Waves) product_stream_kernel(ProductArgs a) {
+  using Sum = typename Operand<T>::Sum;
+  constexpr int kAhead = 4;  // 128-byte steps whose loads are under way at once
+  constexpr int kTiles = Gated ? NT / 2 : NT;
+  static_assert(!Gated || NT % 2 == 0, "a gate's channels lie in one wave with those that it gates");
+  __shared__ Sum sums[Waves][MT * NT][64];
+  const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x / 64u, i = lane & 15u, g = lane / 16u;
+  if (blockIdx.x == 0u && blockIdx.y == 0u && wave == 0u) check_starts(a);
+  const RowTile t = row_tile<16 * MT>(a, blockIdx.y);
+  if (t.rows == 0u) return;
+  const uint32_t n0 = blockIdx.x * (16u * kTiles);
+  const char* weights = a.w + t.expert * a.expert_stride;
+  const char* wp[NT];
+  const char* ap[MT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const uint32_t c = min(n0 + (Gated ? n / 2 : n) * 16u + i, a.n_out - 1u) + (Gated && n % 2 ? a.n_out : 0u);
+    wp[n] = weights + c * a.w_stride;
+  }
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    const uint32_t r = m * 16u + i;
+    bool ok;
+    ap[m] = a.a + source_row(a, t.begin + (r < t.rows ? r : 0u), ok) * a.a_stride;
+  }
+  Sum sum[MT][NT] = {};
+  const uint32_t whole = a.in_bytes / 128u, steps = (a.in_bytes + 127u) / 128u;
+  uint32_t at = wave;
+  for (; at + (kAhead - 1) * Waves < whole; at += kAhead * Waves) {
+    u32x4 wv[kAhead][NT][2], av[kAhead][MT][2];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t byte = (at + u * Waves) * 128u + g * 32u + h * 16u;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) wv[u][n][h] = *reinterpret_cast<const u32x4*>(wp[n] + byte);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) av[u][m][h] = *reinterpret_cast<const u32x4*>(ap[m] + byte);
+      }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int n = 0; n < NT; ++n) sum[m][n] = Operand<T>::mfma(wv[u][n][h], av[u][m][h], sum[m][n]);
+  }
+  if (at < steps) {  // what is left, all of it under way at once; bytes from the rows' end on are zeros in both
+    u32x4 wv[kAhead][NT][2], av[kAhead][MT][2];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t byte = (at + u * Waves) * 128u + g * 32u + h * 16u;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) wv[u][n][h] = row_bytes(wp[n], byte, a.in_bytes);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) av[u][m][h] = row_bytes(ap[m], byte, a.in_bytes);
+      }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int n = 0; n < NT; ++n) sum[m][n] = Operand<T>::mfma(wv[u][n][h], av[u][m][h], sum[m][n]);
+  }
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) sums[wave][m * NT + n][lane] = sum[m][n];
+  __syncthreads();
+  for (uint32_t u = wave; u < (uint32_t)(MT * kTiles); u += Waves) {
+    const uint32_t m = u / kTiles, n = u % kTiles, first = m * NT + (Gated ? 2u * n : n);
+    Sum y = sums[0][first][lane], up = y;
+#pragma unroll
+    for (int w = 1; w < Waves; ++w) y += sums[w][first][lane];
+    if constexpr (Gated) {
+      up = sums[0][first + 1u][lane];
+#pragma unroll
+      for (int w = 1; w < Waves; ++w) up += sums[w][first + 1u][lane];
+    }
+    const uint32_t r = m * 16u + i, col = n0 + n * 16u + g * 4u;
+    if (r >= t.rows || col >= a.n_out) continue;
+    bool ok;
+    const uint32_t source = source_row(a, t.begin + r, ok);
+    if (!ok) {
+      atomicOr(a.status, MAASO_INST_BAD_ROW);
+      continue;
+    }
+    float yf[4] = {(float)y[0], (float)y[1], (float)y[2], (float)y[3]}, uf[4] = {(float)up[0], (float)up[1], (float)up[2], (float)up[3]};
+    finish<T, 4, Gated>(a, t.expert, t.begin + r, source, col, yf, uf);
+  }
+}
+
+// Many rows: a block is BM rows by BN channels, steps of 128 bytes of both come to shared memory asynchronously, into one of
+// two places while the step in the other is multiplied.  A row's eight pieces of 16 bytes lie crossed with the row's lowest three bits, so that
+// reads of one piece of neighbouring rows meet different banks.
+template <typename T, int WM, int WN, int MI, int NI, bool Gated>
+__global__ void __launch_bounds__(64 * WM * WN) product_tile_kernel(ProductArgs a) {
+  using Sum = typename Operand<T>::Sum;
+  constexpr uint32_t kWaves = WM * WN, kRows = WM * MI * 16, kCols = WN * NI * 16, kStage = (kRows + kCols) * 128;
+  constexpr uint32_t kALoads = kRows / 8 / kWaves, kBLoads = kCols / 8 / kWaves;
+  constexpr int H = Gated ? NI / 2 : NI;  // channel tiles of a wave's outputs
+  constexpr uint32_t kOut = WN * H * 16, kAcross = 8;
+  static_assert(kRows % (8 * kWaves) == 0 && kCols % (8 * kWaves) == 0 && (!Gated || NI % 2 == 0), "whole loads, whole gates");
+  __shared__ __attribute__((aligned(1024))) char lds[2 * kStage];
+  const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x / 64u), i = lane & 15u, g = lane / 16u;
+  const uint32_t wm = wave / WN, wn = wave % WN;
+  if (blockIdx.x == 0u && wave == 0u) check_starts(a);
+
+  // Which tile: those of one eighth of the list run on one die, neighbours of up to kAcross row tiles at once, so that the die's
+  // cache holds what they share.
+  uint32_t tiles_down = (a.n_rows + kRows - 1u) / kRows;
+  Groups<kRows> groups;
+  if (a.start) {
+    for (;; groups.base += 64u) {
+      groups.look(a);
+      if (groups.base + 64u >= a.n_experts) break;
+    }
+    tiles_down = groups.seen;
+  }
+  const uint32_t tiles = tiles_down * a.col_tiles, share = (tiles + 7u) / 8u;
+  const uint32_t at = (blockIdx.x & 7u) * share + blockIdx.x / 8u;
+  if (blockIdx.x / 8u >= share || at >= tiles) return;
+  const uint32_t band = at / (kAcross * a.col_tiles), in_band = at - band * kAcross * a.col_tiles, high = min(kAcross, tiles_down - band * kAcross);
+  const uint32_t col_tile = in_band / high, down = band * kAcross + in_band % high;
+  const RowTile t = a.start && a.n_experts <= 64u ? groups.take(down) : row_tile<kRows>(a, down);
+  if (t.rows == 0u) return;
+  const uint32_t n0 = col_tile * kOut;
+
+  const char* ap[kALoads];
+  const char* bp[kBLoads];
+  const uint32_t piece = ((lane & 7u) ^ (lane / 8u)) * 16u;
+#pragma unroll
+  for (uint32_t q = 0; q < kALoads; ++q) {
+    const uint32_t r = (wave * kALoads + q) * 8u + lane / 8u;
+    bool ok;
+    ap[q] = a.a + source_row(a, t.begin + (r < t.rows ? r : 0u), ok) * a.a_stride + piece;
+  }
+  const char* weights = a.w + t.expert * a.expert_stride;
+#pragma unroll
+  for (uint32_t q = 0; q < kBLoads; ++q) {
+    // Row p of a wave's channels lies where its sums come out beside their neighbours': a lane of the matrix unit's result has four
+    // rows of each tile, which are to be 4 H channels in a row.
+    const uint32_t b = (wave * kBLoads + q) * 8u + lane / 8u, p = b % (NI * 16u), n = p / 16u, r = p % 16u;
+    const uint32_t c = n0 + b / (NI * 16u) * (H * 16u) + r / 4u * (4u * H) + n % H * 4u + r % 4u;
+    bp[q] = weights + (min(c, a.n_out - 1u) + (Gated && n >= (uint32_t)H ? a.n_out : 0u)) * a.w_stride + piece;
+  }
+
+  const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+  const uint32_t whole = a.in_bytes / 128u, steps = (a.in_bytes + 127u) / 128u;
+  // (m0 is named as changed, so that none of the compiler's own uses of it, from its setting on, has this between; that it warns of, as of any
+  // reserved register.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+  auto async16 = [&](const char* from, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_base + to), "v"(from) : "memory", "m0");
+  };
+#pragma clang diagnostic pop
+  auto bring = [&](uint32_t step, uint32_t buffer) {
+    const uint32_t to = buffer * kStage, byte = step * 128u;
+    if (step < whole) {
+#pragma unroll
+      for (uint32_t q = 0; q < kALoads; ++q) async16(ap[q] + byte, to + (wave * kALoads + q) * 1024u);
+#pragma unroll
+      for (uint32_t q = 0; q < kBLoads; ++q) async16(bp[q] + byte, to + kRows * 128u + (wave * kBLoads + q) * 1024u);
+    } else {  // the rows' end lies in this step: zeros behind it in both
+#pragma unroll
+      for (uint32_t q = 0; q < kALoads; ++q)
+        *reinterpret_cast<u32x4*>(lds + to + (wave * kALoads + q) * 1024u + lane * 16u) = row_bytes(ap[q] - piece, byte + piece, a.in_bytes);
+#pragma unroll
+      for (uint32_t q = 0; q < kBLoads; ++q)
+        *reinterpret_cast<u32x4*>(lds + to + kRows * 128u + (wave * kBLoads + q) * 1024u + lane * 16u) = row_bytes(bp[q] - piece, byte + piece, a.in_bytes);
+    }
+  };
+
+  Sum sum[MI][NI] = {};
+  bring(0u, 0u);
+  for (uint32_t step = 0; step < steps; ++step) {
+    const uint32_t buffer = step & 1u;
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (step + 1u < steps) bring(step + 1u, buffer ^ 1u);
+    const char* rows = lds + buffer * kStage + (wm * MI * 16u + i) * 128u;
+    const char* cols = lds + buffer * kStage + kRows * 128u + (wn * NI * 16u + i) * 128u;
+#pragma unroll
+    for (uint32_t ks = 0; ks < 2u; ++ks) {
+      const uint32_t place = ((ks * 4u + g) ^ (i & 7u)) * 16u;
+      u32x4 av[MI], bv[NI];
+#pragma unroll
+      for (int n = 0; n < NI; ++n) bv[n] = *reinterpret_cast<const u32x4*>(cols + n * 2048 + place);
+#pragma unroll
+      for (int m = 0; m < MI; ++m) av[m] = *reinterpret_cast<const u32x4*>(rows + m * 2048 + place);
+#pragma unroll
+      for (int m = 0; m < MI; ++m)
+#pragma unroll
+        for (int n = 0; n < NI; ++n) sum[m][n] = Operand<T>::mfma(bv[n], av[m], sum[m][n]);
+    }
+  }
+
+#pragma unroll
+  for (int m = 0; m < MI; ++m) {
+    const uint32_t r = wm * MI * 16u + m * 16u + i, col = n0 + wn * (H * 16u) + g * (4u * H);
+    if (r >= t.rows || col >= a.n_out) continue;
+    bool ok;
+    const uint32_t source = source_row(a, t.begin + r, ok);
+    if (!ok) {
+      atomicOr(a.status, MAASO_INST_BAD_ROW);
+      continue;
+    }
+    float y[4 * H], up[4 * H];
+#pragma unroll
+    for (int n = 0; n < H; ++n)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        y[4 * n + k] = (float)sum[m][n][k];
+        up[4 * n + k] = Gated ? (float)sum[m][n + (Gated ? H : 0)][k] : 0.0f;
+      }
+    finish<T, 4 * H, Gated>(a, t.expert, t.begin + r, source, col, y, up);
+  }
+}
+
+}  // namespace maaso

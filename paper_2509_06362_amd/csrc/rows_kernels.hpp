@@ -1,0 +1,220 @@
+// Rows of activations to 8-bit integers with a scale each, behind a norm or a gate; and the joining of experts' rows.
+// Both are bound by memory.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "../../include/maaso_instance.h"
+#include "element_types.hpp"
+#include "gate.hpp"
+
+namespace maaso {
+
+struct QuantizeArgs {
+  const void* x;
+  const void* weight;
+  int8_t* q;
+  float* scale;
+  uint64_t x_stride, q_stride;  // elements
+  uint32_t n, width;
+  float eps;
+};
+
+// Eight elements that begin anywhere.
+template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) Eight { T v[8]; };
+
+// Elements [at, at + 8) of a row of `width`, zeros from its end on.
+template <typename T> __device__ inline void load8(const T* row, uint32_t at, uint32_t width, float (&y)[8]) {
+  if (at + 8u <= width) {
+    const Eight<T> e = *reinterpret_cast<const Eight<T>*>(row + at);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) y[k] = (float)e.v[k];
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) y[k] = at + (uint32_t)k < width ? (float)row[at + k] : 0.0f;
+  }
+}
+
+// One row to `Threads` threads, eight neighbouring elements of each in turn, the first Held turns in registers; what is
+// longer is read, and its gate worked out, a second time.  One reduction: with a norm, max |x * weight| and the sum of squares are
+// taken together, for y = (x * weight) / sqrt(...) is largest where x * weight is.
+template <typename T, int Form, int Threads, int Held>
+__global__ void __launch_bounds__(Threads == 64 ? 256 : Threads) quantize_kernel(QuantizeArgs a) {
+  constexpr int kRows = Threads == 64 ? 4 : 1, kWaves = Threads / 64;  // rows of a block, waves of a row
+  __shared__ float sums[kWaves];
+  __shared__ uint32_t tops[kWaves];
+  const uint32_t thread = threadIdx.x % Threads, row = blockIdx.x * kRows + threadIdx.x / Threads;
+  if (row >= a.n) return;  // (a whole wave, or a whole block)
+  const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
+  const T* weight = static_cast<const T*>(a.weight);
+  const uint32_t turns = (a.width + 8u * Threads - 1u) / (8u * Threads);
+
+  float sum = 0.0f;
+  uint32_t top = 0u;  // of the magnitudes' bits: an infinity is above every number, a NaN above that
+  auto values = [&](uint32_t turn, float (&y)[8], bool first) {
+    const uint32_t at = (turn * Threads + thread) * 8u;
+    load8(x, at, a.width, y);
+    if constexpr (Form == MAASO_ROWS_NORM) {
+      if (first) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum = fmaf(y[k], y[k], sum);
+      }
+      if (weight) {
+        float w[8];
+        load8(weight, at, a.width, w);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) y[k] *= w[k];
+      }
+    } else if constexpr (Form == MAASO_ROWS_GATED) {
+      float up[8];
+      load8(x + a.width, at, a.width, up);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) y[k] = silu(y[k]) * up[k];
+    }
+    if (first) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) top = max(top, __builtin_bit_cast(uint32_t, y[k]) & 0x7fffffffu);
+    }
+  };
+  float held[Held][8];
+#pragma unroll
+  for (int h = 0; h < Held; ++h) {
+    if ((uint32_t)h < turns) values(h, held[h], true);
+  }
+  for (uint32_t t = Held; t < turns; ++t) {
+    float y[8];
+    values(t, y, true);
+  }
+#pragma unroll
+  for (int d = 32; d > 0; d /= 2) {
+    if constexpr (Form == MAASO_ROWS_NORM) sum += __shfl_xor(sum, d);
+    top = max(top, (uint32_t)__shfl_xor((int)top, d));
+  }
+  if constexpr (kWaves > 1) {
+    if ((thread & 63u) == 0u) {
+      sums[thread / 64u] = sum;
+      tops[thread / 64u] = top;
+    }
+    __syncthreads();
+    sum = 0.0f;
+    top = 0u;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      sum += sums[w];
+      top = max(top, tops[w]);
+    }
+  }
+  float most = __builtin_bit_cast(float, top), by = 1.0f;
+  bool good = top < 0x7f800000u;
+  if constexpr (Form == MAASO_ROWS_NORM) {
+    good = good && __builtin_bit_cast(uint32_t, sum) < 0x7f800000u;
+    if (good && top) {
+      by = 1.0f / sqrtf(sum / (float)a.width + a.eps);
+      most *= by;
+      good = most < __builtin_huge_valf();
+    }
+  }
+  const float scale = good ? most / 127.0f : __builtin_nanf("");
+  // Rows of very small numbers are raised by 2^100 first: 127 / m would be no number for them.
+  const float raise = most < 0x1p-100f ? 0x1p100f : 1.0f;
+  const float per = good && most > 0.0f ? 127.0f / (most * raise) : 0.0f;
+  if (thread == 0u) a.scale[row] = scale;
+  int8_t* q = a.q + row * a.q_stride;
+  auto store = [&](uint32_t turn, const float (&y)[8]) {
+    const uint32_t at = (turn * Threads + thread) * 8u;
+    uint32_t b[2] = {0u, 0u};
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float v = per == 0.0f ? 0.0f : rintf(y[k] * by * raise * per);
+      b[k / 4] |= ((uint32_t)(int)v & 255u) << (8 * (k % 4));
+    }
+    if (at + 8u <= a.width) {
+      *reinterpret_cast<u32x2*>(q + at) = (u32x2){b[0], b[1]};
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (at + (uint32_t)k < a.width) q[at + k] = (int8_t)(b[k / 4] >> (8 * (k % 4)));
+    }
+  };
+#pragma unroll
+  for (int h = 0; h < Held; ++h) {
+    if ((uint32_t)h < turns) store(h, held[h]);
+  }
+  for (uint32_t t = Held; t < turns; ++t) {
+    float y[8];
+    values(t, y, false);
+    store(t, y);
+  }
+}
+
+struct CombineArgs {
+  const void* y;
+  const void* residual;
+  void* out;
+  const int32_t* place;
+  const float* weight;
+  uint64_t y_stride, residual_stride, out_stride;  // elements
+  uint32_t n, k, width, n_rows;
+  uint32_t* status;
+};
+
+template <typename T> __device__ inline void store8(T* row, uint32_t at, uint32_t width, const float (&y)[8]) {
+  if constexpr (sizeof(T) == 4) {
+    if (at + 8u <= width) {
+      Eight<T> e;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) e.v[k] = y[k];
+      *reinterpret_cast<Eight<T>*>(row + at) = e;
+      return;
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (at + (uint32_t)k < width) row[at + k] = y[k];
+  } else {
+    const auto v = narrow8<T>(y);
+    if (at + 8u <= width) {
+      *reinterpret_cast<Eight<T>*>(row + at) = __builtin_bit_cast(Eight<T>, v);
+      return;
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (at + (uint32_t)k < width) row[at + k] = v[k];
+  }
+}
+
+// A thread is eight neighbouring elements of a token; the token's rows are read at once, four at a time.
+template <typename T> __global__ void __launch_bounds__(256) combine_kernel(CombineArgs a) {
+  const uint32_t per = (a.width + 7u) / 8u;
+  const uint64_t at = (uint64_t)blockIdx.x * 256u + threadIdx.x;
+  const uint64_t token = at / per;
+  const uint32_t col = (uint32_t)(at - token * per) * 8u;
+  if (token >= a.n) return;
+  float sum[8] = {};
+  if (a.residual) load8(static_cast<const T*>(a.residual) + token * a.residual_stride, col, a.width, sum);
+  for (uint32_t j = 0; j < a.k; j += 4u) {
+    float y[4][8], w[4];
+#pragma unroll
+    for (uint32_t u = 0; u < 4u; ++u) {
+      const bool in = j + u < a.k;
+      const int32_t p = in ? a.place[token * a.k + j + u] : -1;
+      const bool there = (uint32_t)p < a.n_rows;
+      if (p >= 0 && !there) atomicOr(a.status, MAASO_INST_BAD_ROW);
+      w[u] = there ? a.weight ? a.weight[token * a.k + j + u] : 1.0f : 0.0f;
+      if (there) {
+        load8(static_cast<const T*>(a.y) + (uint64_t)(uint32_t)p * a.y_stride, col, a.width, y[u]);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) y[u][k] = 0.0f;
+      }
+    }
+#pragma unroll
+    for (uint32_t u = 0; u < 4u; ++u)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) sum[k] = fmaf(w[u], y[u][k], sum[k]);
+  }
+  store8(static_cast<T*>(a.out) + token * a.out_stride, col, a.width, sum);
+}
+
+}  // namespace maaso

@@ -11,13 +11,15 @@ import ctypes as C
 
 from .binding import MaasoError, _check, _t, load_library
 
-MAASO_BF16, MAASO_FP16, MAASO_FP32, MAASO_E4M3 = 0, 1, 2, 3
+MAASO_BF16, MAASO_FP16, MAASO_FP32, MAASO_E4M3, MAASO_INT8 = 0, 1, 2, 3, 4
+MAASO_ROWS_PLAIN, MAASO_ROWS_NORM, MAASO_ROWS_GATED = 0, 1, 2
 
 BAD_PAGE, BAD_ROW, NO_PAGES, BAD_BOUND, BAD_TOKEN, BAD_POS = 1, 2, 4, 8, 16, 32
 
 EXPORTS = (
     "maaso_instance_create", "maaso_instance_destroy", "maaso_instance_status", "maaso_kv_extend", "maaso_kv_fork",
     "maaso_kv_trim", "maaso_kv_compact", "maaso_kv_copy", "maaso_kv_append", "maaso_kv_attention", "maaso_logits_adjust",
+    "maaso_rows_quantize", "maaso_scaled_product", "maaso_expert_route", "maaso_expert_product", "maaso_expert_combine",
 )
 
 
@@ -33,7 +35,7 @@ class CacheArgs(C.Structure):
                 ("v_scale", C.c_void_p)]
 
 
-# The three that follow are for callers of the C entry points: the calls below are filled in from the header itself.
+# Those that follow are for callers of the C entry points: the calls below are filled in from the header itself.
 class AppendArgs(C.Structure):
     _fields_ = [("type", C.c_uint32), ("n_tok", C.c_uint32), ("n_heads", C.c_uint32), ("rotary", C.c_uint32),
                 ("interleaved", C.c_uint32), ("n_pos", C.c_uint32), ("eps", C.c_float), ("q", C.c_void_p),
@@ -61,6 +63,37 @@ class LogitsArgs(C.Structure):
                 ("mask", C.c_void_p), ("mask_row", C.c_void_p), ("n_mask", C.c_uint32)]
 
 
+class QuantizeArgs(C.Structure):
+    _fields_ = [("type", C.c_uint32), ("form", C.c_uint32), ("n", C.c_uint32), ("width", C.c_uint32), ("eps", C.c_float),
+                ("x_stride", C.c_uint64), ("q_stride", C.c_uint64), ("x", C.c_void_p), ("weight", C.c_void_p),
+                ("q", C.c_void_p), ("scale", C.c_void_p)]
+
+
+class ProductArgs(C.Structure):
+    _fields_ = [("type", C.c_uint32), ("out_type", C.c_uint32), ("n_a", C.c_uint32), ("n_in", C.c_uint32),
+                ("n_out", C.c_uint32), ("gated", C.c_uint32), ("a_stride", C.c_uint64), ("w_stride", C.c_uint64),
+                ("out_stride", C.c_uint64), ("a", C.c_void_p), ("w", C.c_void_p), ("a_scale", C.c_void_p),
+                ("w_scale", C.c_void_p), ("bias", C.c_void_p), ("out", C.c_void_p)]
+
+
+class RouteArgs(C.Structure):
+    _fields_ = [("type", C.c_uint32), ("n", C.c_uint32), ("n_experts", C.c_uint32), ("k", C.c_uint32),
+                ("sigmoid", C.c_uint32), ("renorm", C.c_uint32), ("scale", C.c_float), ("stride", C.c_uint64),
+                ("logits", C.c_void_p), ("bias", C.c_void_p), ("expert", C.c_void_p), ("weight", C.c_void_p),
+                ("start", C.c_void_p), ("token", C.c_void_p), ("place", C.c_void_p)]
+
+
+class ExpertProductArgs(C.Structure):
+    _fields_ = [("product", ProductArgs), ("n_rows", C.c_uint32), ("n_experts", C.c_uint32),
+                ("expert_stride", C.c_uint64), ("start", C.c_void_p), ("token", C.c_void_p)]
+
+
+class CombineArgs(C.Structure):
+    _fields_ = [("type", C.c_uint32), ("n", C.c_uint32), ("k", C.c_uint32), ("width", C.c_uint32), ("n_rows", C.c_uint32),
+                ("y_stride", C.c_uint64), ("residual_stride", C.c_uint64), ("out_stride", C.c_uint64), ("y", C.c_void_p),
+                ("residual", C.c_void_p), ("out", C.c_void_p), ("place", C.c_void_p), ("weight", C.c_void_p)]
+
+
 _lib = None
 
 
@@ -80,7 +113,9 @@ def _library() -> C.CDLL:
         lib.maaso_kv_copy.argtypes = [p, p, p, u, p]
         lib.maaso_kv_append.argtypes = [p, p, u, p, p]
         lib.maaso_kv_attention.argtypes = [p, p, u, p, p, p]
-        lib.maaso_logits_adjust.argtypes = [p, p, p]
+        for call in (lib.maaso_logits_adjust, lib.maaso_rows_quantize, lib.maaso_scaled_product, lib.maaso_expert_route,
+                     lib.maaso_expert_product, lib.maaso_expert_combine):
+            call.argtypes = [p, p, p]
         missing = [n for n in EXPORTS if getattr(lib, n).argtypes is None]
         if missing:  # an undeclared signature would pass pointers as C ints
             raise RuntimeError(f"instance.py declares no argument types for {missing}")
@@ -102,7 +137,8 @@ def _load_native():
         raise RuntimeError(f"the marshalling module is missing ({e}): build it first "
                            "(python -m paper_2509_06362_amd.build); there is no fallback path") from e
     calls = (lib.maaso_kv_extend, lib.maaso_kv_fork, lib.maaso_kv_trim, lib.maaso_kv_compact, lib.maaso_kv_copy,
-             lib.maaso_kv_append, lib.maaso_kv_attention, lib.maaso_logits_adjust)
+             lib.maaso_kv_append, lib.maaso_kv_attention, lib.maaso_logits_adjust, lib.maaso_rows_quantize,
+             lib.maaso_scaled_product, lib.maaso_expert_route, lib.maaso_expert_product, lib.maaso_expert_combine)
     _marshal.bind(*(C.cast(f, C.c_void_p).value for f in calls))
     _native = _marshal
     return _marshal
@@ -116,7 +152,7 @@ def _type(t) -> int:
     if not _types:
         torch = _t()
         _types.update({torch.bfloat16: MAASO_BF16, torch.float16: MAASO_FP16, torch.float32: MAASO_FP32,
-                       torch.float8_e4m3fn: MAASO_E4M3})
+                       torch.float8_e4m3fn: MAASO_E4M3, torch.int8: MAASO_INT8})
     try:
         return _types[t.dtype]
     except KeyError:
@@ -251,3 +287,38 @@ def maaso_logits_adjust(inst: Instance, *, logits, out=None, chosen=None, repeti
     _check((_native or _load_native()).logits(inst.handle, logits, out, chosen, repetition, frequency, presence, temperature,
                                               history, history_start, bias_token, bias_value, bias_start, mask, mask_row,
                                               stream), "maaso_logits_adjust")
+
+
+def maaso_rows_quantize(inst: Instance, *, x, q, scale, weight=None, norm=False, gated=False, eps=1e-6, stream=None) -> None:
+    """x [rows, width] (gated: [rows, 2 width]), q [rows, width] (int8), scale [rows] (float32); rows 16 bytes apart or a
+    multiple of that.  norm: x / sqrt(mean x^2 + eps) * weight; gated: silu of the first half times the second."""
+    _check((_native or _load_native()).quantize(inst.handle, x, q, scale, weight, norm, gated, eps, stream),
+           "maaso_rows_quantize")
+
+
+def maaso_scaled_product(inst: Instance, *, a, w, out, a_scale=None, w_scale=None, bias=None, gated=False, stream=None) -> None:
+    """a [rows, in], w [channels, in] (int8), rows 16 bytes apart or a multiple of that; out [rows, channels], gated: half as
+    many channels; a_scale [rows], w_scale and bias [channels] (float32)."""
+    _check((_native or _load_native()).scaled_product(inst.handle, a, a_scale, w, w_scale, out, bias, gated, stream),
+           "maaso_scaled_product")
+
+
+def maaso_expert_route(inst: Instance, *, logits, expert, weight, start=None, token=None, place=None, bias=None, sigmoid=False,
+                       renorm=True, scale=1.0, stream=None) -> None:
+    """logits [tokens, experts]; expert, place [tokens, chosen], token [tokens * chosen], start [experts + 1] (int32), weight
+    [tokens, chosen], bias [experts] (float32)."""
+    _check((_native or _load_native()).route(inst.handle, logits, bias, expert, weight, start, token, place, sigmoid, renorm,
+                                             scale, stream), "maaso_expert_route")
+
+
+def maaso_expert_product(inst: Instance, *, a, w, out, start, token=None, a_scale=None, w_scale=None, bias=None, gated=False,
+                         stream=None) -> None:
+    """a [rows, in] and w [experts, channels, in] of one type (bfloat16, float16, int8); out [places, channels], gated: half as
+    many; token [places]; a_scale [rows], w_scale and bias [experts, channels] (float32)."""
+    _check((_native or _load_native()).expert_product(inst.handle, a, a_scale, w, w_scale, out, start, token, bias, gated,
+                                                      stream), "maaso_expert_product")
+
+
+def maaso_expert_combine(inst: Instance, *, y, place, out, weight=None, residual=None, stream=None) -> None:
+    """y [rows, width], residual and out [tokens, width], of one type; place [tokens, chosen] (int32), weight the same (float32)."""
+    _check((_native or _load_native()).combine(inst.handle, y, place, weight, out, residual, stream), "maaso_expert_combine")

@@ -1,0 +1,141 @@
+"""Rows to 8-bit integers against the formulas in 64 bits."""
+import math
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+from paper_2509_06362_amd import instance as I  # noqa: E402
+
+TYPES = {"bf16": torch.bfloat16, "fp16": torch.float16, "fp32": torch.float32}
+HALF = 2.0 ** -24  # half a step of binary32
+
+
+@pytest.fixture(scope="module")
+def inst():
+    with I.maaso_instance_create() as one:
+        yield one
+        assert I.maaso_instance_status(one) == 0
+
+
+def padded(t, step, fill):
+    """Rows of t a multiple of `step` elements apart and one step more, what lies between them `fill`."""
+    wide = -(-t.shape[-1] // step) * step + step
+    held = torch.full((*t.shape[:-1], wide), fill, dtype=t.dtype, device="cuda")
+    held[..., :t.shape[-1]] = t
+    return held[..., :t.shape[-1]]
+
+
+def formula(x, form, weight, eps):
+    x = x.double().cpu()
+    if form == "norm":
+        return x / (x.pow(2).mean(1, keepdim=True) + eps).sqrt() * (weight.double().cpu() if weight is not None else 1.0)
+    if form == "gated":
+        a, b = x.chunk(2, 1)
+        return a * torch.sigmoid(a) * b
+    return x
+
+
+def relative(form, width):
+    """What binary32 may lose of y, relative: nothing; a thread's part of the sum (eight elements a turn of 64 threads), ten additions
+    between threads, mean, eps, root, quotient and two products, one of the squares' errors halved by the root; the gate's
+    exponential (two steps of its own, the argument's rounding made good), reciprocal and products."""
+    return {"plain": 0, "norm": (-(-width // 512) * 8 + 24), "gated": 24}[form] * HALF
+
+
+def check(x, q, scale, form, weight=None, eps=1e-6):
+    y = formula(x, form, weight, eps)
+    width = y.shape[1]
+    most = y.abs().amax(1)
+    rel = relative(form, width) + 4 * HALF  # quotients, products
+    got = scale.double().cpu()
+    assert ((got - most / 127).abs() <= rel * most / 127 + 2.0 ** -150).all()  # (a step of the smallest numbers)
+    want = torch.where(most > 0, 127 / most.clamp(min=1e-300), torch.zeros(())).unsqueeze(1) * y
+    off = (q.double().cpu() - want).abs()
+    assert (off <= 0.5 + 127 * 2 * rel).all(), off.max()
+    assert q.max() <= 127 and q.min() >= -127
+
+
+def run(inst, x, width, form, weight=None, eps=1e-6):
+    q = padded(torch.full((x.shape[0], width), 99, dtype=torch.int8, device="cuda"), 16, 77)
+    scale = torch.full((x.shape[0],), -5.0, device="cuda")
+    I.maaso_rows_quantize(inst, x=x, q=q, scale=scale, weight=weight, norm=form == "norm", gated=form == "gated", eps=eps)
+    torch.cuda.synchronize()
+    if q.shape[0] > 1:  # between the rows nothing is written
+        held = torch.as_strided(q, (q.shape[0] - 1, q.stride(0)), (q.stride(0), 1))
+        assert (held[:, width:] == 77).all()
+    return q, scale
+
+
+@pytest.mark.parametrize("width", [1, 7, 8, 9, 63, 100, 512, 2047, 2048, 2049, 8191, 8192, 9000, 20001])
+@pytest.mark.parametrize("form", ["plain", "norm", "gated"])
+@pytest.mark.parametrize("name", list(TYPES))
+def test_widths(inst, name, form, width):
+    g = torch.Generator().manual_seed(width)
+    x = (torch.randn(5, width * (2 if form == "gated" else 1), generator=g) * 3).to(TYPES[name]).cuda()
+    weight = (1 + 0.3 * torch.randn(width, generator=g)).to(TYPES[name]).cuda() if form == "norm" and width % 2 else None
+    for step in (8, 3):  # rows that begin anywhere
+        x = padded(x, step, math.nan)
+        check(x, *run(inst, x, width, form, weight), form, weight)
+
+
+@pytest.mark.parametrize("n, width", [(1, 2048), (2, 33), (1023, 96), (1024, 96), (1025, 2048), (1027, 2056), (5000, 8)])
+@pytest.mark.parametrize("form", ["plain", "norm", "gated"])
+def test_rows(inst, form, n, width):
+    g = torch.Generator().manual_seed(n)
+    x = torch.randn(n, width * (2 if form == "gated" else 1), generator=g).to(torch.bfloat16).cuda()
+    weight = (1 + 0.3 * torch.randn(width, generator=g)).to(torch.bfloat16).cuda() if form == "norm" else None
+    check(x, *run(inst, x, width, form, weight), form, weight)
+
+
+@pytest.mark.parametrize("n", [6, 1030])
+@pytest.mark.parametrize("form", ["plain", "norm", "gated"])
+def test_rows_without_numbers(inst, form, n):
+    """Zeros give zeros, a NaN or an infinity the row's NaN scale, and no other row has a part in it."""
+    width = 200
+    x = torch.randn(n, width * (2 if form == "gated" else 1), generator=torch.Generator().manual_seed(3))
+    x[0] = 0
+    x[1, 17] = math.nan
+    x[2, 199] = math.inf
+    x[3, 5] = -math.inf
+    x = x.cuda()
+    q, scale = run(inst, x, width, form)
+    assert (q[:4] == 0).all() and scale[0] == 0 and scale[1:4].isnan().all()
+    check(x[4:], q[4:], scale[4:], form)
+    if form == "norm":  # eps 0: zeros are still zeros
+        q, scale = run(inst, x, width, form, eps=0.0)
+        assert (q[:4] == 0).all() and scale[0] == 0 and scale[1:4].isnan().all()
+        check(x[4:], q[4:], scale[4:], form, eps=0.0)
+
+
+def test_rows_of_very_small_and_large_numbers(inst):
+    x = torch.randn(8, 64, generator=torch.Generator().manual_seed(4)).clamp(-3, 3)
+    by = torch.tensor([2.0 ** -140, 2.0 ** -120, 2.0 ** -101, 2.0 ** -99, 2.0 ** -60, 1.0, 2.0 ** 100, 2.0 ** 126])
+    x = (x.double() * by.double()[:, None]).float().cuda()  # (the first row is rounded to steps of 2^-149)
+    check(x, *run(inst, x, 64, "plain"), "plain")
+    big = torch.full((1, 64), 1e25, device="cuda")  # its squares are beyond binary32
+    q, scale = run(inst, big, 64, "norm")
+    assert (q == 0).all() and scale.isnan().all()
+
+
+def test_the_gate_far_out(inst):
+    gate = torch.tensor([-1e30, -200.0, -80.0, -20.0, -1.0, -1e-30, 0.0, 1e-30, 1.0, 20.0, 80.0, 200.0, 1e30]).repeat(3, 1)
+    up = torch.tensor([[1.0], [-2.0], [1e-25]]).expand(3, 13).clone()
+    x = padded(torch.cat([gate, up], 1).cuda(), 8, math.nan)
+    q, scale = run(inst, x, 13, "gated")
+    check(x, q, scale, "gated")
+
+
+def test_ties_go_to_even(inst):
+    x = torch.tensor([[127.0, 0.5, 1.5, 2.5, -0.5, -1.5, -2.5, 63.5]], device="cuda")
+    q, scale = run(inst, x, 8, "plain")
+    assert q.tolist() == [[127, 0, 2, 2, 0, -2, -2, 64]] and scale.item() == 1.0
+
+
+def test_other_alignments_of_the_weight(inst):
+    x = torch.randn(3, 24, generator=torch.Generator().manual_seed(6)).to(torch.float16).cuda()
+    held = (1 + 0.5 * torch.randn(30, generator=torch.Generator().manual_seed(7))).to(torch.float16).cuda()
+    for at in range(6):
+        check(x, *run(inst, x, 24, "norm", held[at:at + 24]), "norm", held[at:at + 24])
