@@ -1,22 +1,24 @@
-// The gate of a feed-forward: silu(x) = x / (1 + exp(-x)).
+// Exponentials, and the gate of a feed-forward: silu(x) = x / (1 + exp(-x)).
 #pragma once
 
 #include <hip/hip_runtime.h>
 
 namespace maaso {
 
-// exp(-|x|), which cannot overflow, from the exponential to base 2: what the rounding of |x| log2(e) loses is made good in the
-// first order.  1 / (1 + e) with one Newton step on the reciprocal.
+// exp(d) for d <= 0 from the exponential to base 2; what the rounding of d log2(e) loses is made good in the first order.
+__device__ inline float exp_below(float d) {
+  constexpr float kLog2E = 1.44269504f, kRest = 1.92596299e-8f, kLn2 = 0.693147181f;  // log2(e) = kLog2E + kRest
+  const float t = d * kLog2E;
+  const float rest = fmaf(d, kRest, fmaf(d, kLog2E, -t));
+  const float p = __builtin_amdgcn_exp2f(t);
+  return t > -160.0f ? fmaf(p, rest * kLn2, p) : d != d ? d : 0.0f;
+}
+
 struct Halves {
-  float e, r;  // exp(-|x|), 1 / (1 + e)
+  float e, r;  // exp(-|x|), which cannot overflow, and 1 / (1 + e), with one Newton step on the reciprocal
 };
 __device__ inline Halves halves(float x) {
-  constexpr float kLog2E = 1.44269504f, kRest = 1.92596299e-8f, kLn2 = 0.693147181f;  // log2(e) = kLog2E + kRest
-  const float m = fabsf(x), t = m * kLog2E;
-  const float rest = fmaf(m, kRest, fmaf(m, kLog2E, -t));
-  const float p = __builtin_amdgcn_exp2f(-t);
-  const float e = t < 160.0f ? fmaf(p, -rest * kLn2, p) : x != x ? x : 0.0f;
-  const float d = 1.0f + e, q = __builtin_amdgcn_rcpf(d);
+  const float e = exp_below(-fabsf(x)), d = 1.0f + e, q = __builtin_amdgcn_rcpf(d);
   return {e, fmaf(q, fmaf(-d, q, 1.0f), q)};
 }
 __device__ inline float sigmoid(float x) {

@@ -104,20 +104,31 @@ int launch_product(uint32_t type, ProductArgs& a, bool gated, uint32_t n_cu, hip
   return launch_product<_Float16>(a, gated, n_cu, s);
 }
 
-template <typename T, int Per>
-void launch_choose(const RouteArgs& a, hipStream_t s) {
-  const dim3 g((a.n + 3u) / 4u);
-  if (a.bias) hipLaunchKernelGGL((route_choose_kernel<T, Per, true>), g, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((route_choose_kernel<T, Per, false>), g, dim3(256), 0, s, a);
+template <typename T, int Lanes, int Quads, bool Biased>
+void launch_route(const RouteArgs& a, hipStream_t s) {
+  if (a.start && a.n <= kOneBlock) {
+    hipLaunchKernelGGL((route_kernel<T, Lanes, Quads, Biased>), dim3(1), dim3(1024), a.n_experts * ((a.n + 31u) / 32u + 1u) * 4u, s, a);
+    return;
+  }
+  hipLaunchKernelGGL((route_choose_kernel<T, Lanes, Quads, Biased>), dim3(a.chunks), dim3(1024), 0, s, a);
+  if (!a.start) return;
+  hipLaunchKernelGGL(route_before_kernel, dim3((a.n_experts + 15u) / 16u), dim3(1024), 0, s, a);
+  hipLaunchKernelGGL(route_place_kernel, dim3(a.chunks), dim3(1024), 0, s, a);
+}
+
+template <typename T, bool Biased>
+void launch_route(const RouteArgs& a, hipStream_t s) {
+  if (a.n_experts <= 64u) launch_route<T, 16, 1, Biased>(a, s);
+  else if (a.n_experts <= 128u) launch_route<T, 16, 2, Biased>(a, s);
+  else if (a.n_experts <= 256u) launch_route<T, 16, 4, Biased>(a, s);
+  else if (a.n_experts <= 512u) launch_route<T, 32, 4, Biased>(a, s);
+  else launch_route<T, 64, 4, Biased>(a, s);
 }
 
 template <typename T>
-void launch_choose(const RouteArgs& a, hipStream_t s) {
-  if (a.n_experts <= 64u) launch_choose<T, 1>(a, s);
-  else if (a.n_experts <= 128u) launch_choose<T, 2>(a, s);
-  else if (a.n_experts <= 256u) launch_choose<T, 4>(a, s);
-  else if (a.n_experts <= 512u) launch_choose<T, 8>(a, s);
-  else launch_choose<T, 16>(a, s);
+void launch_route(const RouteArgs& a, hipStream_t s) {
+  if (a.bias) launch_route<T, true>(a, s);
+  else launch_route<T, false>(a, s);
 }
 
 }  // namespace
@@ -186,30 +197,19 @@ int maaso_expert_route(maaso_instance* inst, const maaso_expert_route_args* p, v
   if ((uint64_t)p->n * p->k > 0x7fffffffull || (p->n > 1u && p->stride < p->n_experts)) return MAASO_E_SHAPE;
   if (p->n == 0 && !p->start) return MAASO_OK;
   RouteArgs a{p->logits, p->bias, p->expert, p->weight, p->start, p->token, p->place, p->stride, p->n, p->n_experts, p->k,
-              p->sigmoid != 0u, p->renorm != 0u, p->scale, (p->n + kChunk - 1u) / kChunk, nullptr};
+              p->sigmoid != 0u, p->renorm != 0u, p->scale, (p->n + kChunk - 1u) / kChunk, nullptr, nullptr};
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
   InstanceCall call(inst, s);
   if (call.rc != MAASO_OK) return call.rc;
   if (order && a.n > kOneBlock) {
     Carve ws{inst->ws, inst->ws_bytes};
-    a.counts = ws.take<uint32_t>((size_t)a.chunks * a.n_experts);
+    a.before = ws.take<uint32_t>((size_t)a.chunks * a.n_experts);
+    a.total = ws.take<uint32_t>(a.n_experts);
     if (!ws.fits) return MAASO_E_WORKSPACE;
   }
-  if (a.n) {
-    if (p->type == MAASO_BF16) launch_choose<__bf16>(a, s);
-    else if (p->type == MAASO_FP16) launch_choose<_Float16>(a, s);
-    else launch_choose<float>(a, s);
-  }
-  if (!order) return launched();
-  if (a.n <= kOneBlock) {
-    const uint32_t words = (a.n + 31u) / 32u;
-    hipLaunchKernelGGL(route_order_kernel, dim3(1), dim3(1024), a.n_experts * (words + 1u) * 4u, s, a);
-    return launched();
-  }
-  const uint32_t room = a.n_experts * (kChunk / 32u) * 4u;
-  hipLaunchKernelGGL(route_count_kernel, dim3(a.chunks), dim3(256), room, s, a);
-  hipLaunchKernelGGL(route_starts_kernel, dim3(1), dim3(1024), 0, s, a);
-  hipLaunchKernelGGL(route_place_kernel, dim3(a.chunks), dim3(256), room, s, a);
+  if (p->type == MAASO_BF16) launch_route<__bf16>(a, s);
+  else if (p->type == MAASO_FP16) launch_route<_Float16>(a, s);
+  else launch_route<float>(a, s);
   return launched();
 }
 

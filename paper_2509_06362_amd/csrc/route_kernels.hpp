@@ -25,112 +25,186 @@ struct RouteArgs {
   uint32_t n, n_experts, k;
   bool sigmoid, renorm;
   float scale;
-  uint32_t chunks;     // of kChunk tokens
-  uint32_t* counts;    // workspace [chunks][n_experts]: an expert's tokens in a chunk, then those before the chunk, from the expert's start on
+  uint32_t chunks;   // of kChunk tokens
+  uint32_t* before;  // workspace [chunks][n_experts]: an expert's tokens in a chunk, then those of the chunks before it
+  uint32_t* total;   // workspace [n_experts]
 };
 
-constexpr uint32_t kChunk = 64;       // tokens whose places are worked out together
-constexpr uint32_t kOneBlock = 256;   // tokens that one block does alone
+constexpr uint32_t kChunk = 64;      // tokens whose places are worked out together
+constexpr uint32_t kOneBlock = 256;  // tokens that one block chooses for and puts in order alone
+
+template <int Ctrl> __device__ inline float dpp(float v) {
+  const int b = __builtin_bit_cast(int, v);
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(b, b, Ctrl, 0xf, 0xf, false));
+}
+template <int Ctrl> __device__ inline uint32_t dpp(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, Ctrl, 0xf, 0xf, false);
+}
+
+// Over groups of Lanes neighbouring lanes (16, 32 or 64); every lane ends with the group's value.
+template <int Lanes, typename V, typename Op> __device__ inline V join(V v, Op op) {
+  v = op(v, dpp<0xb1>(v));   // lane ^ 1
+  v = op(v, dpp<0x4e>(v));   // lane ^ 2
+  v = op(v, dpp<0x141>(v));  // the mirrored half of eight
+  v = op(v, dpp<0x140>(v));  // the mirrored sixteen
+  if constexpr (Lanes >= 32) v = op(v, (V)__shfl_xor(v, 16));
+  if constexpr (Lanes >= 64) v = op(v, (V)__shfl_xor(v, 32));
+  return v;
+}
+template <int Lanes> __device__ inline float largest(float v) {
+  return join<Lanes>(v, [](float a, float b) { return fmaxf(a, b); });
+}
+template <int Lanes> __device__ inline uint32_t lowest(uint32_t v) {
+  return join<Lanes>(v, [](uint32_t a, uint32_t b) { return min(a, b); });
+}
+template <int Lanes> __device__ inline uint32_t in_all(uint32_t v) {
+  return join<Lanes>(v, [](uint32_t a, uint32_t b) { return a + b; });
+}
+template <int Lanes> __device__ inline float in_all(float v) {
+  return join<Lanes>(v, [](float a, float b) { return a + b; });
+}
+
+constexpr float kNever = -__builtin_huge_valf();  // the score of what is not chosen, or has been
 
 __device__ inline double score64(float x, float bias) { return 1.0 / (1.0 + exp(-(double)x)) + (double)bias; }
 
-// The experts of one token, by one wave: lane l has the logits of experts l, l + 64, ...; Per of them.
-template <typename T, int Per, bool Biased>
-__device__ inline void choose(const RouteArgs& a, uint32_t t) {
-  const uint32_t lane = threadIdx.x & 63u;
+// Four neighbouring logits that begin anywhere.
+template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) Four { T v[4]; };
+
+// The experts of one token, by Lanes lanes that hold 4 Quads scores each; lane l those of experts 4 l + 4 Lanes q + c.  A round
+// takes the largest score, then the lowest expert that has it.  Scores with a bias are compared in 64 bits: they are worked
+// out in 32, whose error is below 2^-22 of (1 + |score|), and where more than one lies within 2^-20 of that of the largest, these are
+// worked out again.  `marks`, where there is one, gets the token's bit for each expert chosen.
+template <typename T, int Lanes, int Quads, bool Biased>
+__device__ inline void choose(const RouteArgs& a, uint32_t t, uint32_t* marks, uint32_t words, uint32_t bit) {
+  constexpr int kHeld = 4 * Quads, kSlots = Lanes >= 32 ? 1 : 2;
+  const uint32_t lane = threadIdx.x % Lanes;
   const T* row = static_cast<const T*>(a.logits) + t * a.stride;
-  constexpr float kLow = -__builtin_huge_valf();
-  float x[Per];
-  double score[Per];
-  float top = kLow;
+  float x[kHeld], s[kHeld];
+  float top = kNever;
 #pragma unroll
-  for (int i = 0; i < Per; ++i) {
-    const uint32_t e = lane + 64u * i;
-    x[i] = e < a.n_experts ? (float)row[e] : kLow;
-    if (x[i] != x[i]) x[i] = kLow;
-    x[i] = fminf(x[i], 3.40282347e38f);
-    score[i] = (double)x[i];
-    if constexpr (Biased) {
-      if (x[i] > kLow) {
-        score[i] = score64(x[i], a.bias[e]);
-        if (!(score[i] > (double)kLow)) x[i] = kLow;
-      }
-      if (x[i] == kLow) score[i] = (double)kLow;
+  for (int q = 0; q < Quads; ++q) {
+    const uint32_t e = 4u * lane + 4u * Lanes * q;
+    if (e + 4u <= a.n_experts) {
+      const Four<T> f = *reinterpret_cast<const Four<T>*>(row + e);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) x[4 * q + c] = (float)f.v[c];
+    } else {
+#pragma unroll
+      for (int c = 0; c < 4; ++c) x[4 * q + c] = e + (uint32_t)c < a.n_experts ? (float)row[e + c] : kNever;
     }
-    top = fmaxf(top, x[i]);
   }
-  float total = 1.0f;
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    x[i] = fminf(x[i] != x[i] ? kNever : x[i], 3.40282347e38f);
+    s[i] = x[i];
+    if constexpr (Biased) {
+      const uint32_t e = 4u * lane + 4u * Lanes * (i / 4) + i % 4;
+      s[i] = x[i] > kNever ? sigmoid(x[i]) + a.bias[e < a.n_experts ? e : 0u] : kNever;
+      if (s[i] != s[i]) s[i] = kNever;
+    }
+  }
+  float sum = 1.0f;
   if (!a.sigmoid) {
 #pragma unroll
-    for (int d = 32; d > 0; d /= 2) top = fmaxf(top, __shfl_xor(top, d));
-    total = 0.0f;
+    for (int i = 0; i < kHeld; ++i) top = fmaxf(top, x[i]);
+    top = largest<Lanes>(top);
+    if (!a.renorm) {  // (where the chosen are divided by their sum, that of all is no part of it)
+      sum = 0.0f;
 #pragma unroll
-    for (int i = 0; i < Per; ++i) total += x[i] > kLow ? expf(x[i] - top) : 0.0f;
-#pragma unroll
-    for (int d = 32; d > 0; d /= 2) total += __shfl_xor(total, d);
+      for (int i = 0; i < kHeld; ++i) sum += x[i] > kNever ? exp_below(x[i] - top) : 0.0f;
+      sum = in_all<Lanes>(sum);
+    }
   }
-  float chosen = 0.0f, mine = 0.0f;
-  int32_t which = -1;
+  float mine[kSlots];
+  int32_t which[kSlots];
+#pragma unroll
+  for (int h = 0; h < kSlots; ++h) {
+    mine[h] = kNever;
+    which[h] = -1;
+  }
   for (uint32_t j = 0; j < a.k; ++j) {
-    double best = (double)kLow;
-    uint32_t at = 0xffffffffu;
+    float m = s[0];
 #pragma unroll
-    for (int i = 0; i < Per; ++i) {
-      if (score[i] > best) {
-        best = score[i];
-        at = lane + 64u * i;
+    for (int i = 1; i < kHeld; ++i) m = fmaxf(m, s[i]);
+    m = largest<Lanes>(m);
+    const float least = Biased ? m - 0x1p-20f * (1.0f + fabsf(m)) : m;
+    uint32_t at = 0xffffffffu, near = 0u;
+#pragma unroll
+    for (int i = kHeld - 1; i >= 0; --i) {
+      const bool is = s[i] >= least;
+      at = is ? 4u * lane + 4u * Lanes * (i / 4) + i % 4 : at;
+      near += is ? 1u : 0u;
+    }
+    at = lowest<Lanes>(at);
+    const bool none = m == kNever;
+    if constexpr (Biased) {
+      near = none ? 0u : in_all<Lanes>(near);
+      if (__ballot(near > 1u)) {
+        double best = (double)kNever;
+        uint32_t best_at = 0xffffffffu;
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+          const uint32_t e = 4u * lane + 4u * Lanes * (i / 4) + i % 4;
+          if (near > 1u && s[i] >= least) {
+            const double d = score64(x[i], a.bias[e]);
+            if (d > best) {
+              best = d;
+              best_at = e;
+            }
+          }
+        }
+#pragma unroll
+        for (int d = Lanes / 2; d > 0; d /= 2) {
+          const double o = __shfl_xor(best, d);
+          const uint32_t oa = (uint32_t)__shfl_xor((int)best_at, d);
+          if (o > best || (o == best && oa < best_at)) {
+            best = o;
+            best_at = oa;
+          }
+        }
+        if (near > 1u) at = best_at;
       }
     }
+    if (none) at = 0xffffffffu;
+    float logit = Biased ? kNever : m;
 #pragma unroll
-    for (int d = 32; d > 0; d /= 2) {
-      const double o = __shfl_xor(best, d);
-      const uint32_t oa = (uint32_t)__shfl_xor((int)at, d);
-      if (o > best || (o == best && oa < at)) {
-        best = o;
-        at = oa;
-      }
+    for (int i = 0; i < kHeld; ++i) {
+      const bool is = at == 4u * lane + 4u * Lanes * (i / 4) + i % 4;
+      if constexpr (Biased) logit = is ? x[i] : logit;
+      s[i] = is ? kNever : s[i];
     }
-    if (at == 0xffffffffu) break;  // the same for every lane
-    float p = 0.0f;
+    if constexpr (Biased) logit = largest<Lanes>(logit);
 #pragma unroll
-    for (int i = 0; i < Per; ++i) {
-      if (at == lane + 64u * i) {
-        p = a.sigmoid ? sigmoid(x[i]) : expf(x[i] - top) / total;
-        score[i] = (double)kLow;
-      }
-    }
-    p = __shfl(p, (int)(at & 63u));
-    chosen += p;
-    if (lane == j) {
-      mine = p;
-      which = (int32_t)at;
+    for (int h = 0; h < kSlots; ++h) {
+      const bool is = j == lane + (uint32_t)(h * Lanes);
+      mine[h] = is ? logit : mine[h];
+      which[h] = is ? (int32_t)at : which[h];
     }
   }
-  if (lane < a.k) {
-    const float by = a.renorm ? chosen > 0.0f ? mine / chosen : 0.0f : mine;
-    a.expert[(uint64_t)t * a.k + lane] = which;
-    a.weight[(uint64_t)t * a.k + lane] = which < 0 ? 0.0f : by * a.scale;
+  float chosen = 0.0f;
+#pragma unroll
+  for (int h = 0; h < kSlots; ++h) {
+    mine[h] = which[h] < 0 ? 0.0f : a.sigmoid ? sigmoid(mine[h]) : exp_below(mine[h] - top);
+    chosen += mine[h];
+  }
+  chosen = in_all<Lanes>(chosen);
+  const float by = a.renorm ? chosen : sum;
+#pragma unroll
+  for (int h = 0; h < kSlots; ++h) {
+    const uint32_t j = lane + (uint32_t)(h * Lanes);
+    if (j >= a.k) continue;
+    a.expert[(uint64_t)t * a.k + j] = which[h];
+    a.weight[(uint64_t)t * a.k + j] = which[h] < 0 || by == 0.0f ? 0.0f : mine[h] / by * a.scale;
+    if (marks && which[h] >= 0) atomicOr(&marks[(uint32_t)which[h] * words + bit / 32u], 1u << (bit & 31u));
   }
 }
 
-template <typename T, int Per, bool Biased> __global__ void __launch_bounds__(256) route_choose_kernel(RouteArgs a) {
-  const uint32_t t = blockIdx.x * 4u + threadIdx.x / 64u;
-  if (t < a.n) choose<T, Per, Biased>(a, t);
-}
+// How many tokens a wave chooses for at once.
+template <int Lanes> constexpr uint32_t kAtOnce = 64 / Lanes;
 
-// Which tokens of the chunk go to each expert, a bit each: an expert is chosen by a token once at most, so a token's rank among its
-// expert's is the number of bits below its own.  bits: [n_experts][words].
-__device__ inline void mark_chosen(const RouteArgs& a, uint32_t first, uint32_t tokens, uint32_t* bits, uint32_t words) {
-  for (uint32_t i = threadIdx.x; i < a.n_experts * words; i += blockDim.x) bits[i] = 0u;
-  __syncthreads();
-  for (uint32_t i = threadIdx.x; i < tokens * a.k; i += blockDim.x) {
-    const int32_t e = a.expert[(uint64_t)first * a.k + i];
-    const uint32_t t = i / a.k;
-    if (e >= 0) atomicOr(&bits[(uint32_t)e * words + t / 32u], 1u << (t & 31u));
-  }
-  lds_atomics_barrier();
-}
-
+// Which tokens go to each expert is a bit each: an expert is chosen by a token once at most, so a token's rank among its
+// expert's is the number of bits below its own.  `experts` holds bits [n_experts][words], first tokens `first` .. `first + tokens`.
 __device__ inline void put_chosen(const RouteArgs& a, uint32_t first, uint32_t tokens, const uint32_t* bits, uint32_t words, const uint32_t* before) {
   for (uint32_t i = threadIdx.x; i < tokens * a.k; i += blockDim.x) {
     const int32_t e = a.expert[(uint64_t)first * a.k + i];
@@ -167,13 +241,16 @@ __device__ inline uint32_t block_before(uint32_t v, uint32_t* meet, uint32_t& al
   return below + upto - v;
 }
 
-// Few tokens: chosen and put in order by one block.  dynamic: bits [n_experts][words], before [n_experts]
-__global__ void __launch_bounds__(1024) route_order_kernel(RouteArgs a) {
+// Few tokens: chosen and put in order by one block.  Shared memory: bits [n_experts][words], then before [n_experts].
+template <typename T, int Lanes, int Quads, bool Biased> __global__ void __launch_bounds__(1024) route_kernel(RouteArgs a) {
   extern __shared__ uint32_t room[];
   __shared__ uint32_t meet[16];
   const uint32_t words = (a.n + 31u) / 32u;
   uint32_t* before = room + a.n_experts * words;
-  mark_chosen(a, 0u, a.n, room, words);
+  for (uint32_t i = threadIdx.x; i < a.n_experts * words; i += 1024u) room[i] = 0u;
+  __syncthreads();
+  for (uint32_t t = threadIdx.x / Lanes; t < a.n; t += 1024u / Lanes) choose<T, Lanes, Quads, Biased>(a, t, room, words, t);
+  lds_atomics_barrier();
   uint32_t mine = 0u, all;
   if (threadIdx.x < a.n_experts) {
     for (uint32_t w = 0; w < words; ++w) mine += (uint32_t)__builtin_popcount(room[threadIdx.x * words + w]);
@@ -189,42 +266,71 @@ __global__ void __launch_bounds__(1024) route_order_kernel(RouteArgs a) {
   for (uint32_t i = all + threadIdx.x; i < a.n * a.k; i += 1024u) a.token[i] = -1;
 }
 
-__global__ void __launch_bounds__(256) route_count_kernel(RouteArgs a) {
-  extern __shared__ uint32_t room[];
-  const uint32_t first = blockIdx.x * kChunk, tokens = min(kChunk, a.n - first), words = kChunk / 32u;
-  mark_chosen(a, first, tokens, room, words);
-  for (uint32_t e = threadIdx.x; e < a.n_experts; e += 256u)
-    a.counts[(uint64_t)blockIdx.x * a.n_experts + e] = (uint32_t)__builtin_popcount(room[e * words]) + (uint32_t)__builtin_popcount(room[e * words + 1u]);
+// A chunk of tokens to a block, and, where an order is asked for, how many of them go to each expert.
+template <typename T, int Lanes, int Quads, bool Biased> __global__ void __launch_bounds__(1024) route_choose_kernel(RouteArgs a) {
+  __shared__ uint32_t marks[2 * MAASO_EXPERT_MAX];
+  const uint32_t first = blockIdx.x * kChunk;
+  if (a.before) {
+    for (uint32_t i = threadIdx.x; i < 2u * a.n_experts; i += 1024u) marks[i] = 0u;
+    __syncthreads();
+  }
+  for (uint32_t t = threadIdx.x / Lanes; t < kChunk && first + t < a.n; t += 1024u / Lanes)
+    choose<T, Lanes, Quads, Biased>(a, first + t, a.before ? marks : nullptr, 2u, t);
+  if (!a.before) return;
+  lds_atomics_barrier();
+  for (uint32_t e = threadIdx.x; e < a.n_experts; e += 1024u)
+    a.before[(uint64_t)blockIdx.x * a.n_experts + e] = (uint32_t)(__builtin_popcount(marks[2u * e]) + __builtin_popcount(marks[2u * e + 1u]));
 }
 
-// One block: the experts' starts, and each chunk's before it.
-__global__ void __launch_bounds__(1024) route_starts_kernel(RouteArgs a) {
-  __shared__ uint32_t meet[16];
-  uint32_t mine = 0u, all;
-  const uint32_t e = threadIdx.x;
-  if (e < a.n_experts) {
-    for (uint32_t c = 0; c < a.chunks; ++c) mine += a.counts[(uint64_t)c * a.n_experts + e];
-  }
-  uint32_t at = block_before(mine, meet, all);
-  if (e < a.n_experts) {
-    a.start[e] = (int32_t)at;
-    for (uint32_t c = 0; c < a.chunks; ++c) {
-      const uint64_t i = (uint64_t)c * a.n_experts + e;
-      const uint32_t n = a.counts[i];
-      a.counts[i] = at;
-      at += n;
+// 16 experts to a block: their tokens before each chunk, and in all.  64 chunks side by side, the next 64 behind them.
+__global__ void __launch_bounds__(1024) route_before_kernel(RouteArgs a) {
+  __shared__ uint32_t sums[64][17];
+  const uint32_t e = blockIdx.x * 16u + threadIdx.x % 16u, c = threadIdx.x / 16u;
+  uint32_t seen = 0u;
+  for (uint32_t base = 0; base < a.chunks; base += 64u) {
+    const bool in = e < a.n_experts && base + c < a.chunks;
+    uint32_t* p = a.before + (uint64_t)(base + c) * a.n_experts + e;
+    const uint32_t mine = in ? *p : 0u;
+    uint32_t upto = mine;  // over the chunks: neighbours are 16 lanes apart in a wave, and 4 rows of `sums` are a wave's
+    uint32_t o = (uint32_t)__shfl_up((int)upto, 16);
+    upto += (threadIdx.x & 63u) >= 16u ? o : 0u;
+    o = (uint32_t)__shfl_up((int)upto, 32);
+    upto += (threadIdx.x & 63u) >= 32u ? o : 0u;
+    sums[c][threadIdx.x % 16u] = upto;
+    __syncthreads();
+    uint32_t below = 0u, all = 0u;
+    for (uint32_t w = 0; w < 16u; ++w) {
+      const uint32_t v = sums[4u * w + 3u][threadIdx.x % 16u];
+      below += w < c / 4u ? v : 0u;
+      all += v;
     }
+    if (in) *p = seen + below + upto - mine;
+    seen += all;
+    __syncthreads();
   }
-  if (e == 0u) a.start[a.n_experts] = (int32_t)all;
+  if (c == 0u && e < a.n_experts) a.total[e] = seen;
 }
 
-__global__ void __launch_bounds__(256) route_place_kernel(RouteArgs a) {
-  extern __shared__ uint32_t room[];
-  const uint32_t first = blockIdx.x * kChunk, tokens = min(kChunk, a.n - first), words = kChunk / 32u;
-  mark_chosen(a, first, tokens, room, words);
-  put_chosen(a, first, tokens, room, words, a.counts + (uint64_t)blockIdx.x * a.n_experts);
-  const uint32_t all = (uint32_t)a.start[a.n_experts];
-  for (uint32_t i = first * a.k + threadIdx.x; i < (first + tokens) * a.k; i += 256u)
+__global__ void __launch_bounds__(1024) route_place_kernel(RouteArgs a) {
+  __shared__ uint32_t marks[2 * MAASO_EXPERT_MAX], before[MAASO_EXPERT_MAX], meet[16];
+  const uint32_t first = blockIdx.x * kChunk, tokens = min(kChunk, a.n - first), e = threadIdx.x;
+  for (uint32_t i = threadIdx.x; i < 2u * a.n_experts; i += 1024u) marks[i] = 0u;
+  uint32_t all;
+  const uint32_t mine = e < a.n_experts ? a.total[e] : 0u, in_chunks = e < a.n_experts ? a.before[(uint64_t)blockIdx.x * a.n_experts + e] : 0u;
+  const uint32_t at = block_before(mine, meet, all);  // (a barrier in it, behind the marks' zeros)
+  if (e < a.n_experts) {
+    before[e] = at + in_chunks;
+    if (blockIdx.x == 0u) a.start[e] = (int32_t)at;
+  }
+  if (blockIdx.x == 0u && e == 0u) a.start[a.n_experts] = (int32_t)all;
+  for (uint32_t i = threadIdx.x; i < tokens * a.k; i += 1024u) {
+    const int32_t x = a.expert[(uint64_t)first * a.k + i];
+    const uint32_t t = i / a.k;
+    if (x >= 0) atomicOr(&marks[(uint32_t)x * 2u + t / 32u], 1u << (t & 31u));
+  }
+  lds_atomics_barrier();
+  put_chosen(a, first, tokens, marks, 2u, before);
+  for (uint32_t i = first * a.k + threadIdx.x; i < (first + tokens) * a.k; i += 1024u)
     if (i >= all) a.token[i] = -1;
 }
 
