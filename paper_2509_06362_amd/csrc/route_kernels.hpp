@@ -72,109 +72,21 @@ __device__ inline double score64(float x, float bias) { return 1.0 / (1.0 + exp(
 template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) Four { T v[4]; };
 
 // The experts of one token, by Lanes lanes that hold 4 Quads scores each; lane l those of experts 4 l + 4 Lanes q + c.  A round
-// takes the largest score, then the lowest expert that has it.  Scores with a bias are compared in 64 bits: they are worked
-// out in 32, whose error is below 2^-22 of (1 + |score|), and where more than one lies within 2^-20 of that of the largest, these are
-// worked out again.  `marks`, where there is one, gets the token's bit for each expert chosen.
-template <typename T, int Lanes, int Quads, bool Biased>
-__device__ inline void choose(const RouteArgs& a, uint32_t t, uint32_t* marks, uint32_t words, uint32_t bit) {
-  constexpr int kHeld = 4 * Quads, kSlots = Lanes >= 32 ? 1 : 2;
-  const uint32_t lane = threadIdx.x % Lanes;
-  const T* row = static_cast<const T*>(a.logits) + t * a.stride;
-  float x[kHeld], s[kHeld];
-  float top = kNever;
-#pragma unroll
-  for (int q = 0; q < Quads; ++q) {
-    const uint32_t e = 4u * lane + 4u * Lanes * q;
-    if (e + 4u <= a.n_experts) {
-      const Four<T> f = *reinterpret_cast<const Four<T>*>(row + e);
-#pragma unroll
-      for (int c = 0; c < 4; ++c) x[4 * q + c] = (float)f.v[c];
-    } else {
-#pragma unroll
-      for (int c = 0; c < 4; ++c) x[4 * q + c] = e + (uint32_t)c < a.n_experts ? (float)row[e + c] : kNever;
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < kHeld; ++i) {
-    x[i] = fminf(x[i] != x[i] ? kNever : x[i], 3.40282347e38f);
-    s[i] = x[i];
-    if constexpr (Biased) {
-      const uint32_t e = 4u * lane + 4u * Lanes * (i / 4) + i % 4;
-      s[i] = x[i] > kNever ? sigmoid(x[i]) + a.bias[e < a.n_experts ? e : 0u] : kNever;
-      if (s[i] != s[i]) s[i] = kNever;
-    }
-  }
-  float sum = 1.0f;
-  if (!a.sigmoid) {
-#pragma unroll
-    for (int i = 0; i < kHeld; ++i) top = fmaxf(top, x[i]);
-    top = largest<Lanes>(top);
-    if (!a.renorm) {  // (where the chosen are divided by their sum, that of all is no part of it)
-      sum = 0.0f;
-#pragma unroll
-      for (int i = 0; i < kHeld; ++i) sum += x[i] > kNever ? exp_below(x[i] - top) : 0.0f;
-      sum = in_all<Lanes>(sum);
-    }
-  }
-  float mine[kSlots];
+// takes the largest score, then the lowest expert that has it.  Scores with a bias are compared in 64 bits: they are worked out in
+// 32, which is wrong by 2^-22 + 2^-24 |score| at most.  Where two that follow each other are within 2^-21 (1 + |score|) of each
+// other, those taken, and as many more as follow so closely, are put in order in 64 bits, a lane to each; where there are more of them
+// than lanes' places, every round is gone through again in 64.
+template <typename T, int Lanes, int Quads, bool Biased> struct Chooser {
+  static constexpr int kHeld = 4 * Quads, kSlots = Lanes >= 32 ? 1 : 2;
+  uint32_t lane;
+  float x[kHeld];
+  float mine[kSlots];      // the logits of choices lane, lane + Lanes
   int32_t which[kSlots];
-#pragma unroll
-  for (int h = 0; h < kSlots; ++h) {
-    mine[h] = kNever;
-    which[h] = -1;
-  }
-  for (uint32_t j = 0; j < a.k; ++j) {
-    float m = s[0];
-#pragma unroll
-    for (int i = 1; i < kHeld; ++i) m = fmaxf(m, s[i]);
-    m = largest<Lanes>(m);
-    const float least = Biased ? m - 0x1p-20f * (1.0f + fabsf(m)) : m;
-    uint32_t at = 0xffffffffu, near = 0u;
-#pragma unroll
-    for (int i = kHeld - 1; i >= 0; --i) {
-      const bool is = s[i] >= least;
-      at = is ? 4u * lane + 4u * Lanes * (i / 4) + i % 4 : at;
-      near += is ? 1u : 0u;
-    }
-    at = lowest<Lanes>(at);
-    const bool none = m == kNever;
-    if constexpr (Biased) {
-      near = none ? 0u : in_all<Lanes>(near);
-      if (__ballot(near > 1u)) {
-        double best = (double)kNever;
-        uint32_t best_at = 0xffffffffu;
-#pragma unroll
-        for (int i = 0; i < kHeld; ++i) {
-          const uint32_t e = 4u * lane + 4u * Lanes * (i / 4) + i % 4;
-          if (near > 1u && s[i] >= least) {
-            const double d = score64(x[i], a.bias[e]);
-            if (d > best) {
-              best = d;
-              best_at = e;
-            }
-          }
-        }
-#pragma unroll
-        for (int d = Lanes / 2; d > 0; d /= 2) {
-          const double o = __shfl_xor(best, d);
-          const uint32_t oa = (uint32_t)__shfl_xor((int)best_at, d);
-          if (o > best || (o == best && oa < best_at)) {
-            best = o;
-            best_at = oa;
-          }
-        }
-        if (near > 1u) at = best_at;
-      }
-    }
-    if (none) at = 0xffffffffu;
-    float logit = Biased ? kNever : m;
-#pragma unroll
-    for (int i = 0; i < kHeld; ++i) {
-      const bool is = at == 4u * lane + 4u * Lanes * (i / 4) + i % 4;
-      if constexpr (Biased) logit = is ? x[i] : logit;
-      s[i] = is ? kNever : s[i];
-    }
-    if constexpr (Biased) logit = largest<Lanes>(logit);
+  uint32_t rank[kSlots];   // where they stand
+
+  __device__ inline uint32_t expert(int i) const { return 4u * lane + 4u * Lanes * (uint32_t)(i / 4) + (uint32_t)(i % 4); }
+
+  __device__ inline void keep(uint32_t j, uint32_t at, float logit) {
 #pragma unroll
     for (int h = 0; h < kSlots; ++h) {
       const bool is = j == lane + (uint32_t)(h * Lanes);
@@ -182,26 +94,180 @@ __device__ inline void choose(const RouteArgs& a, uint32_t t, uint32_t* marks, u
       which[h] = is ? (int32_t)at : which[h];
     }
   }
+
+  // The rounds by scores s.  With a bias: true where all of them would have to be in 64 bits.
+  __device__ inline bool rounds(uint32_t k, const float* bias, float (&s)[kHeld]) {
+    bool near = false, full = false;
+    float before = __builtin_huge_valf();
+    uint32_t j = 0;
+    for (; Biased || j < k; ++j) {
+      float m = s[0];
+#pragma unroll
+      for (int i = 1; i < kHeld; ++i) m = fmaxf(m, s[i]);
+      m = largest<Lanes>(m);
+      if constexpr (Biased) {
+        const bool follows = m > kNever && before - m <= 0x1p-21f * (1.0f + fabsf(m));
+        near = near || (follows && j <= k);
+        if (j >= k && !__ballot(follows)) break;
+        full = j == (uint32_t)(Lanes * kSlots);
+        if (full) break;
+        before = m;
+      }
+      uint32_t at = 0xffffffffu;
+#pragma unroll
+      for (int i = kHeld - 1; i >= 0; --i) at = s[i] == m ? expert(i) : at;
+      at = lowest<Lanes>(at);
+      if (m == kNever) at = 0xffffffffu;
+      float logit = Biased ? kNever : m;
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i) {
+        const bool is = at == expert(i);
+        if constexpr (Biased) logit = is ? x[i] : logit;
+        s[i] = is ? kNever : s[i];
+      }
+      if constexpr (Biased) logit = largest<Lanes>(logit);
+      keep(j, at, logit);
+    }
+    if constexpr (!Biased) return false;
+    if (!__ballot(near)) return false;
+    if (full) return near;
+    double d[kSlots];
+#pragma unroll
+    for (int h = 0; h < kSlots; ++h) {
+      d[h] = which[h] < 0 ? (double)kNever : score64(mine[h], bias[which[h]]);
+      rank[h] = which[h] < 0 ? rank[h] : 0u;
+    }
+#pragma unroll
+    for (int h = 0; h < kSlots; ++h) {
+      for (uint32_t l = 0; l < (uint32_t)Lanes && l + (uint32_t)(h * Lanes) < j; ++l) {
+        const double o = __shfl(d[h], (int)l, Lanes);
+        const int32_t ow = __shfl(which[h], (int)l, Lanes);
+#pragma unroll
+        for (int g = 0; g < kSlots; ++g) rank[g] += which[g] >= 0 && ow >= 0 && (o > d[g] || (o == d[g] && ow < which[g])) ? 1u : 0u;
+      }
+    }
+    return false;
+  }
+
+  __device__ inline void rounds64(uint32_t k, const float* bias, const float (&s)[kHeld], bool again) {
+    double d[kHeld];
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) d[i] = s[i] > kNever ? score64(x[i], bias[expert(i)]) : (double)kNever;
+    for (uint32_t j = 0; j < k; ++j) {
+      double best = (double)kNever;
+      uint32_t at = 0xffffffffu;
+      float logit = kNever;
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i) {
+        if (d[i] > best) {
+          best = d[i];
+          at = expert(i);
+          logit = x[i];
+        }
+      }
+#pragma unroll
+      for (int l = Lanes / 2; l > 0; l /= 2) {
+        const double o = __shfl_xor(best, l);
+        const uint32_t oa = (uint32_t)__shfl_xor((int)at, l);
+        const float ol = __shfl_xor(logit, l);
+        if (o > best || (o == best && oa < at)) {
+          best = o;
+          at = oa;
+          logit = ol;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i) d[i] = at == expert(i) ? (double)kNever : d[i];
+      if (again) keep(j, at, logit);
+    }
+  }
+};
+
+// One token's experts and their weights; `marks`, where there is one, gets the token's bit for each expert chosen.
+template <typename T, int Lanes, int Quads, bool Biased>
+__device__ inline void choose(const RouteArgs& a, uint32_t t, uint32_t* marks, uint32_t words, uint32_t bit) {
+  using C = Chooser<T, Lanes, Quads, Biased>;
+  constexpr int kHeld = C::kHeld, kSlots = C::kSlots;
+  C c;
+  c.lane = threadIdx.x % Lanes;
+  const T* row = static_cast<const T*>(a.logits) + t * a.stride;
+  float s[kHeld];
+#pragma unroll
+  for (int q = 0; q < Quads; ++q) {
+    const uint32_t e = c.expert(4 * q);
+    if (e + 4u <= a.n_experts) {
+      const Four<T> f = *reinterpret_cast<const Four<T>*>(row + e);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) c.x[4 * q + i] = (float)f.v[i];
+      if constexpr (Biased) {
+        const Four<float> b = *reinterpret_cast<const Four<float>*>(a.bias + e);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[4 * q + i] = b.v[i];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const bool in = e + (uint32_t)i < a.n_experts;
+        c.x[4 * q + i] = in ? (float)row[e + i] : kNever;
+        if constexpr (Biased) s[4 * q + i] = in ? a.bias[e + i] : 0.0f;
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    float& x = c.x[i];
+    x = fminf(x != x ? kNever : x, 3.40282347e38f);
+    if constexpr (Biased) {
+      const float both = sigmoid(x) + s[i];
+      s[i] = x > kNever && both == both ? both : kNever;
+    } else {
+      s[i] = x;
+    }
+  }
+  float sum = 1.0f, top = kNever;
+  if (!a.sigmoid) {
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) top = fmaxf(top, c.x[i]);
+    top = largest<Lanes>(top);
+    if (!a.renorm) {  // (where the chosen are divided by their sum, that of all is no part of it)
+      sum = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i) sum += c.x[i] > kNever ? exp_below(c.x[i] - top) : 0.0f;
+      sum = in_all<Lanes>(sum);
+    }
+  }
+#pragma unroll
+  for (int h = 0; h < kSlots; ++h) {
+    c.mine[h] = kNever;
+    c.which[h] = -1;
+    c.rank[h] = c.lane + (uint32_t)(h * Lanes);
+  }
+  if constexpr (Biased) {
+    float once[kHeld];
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) once[i] = s[i];
+    const bool again = c.rounds(a.k, a.bias, once);
+    if (__ballot(again)) c.rounds64(a.k, a.bias, s, again);
+  } else {
+    c.rounds(a.k, nullptr, s);
+  }
   float chosen = 0.0f;
 #pragma unroll
   for (int h = 0; h < kSlots; ++h) {
-    mine[h] = which[h] < 0 ? 0.0f : a.sigmoid ? sigmoid(mine[h]) : exp_below(mine[h] - top);
-    chosen += mine[h];
+    c.mine[h] = c.which[h] < 0 || c.rank[h] >= a.k ? 0.0f : a.sigmoid ? sigmoid(c.mine[h]) : exp_below(c.mine[h] - top);
+    chosen += c.mine[h];
   }
   chosen = in_all<Lanes>(chosen);
   const float by = a.renorm ? chosen : sum;
 #pragma unroll
   for (int h = 0; h < kSlots; ++h) {
-    const uint32_t j = lane + (uint32_t)(h * Lanes);
+    const uint32_t j = c.rank[h];
     if (j >= a.k) continue;
-    a.expert[(uint64_t)t * a.k + j] = which[h];
-    a.weight[(uint64_t)t * a.k + j] = which[h] < 0 || by == 0.0f ? 0.0f : mine[h] / by * a.scale;
-    if (marks && which[h] >= 0) atomicOr(&marks[(uint32_t)which[h] * words + bit / 32u], 1u << (bit & 31u));
+    a.expert[(uint64_t)t * a.k + j] = c.which[h];
+    a.weight[(uint64_t)t * a.k + j] = c.which[h] < 0 || by == 0.0f ? 0.0f : c.mine[h] / by * a.scale;
+    if (marks && c.which[h] >= 0) atomicOr(&marks[(uint32_t)c.which[h] * words + bit / 32u], 1u << (bit & 31u));
   }
 }
-
-// How many tokens a wave chooses for at once.
-template <int Lanes> constexpr uint32_t kAtOnce = 64 / Lanes;
 
 // Which tokens go to each expert is a bit each: an expert is chosen by a token once at most, so a token's rank among its
 // expert's is the number of bits below its own.  `experts` holds bits [n_experts][words], first tokens `first` .. `first + tokens`.
