@@ -64,33 +64,68 @@ uint64_t most_tiles(const ProductArgs& a, uint32_t rows) {
   return a.start ? a.n_rows / rows + std::min(a.n_experts, a.n_rows) : (a.n_rows + rows - 1u) / rows;
 }
 
-template <typename T, int MT, int NT, bool Gated>
+template <typename T, bool Gated>
 int launch_stream(ProductArgs& a, hipStream_t s) {
-  const uint32_t cols = 16u * (Gated ? NT / 2 : NT);
-  const uint64_t down = most_tiles(a, 16u * MT);
+  const uint64_t down = most_tiles(a, 16u);
   if (down > 65535u) return MAASO_E_SHAPE;
-  hipLaunchKernelGGL((product_stream_kernel<T, MT, NT, Gated, 4>), dim3((a.n_out + cols - 1u) / cols, (uint32_t)down), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((product_stream_kernel<T, Gated, 4>), dim3((a.n_out + 15u) / 16u, (uint32_t)down), dim3(256), 0, s, a);
   return launched();
 }
 
-template <typename T, int WM, int WN, int MI, int NI, bool Gated>
+template <typename T, int WM, int WN, int MI, int NI, int Stages, bool Gated>
 int launch_tiles(ProductArgs& a, hipStream_t s) {
   const uint32_t cols = WN * NI * 16u / (Gated ? 2u : 1u);
   a.col_tiles = (a.n_out + cols - 1u) / cols;
-  const uint64_t blocks = (most_tiles(a, WM * MI * 16u) * a.col_tiles + 7u) / 8u * 8u;
-  if (blocks > 0x7fffffffull) return MAASO_E_SHAPE;
-  hipLaunchKernelGGL((product_tile_kernel<T, WM, WN, MI, NI, Gated>), dim3((uint32_t)blocks), dim3(64 * WM * WN), 0, s, a);
+  const uint64_t most = (most_tiles(a, WM * MI * 16u) * a.col_tiles + 7u) / 8u * 8u;
+  if (most > 0x7fffffffull) return MAASO_E_SHAPE;
+  hipLaunchKernelGGL((product_tile_kernel<T, WM, WN, MI, NI, Stages, Gated>), dim3((uint32_t)most), dim3(64 * WM * WN), 0, s, a);
   return launched();
 }
 
+// Which tiles.  What a form takes is its rounds (tiles over the tiles that the card has places for) by what a round takes: us to begin and to
+// end it, and us for each step of 128 bytes.  Ragged groups end in a tile of which half is empty, on the average.
+struct Form {
+  uint32_t rows, cols, places;  // of a tile; tiles of a compute unit
+  float round, step;
+};
+// As measured, 8 bits, 2048 bytes to sum over, 4096 channels, us of 64 x 64, 128 x 128 in four stages (a place to a unit) and in two (two places),
+// 256 x 256: 128 rows 7.9, 14.5, 16.3, 27.7; 512 rows 10.8, 15.4, 16.8, 29.3; 1024 rows 19.0, 17.0, 18.1, 30.3; 2048 rows 34.5, 30.5, 22.8, 32.5;
+// 4096 rows of 4096 bytes 104, 88, 68, 62.  16 bits, 8 experts, 8192 channels, 4096 bytes: 64 rows each 62.5, 76, 75, 79; 128 rows 87, 79, 75, 86; 256 rows
+// 140, 112, 101, 89; 512 rows 256, 204, 177, 137.
+constexpr Form kForms[] = {{64, 64, 1, 2.5f, 0.37f}, {64, 64, 2, 2.5f, 0.52f}, {128, 128, 1, 3.0f, 0.87f}, {128, 128, 2, 3.0f, 1.24f}, {256, 256, 1, 6.0f, 1.65f}};
+
+uint32_t best_form(const ProductArgs& a, uint32_t n_cu) {
+  const float steps = (float)((a.in_bytes + 127u) / 128u), experts = (float)std::min(a.n_experts, a.n_rows);
+  uint32_t best = 0;
+  float least = 0.0f;
+  for (uint32_t f = 0; f < sizeof(kForms) / sizeof(kForms[0]); ++f) {
+    const Form& form = kForms[f];
+    const float whole = (float)a.n_rows / (float)form.rows, down = a.start ? std::max(whole + 0.5f * experts, experts) : std::ceil(whole);
+    const float rounds = std::ceil(down * (float)((a.channels + form.cols - 1u) / form.cols) / (float)(form.places * n_cu));
+    const float us = rounds * (form.round + steps * form.step);
+    if (f == 0 || us < least) {
+      least = us;
+      best = f;
+    }
+  }
+  return best;
+}
+
+// Few rows go through waves that hold their operands in registers only: up to 16 of one matrix or of an expert where its weights are no more than 32
+// MiB, which many small blocks bring sooner (8 bits, 8 MiB, 16 rows 4.7 us for 7.3 in tiles; 32 MiB 11.4 and 11.3), and up to 4 whatever the weights, for
+// rows beside the last are read again by each block (64 experts of 2.3 MiB, a row each 30.6 us for 35.7, 6 rows 37.8 and 36.3; 8 experts of 32 MiB, 8 rows
+// 63.4 and 58.6).
 template <typename T, bool Gated>
 int launch_product(ProductArgs& a, uint32_t n_cu, hipStream_t s) {
-  const uint64_t rows = (a.n_rows + a.n_experts - 1u) / a.n_experts;  // of an expert, on the average
-  if (rows <= 16u) return launch_stream<T, 1, 2, Gated>(a, s);
-  if (rows <= 64u) return launch_stream<T, 2, 2, Gated>(a, s);
-  const uint64_t large = most_tiles(a, 256u) * ((a.channels + 255u) / 256u);
-  if (large >= n_cu) return launch_tiles<T, 2, 4, 8, 4, Gated>(a, s);
-  return launch_tiles<T, 2, 2, 4, 4, Gated>(a, s);
+  const uint64_t rows = (a.n_rows + a.n_experts - 1u) / a.n_experts, weights = (uint64_t)a.n_experts * a.channels * a.in_bytes;
+  if (rows <= 4u || (rows <= 16u && weights <= (32u << 20))) return launch_stream<T, Gated>(a, s);
+  switch (best_form(a, n_cu)) {
+    case 0:
+    case 1: return launch_tiles<T, 2, 2, 2, 2, 4, Gated>(a, s);
+    case 2: return launch_tiles<T, 2, 2, 4, 4, 4, Gated>(a, s);
+    case 3: return launch_tiles<T, 2, 2, 4, 4, 2, Gated>(a, s);
+    default: return launch_tiles<T, 2, 4, 8, 4, 2, Gated>(a, s);
+  }
 }
 
 template <typename T>

@@ -158,30 +158,48 @@ __device__ inline u32x4 row_bytes(const char* row, uint32_t at, uint32_t in_byte
   return first_bytes(v, (int)in_bytes - (int)at);
 }
 
-// N neighbouring channels of one row: scales, bias, gate, the one rounding.
+// N neighbouring numbers that begin anywhere.
+template <int N> struct __attribute__((packed, aligned(4))) Floats { float v[N]; };
+
+// What N neighbouring channels of an expert, from `col` on, are scaled by and raised by, gate and gated.
+template <typename T, int N, bool Gated> struct Channels {
+  static constexpr int kBoth = Gated ? 2 : 1;
+  static constexpr bool kScaled = sizeof(T) == 1;
+  float scale[kBoth][N], bias[kBoth][N];
+  __device__ inline void take(const float* from, uint64_t at, uint32_t left, float none, float (&to)[N]) {
+    if (!from) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) to[k] = none;
+    } else if (left >= (uint32_t)N) {
+      const Floats<N> f = *reinterpret_cast<const Floats<N>*>(from + at);
+#pragma unroll
+      for (int k = 0; k < N; ++k) to[k] = f.v[k];
+    } else {
+#pragma unroll
+      for (int k = 0; k < N; ++k) to[k] = (uint32_t)k < left ? from[at + k] : none;
+    }
+  }
+  __device__ inline void load(const ProductArgs& a, uint32_t expert, uint32_t col) {
+    const uint64_t at = (uint64_t)expert * a.channels + col;
+#pragma unroll
+    for (int h = 0; h < kBoth; ++h) {
+      if constexpr (kScaled) take(a.w_scale, at + (uint64_t)h * a.n_out, a.n_out - col, 1.0f, scale[h]);
+      take(a.bias, at + (uint64_t)h * a.n_out, a.n_out - col, 0.0f, bias[h]);
+    }
+  }
+};
+
+// N neighbouring channels of one row: scales, bias, gate, the one rounding.  (Adding the bias that is not there changes no number but -0.)
 template <typename T, int N, bool Gated>
-__device__ inline void finish(const ProductArgs& a, uint32_t expert, uint32_t row, uint32_t source, uint32_t col, float (&y)[N], float (&up)[N]) {
-  const uint64_t at = (uint64_t)expert * a.channels + col;
-  if constexpr (sizeof(T) == 1) {
-    const float s = a.a_scale ? a.a_scale[source] : 1.0f;
+__device__ inline void finish(const ProductArgs& a, const Channels<T, N, Gated>& c, uint32_t row, float row_scale, uint32_t col, float (&y)[N], float (&up)[N]) {
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
-      if (col + (uint32_t)k >= a.n_out) break;
-      y[k] = y[k] * s * (a.w_scale ? a.w_scale[at + k] : 1.0f);
-      if constexpr (Gated) up[k] = up[k] * s * (a.w_scale ? a.w_scale[at + a.n_out + k] : 1.0f);
+  for (int k = 0; k < N; ++k) {
+    if constexpr (sizeof(T) == 1) y[k] = y[k] * row_scale * c.scale[0][k];
+    y[k] += c.bias[0][k];
+    if constexpr (Gated) {
+      if constexpr (sizeof(T) == 1) up[k] = up[k] * row_scale * c.scale[Gated][k];
+      y[k] = silu(y[k]) * (up[k] + c.bias[Gated][k]);
     }
-  }
-  if (a.bias) {
-#pragma unroll
-    for (int k = 0; k < N; ++k) {
-      if (col + (uint32_t)k >= a.n_out) break;
-      y[k] += a.bias[at + k];
-      if constexpr (Gated) up[k] += a.bias[at + a.n_out + k];
-    }
-  }
-  if constexpr (Gated) {
-#pragma unroll
-    for (int k = 0; k < N; ++k) y[k] = silu(y[k]) * up[k];
   }
   const uint64_t to = (uint64_t)row * a.out_stride + col;
   const bool whole = a.wide && col + (uint32_t)N <= a.n_out;
@@ -207,13 +225,8 @@ __device__ inline void finish(const ProductArgs& a, uint32_t expert, uint32_t ro
   }
   uint16_t* p = static_cast<uint16_t*>(a.out) + to;
   if (whole) {
-    if constexpr (N % 8 == 0) {
-#pragma unroll
-      for (int k = 0; k < N / 2; k += 4) *reinterpret_cast<u32x4*>(p + 2 * k) = (u32x4){pair[k], pair[k + 1], pair[k + 2], pair[k + 3]};
-    } else {
-#pragma unroll
-      for (int k = 0; k < N / 2; k += 2) *reinterpret_cast<u32x2*>(p + 2 * k) = (u32x2){pair[k], pair[k + 1]};
-    }
+    if constexpr (N == 8) *reinterpret_cast<u32x4*>(p) = (u32x4){pair[0], pair[1], pair[2], pair[3]};
+    else *reinterpret_cast<u32x2*>(p) = (u32x2){pair[0], pair[1]};
   } else {
 #pragma unroll
     for (int k = 0; k < N; ++k)
@@ -222,119 +235,119 @@ __device__ inline void finish(const ProductArgs& a, uint32_t expert, uint32_t ro
 }
 
 // Few rows: the weights are read once, straight into registers, and what bounds it is that reading.  A block is 16 rows by
-// MT and 16 channels by NT (gated: NT / 2 of the gate and as many beside them); its waves share what is summed over, 128
-// bytes of a row in turn, and their sums meet in shared memory, in the order of the waves.
-template <typename T, int MT, int NT, bool Gated, int Waves>
+// 16 channels, those that gate them beside them; its waves share what is summed over, 128 bytes of a row in turn, and their sums meet in
+// shared memory, in the order of the waves.
+template <typename T, bool Gated, int Waves>
 __global__ void __launch_bounds__(64 * Waves) product_stream_kernel(ProductArgs a) {
   using Sum = typename Operand<T>::Sum;
-  constexpr int kAhead = 4;  // 128-byte steps whose loads are under way at once
-  constexpr int kTiles = Gated ? NT / 2 : NT;
-  static_assert(!Gated || NT % 2 == 0, "a gate's channels lie in one wave with those that it gates");
-  __shared__ Sum sums[Waves][MT * NT][64];
+  constexpr int kAhead = 4, kTiles = Gated ? 2 : 1;  // 128-byte steps whose loads are under way at once
+  __shared__ Sum sums[Waves][kTiles][64];
   const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x / 64u, i = lane & 15u, g = lane / 16u;
   if (blockIdx.x == 0u && blockIdx.y == 0u && wave == 0u) check_starts(a);
-  const RowTile t = row_tile<16 * MT>(a, blockIdx.y);
+  const RowTile t = row_tile<16>(a, blockIdx.y);
   if (t.rows == 0u) return;
-  const uint32_t n0 = blockIdx.x * (16u * kTiles);
-  const char* weights = a.w + t.expert * a.expert_stride;
-  const char* wp[NT];
-  const char* ap[MT];
+  const uint32_t n0 = blockIdx.x * 16u;
+  bool ok;
+  const uint32_t source = source_row(a, t.begin + (i < t.rows ? i : 0u), ok);
+  const char* ap = a.a + source * a.a_stride;
+  const char* wp[kTiles];
 #pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    const uint32_t c = min(n0 + (Gated ? n / 2 : n) * 16u + i, a.n_out - 1u) + (Gated && n % 2 ? a.n_out : 0u);
-    wp[n] = weights + c * a.w_stride;
-  }
-#pragma unroll
-  for (int m = 0; m < MT; ++m) {
-    const uint32_t r = m * 16u + i;
-    bool ok;
-    ap[m] = a.a + source_row(a, t.begin + (r < t.rows ? r : 0u), ok) * a.a_stride;
-  }
-  Sum sum[MT][NT] = {};
+  for (int n = 0; n < kTiles; ++n) wp[n] = a.w + t.expert * a.expert_stride + (min(n0 + i, a.n_out - 1u) + n * a.n_out) * a.w_stride;
+  Sum sum[kTiles] = {};
   const uint32_t whole = a.in_bytes / 128u, steps = (a.in_bytes + 127u) / 128u;
   uint32_t at = wave;
+  u32x4 wv[kAhead][kTiles][2], av[kAhead][2];
+  auto multiply = [&]() {
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int n = 0; n < kTiles; ++n) sum[n] = Operand<T>::mfma(wv[u][n][h], av[u][h], sum[n]);
+  };
   for (; at + (kAhead - 1) * Waves < whole; at += kAhead * Waves) {
-    u32x4 wv[kAhead][NT][2], av[kAhead][MT][2];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const uint32_t byte = (at + u * Waves) * 128u + g * 32u + h * 16u;
 #pragma unroll
-        for (int n = 0; n < NT; ++n) wv[u][n][h] = *reinterpret_cast<const u32x4*>(wp[n] + byte);
-#pragma unroll
-        for (int m = 0; m < MT; ++m) av[u][m][h] = *reinterpret_cast<const u32x4*>(ap[m] + byte);
+        for (int n = 0; n < kTiles; ++n) wv[u][n][h] = *reinterpret_cast<const u32x4*>(wp[n] + byte);
+        av[u][h] = *reinterpret_cast<const u32x4*>(ap + byte);
       }
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u)
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-          for (int n = 0; n < NT; ++n) sum[m][n] = Operand<T>::mfma(wv[u][n][h], av[u][m][h], sum[m][n]);
+    multiply();
   }
   if (at < steps) {  // what is left, all of it under way at once; bytes from the rows' end on are zeros in both
-    u32x4 wv[kAhead][NT][2], av[kAhead][MT][2];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const uint32_t byte = (at + u * Waves) * 128u + g * 32u + h * 16u;
 #pragma unroll
-        for (int n = 0; n < NT; ++n) wv[u][n][h] = row_bytes(wp[n], byte, a.in_bytes);
-#pragma unroll
-        for (int m = 0; m < MT; ++m) av[u][m][h] = row_bytes(ap[m], byte, a.in_bytes);
+        for (int n = 0; n < kTiles; ++n) wv[u][n][h] = row_bytes(wp[n], byte, a.in_bytes);
+        av[u][h] = row_bytes(ap, byte, a.in_bytes);
       }
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u)
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-          for (int n = 0; n < NT; ++n) sum[m][n] = Operand<T>::mfma(wv[u][n][h], av[u][m][h], sum[m][n]);
+    multiply();
   }
 #pragma unroll
-  for (int m = 0; m < MT; ++m)
-#pragma unroll
-    for (int n = 0; n < NT; ++n) sums[wave][m * NT + n][lane] = sum[m][n];
+  for (int n = 0; n < kTiles; ++n) sums[wave][n][lane] = sum[n];
   __syncthreads();
-  for (uint32_t u = wave; u < (uint32_t)(MT * kTiles); u += Waves) {
-    const uint32_t m = u / kTiles, n = u % kTiles, first = m * NT + (Gated ? 2u * n : n);
-    Sum y = sums[0][first][lane], up = y;
+  if (wave != 0u) return;
+  Sum y[kTiles];
 #pragma unroll
-    for (int w = 1; w < Waves; ++w) y += sums[w][first][lane];
-    if constexpr (Gated) {
-      up = sums[0][first + 1u][lane];
+  for (int n = 0; n < kTiles; ++n) {
+    y[n] = sums[0][n][lane];
 #pragma unroll
-      for (int w = 1; w < Waves; ++w) up += sums[w][first + 1u][lane];
-    }
-    const uint32_t r = m * 16u + i, col = n0 + n * 16u + g * 4u;
-    if (r >= t.rows || col >= a.n_out) continue;
-    bool ok;
-    const uint32_t source = source_row(a, t.begin + r, ok);
-    if (!ok) {
-      atomicOr(a.status, MAASO_INST_BAD_ROW);
-      continue;
-    }
-    float yf[4] = {(float)y[0], (float)y[1], (float)y[2], (float)y[3]}, uf[4] = {(float)up[0], (float)up[1], (float)up[2], (float)up[3]};
-    finish<T, 4, Gated>(a, t.expert, t.begin + r, source, col, yf, uf);
+    for (int w = 1; w < Waves; ++w) y[n] += sums[w][n][lane];
+  }
+  const uint32_t col = n0 + g * 4u;
+  if (i >= t.rows || col >= a.n_out) return;
+  if (!ok) {
+    atomicOr(a.status, MAASO_INST_BAD_ROW);
+    return;
+  }
+  float yf[4], uf[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    yf[k] = (float)y[0][k];
+    uf[k] = Gated ? (float)y[kTiles - 1][k] : 0.0f;
+  }
+  Channels<T, 4, Gated> c;
+  c.load(a, t.expert, col);
+  finish<T, 4, Gated>(a, c, t.begin + i, a.a_scale ? a.a_scale[source] : 1.0f, col, yf, uf);
+}
+
+// Waits until no more than N of this wave's loads to shared memory are under way, its other accesses to shared memory are done, and all
+// waves have come here.
+template <uint32_t N> __device__ inline void meet() {
+  static_assert(N < 64u, "the counter has six bits");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+// ... of the steps of Loads loads that are under way, no more than `steps`, at most Most.
+template <uint32_t Loads, uint32_t Most> __device__ inline void meet_behind(uint32_t steps) {
+  if constexpr (Most == 0u) {
+    meet<0>();
+  } else {
+    if (steps >= Most) meet<Most * Loads>();
+    else meet_behind<Loads, Most - 1u>(steps);
   }
 }
 
-// Many rows: a block is BM rows by BN channels, steps of 128 bytes of both come to shared memory asynchronously, into one of
-// two places while the step in the other is multiplied.  A row's eight pieces of 16 bytes lie crossed with the row's lowest three bits, so that
-// reads of one piece of neighbouring rows meet different banks.
-template <typename T, int WM, int WN, int MI, int NI, bool Gated>
-__global__ void __launch_bounds__(64 * WM * WN) product_tile_kernel(ProductArgs a) {
+// More rows: a block is kRows rows by kCols channels, a wave MI by NI times 16 of each.  Steps of 128 bytes of both come to shared
+// memory asynchronously, Stages of them under way or in use.  A step is two halves: while one is multiplied the operands of the next
+// are read, and the waves meet between the halves, where their operands lie in registers already; there a step's place becomes free for the step
+// Stages later.  A row's eight pieces of 16 bytes lie crossed with the row's lowest three bits, so that reads of one piece of neighbouring
+// rows meet different banks.
+template <typename T, int WM, int WN, int MI, int NI, int Stages, bool Gated>
+__global__ void __launch_bounds__(64 * WM * WN, Stages * (WM * MI + WN * NI) * 2 <= 80 ? 2 : 1) product_tile_kernel(ProductArgs a) {
   using Sum = typename Operand<T>::Sum;
   constexpr uint32_t kWaves = WM * WN, kRows = WM * MI * 16, kCols = WN * NI * 16, kStage = (kRows + kCols) * 128;
-  constexpr uint32_t kALoads = kRows / 8 / kWaves, kBLoads = kCols / 8 / kWaves;
+  constexpr uint32_t kALoads = kRows / 8 / kWaves, kBLoads = kCols / 8 / kWaves, kLoads = kALoads + kBLoads;
   constexpr int H = Gated ? NI / 2 : NI;  // channel tiles of a wave's outputs
-  constexpr uint32_t kOut = WN * H * 16, kAcross = 8;
+  constexpr uint32_t kOut = WN * H * 16, kAcross = 8, kTwo = H % 2 ? 1 : 2;
   static_assert(kRows % (8 * kWaves) == 0 && kCols % (8 * kWaves) == 0 && (!Gated || NI % 2 == 0), "whole loads, whole gates");
-  __shared__ __attribute__((aligned(1024))) char lds[2 * kStage];
+  static_assert(Stages >= 2 && (Stages - 1) * kLoads < 64, "loads under way that can be counted");
+  __shared__ __attribute__((aligned(1024))) char lds[Stages * kStage];
   const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x / 64u), i = lane & 15u, g = lane / 16u;
   const uint32_t wm = wave / WN, wn = wave % WN;
   if (blockIdx.x == 0u && wave == 0u) check_starts(a);
@@ -359,94 +372,121 @@ __global__ void __launch_bounds__(64 * WM * WN) product_tile_kernel(ProductArgs 
   if (t.rows == 0u) return;
   const uint32_t n0 = col_tile * kOut;
 
-  const char* ap[kALoads];
-  const char* bp[kBLoads];
+  const char* from[kLoads];  // a's, then w's
   const uint32_t piece = ((lane & 7u) ^ (lane / 8u)) * 16u;
 #pragma unroll
   for (uint32_t q = 0; q < kALoads; ++q) {
     const uint32_t r = (wave * kALoads + q) * 8u + lane / 8u;
     bool ok;
-    ap[q] = a.a + source_row(a, t.begin + (r < t.rows ? r : 0u), ok) * a.a_stride + piece;
+    from[q] = a.a + source_row(a, t.begin + (r < t.rows ? r : 0u), ok) * a.a_stride + piece;
   }
   const char* weights = a.w + t.expert * a.expert_stride;
 #pragma unroll
   for (uint32_t q = 0; q < kBLoads; ++q) {
     // Row p of a wave's channels lies where its sums come out beside their neighbours': a lane of the matrix unit's result has four
-    // rows of each tile, which are to be 4 H channels in a row.
+    // rows of each tile, and those of two tiles are to be eight channels in a row, those of four lanes then 64 bytes of 16-bit outputs.
     const uint32_t b = (wave * kBLoads + q) * 8u + lane / 8u, p = b % (NI * 16u), n = p / 16u, r = p % 16u;
-    const uint32_t c = n0 + b / (NI * 16u) * (H * 16u) + r / 4u * (4u * H) + n % H * 4u + r % 4u;
-    bp[q] = weights + (min(c, a.n_out - 1u) + (Gated && n >= (uint32_t)H ? a.n_out : 0u)) * a.w_stride + piece;
+    const uint32_t c = n0 + b / (NI * 16u) * (H * 16u) + n % H / kTwo * (kTwo * 16u) + r / 4u * (kTwo * 4u) + n % H % kTwo * 4u + r % 4u;
+    from[kALoads + q] = weights + (min(c, a.n_out - 1u) + (Gated && n >= (uint32_t)H ? a.n_out : 0u)) * a.w_stride + piece;
   }
 
   const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
   const uint32_t whole = a.in_bytes / 128u, steps = (a.in_bytes + 127u) / 128u;
-  // (m0 is named as changed, so that none of the compiler's own uses of it, from its setting on, has this between; that it warns of, as of any
-  // reserved register.)
+  // Written out, because the compiler would have every later read of shared memory wait for it.  (m0 is named as changed, so that none of the
+  // compiler's own uses of it, from its setting on, has this between; that it warns of, as of any reserved register.)
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
-  auto async16 = [&](const char* from, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_base + to), "v"(from) : "memory", "m0");
+  auto async16 = [&](const char* p, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_base + to), "v"(p) : "memory", "m0");
   };
 #pragma clang diagnostic pop
-  auto bring = [&](uint32_t step, uint32_t buffer) {
-    const uint32_t to = buffer * kStage, byte = step * 128u;
-    if (step < whole) {
-#pragma unroll
-      for (uint32_t q = 0; q < kALoads; ++q) async16(ap[q] + byte, to + (wave * kALoads + q) * 1024u);
-#pragma unroll
-      for (uint32_t q = 0; q < kBLoads; ++q) async16(bp[q] + byte, to + kRows * 128u + (wave * kBLoads + q) * 1024u);
-    } else {  // the rows' end lies in this step: zeros behind it in both
-#pragma unroll
-      for (uint32_t q = 0; q < kALoads; ++q)
-        *reinterpret_cast<u32x4*>(lds + to + (wave * kALoads + q) * 1024u + lane * 16u) = row_bytes(ap[q] - piece, byte + piece, a.in_bytes);
-#pragma unroll
-      for (uint32_t q = 0; q < kBLoads; ++q)
-        *reinterpret_cast<u32x4*>(lds + to + kRows * 128u + (wave * kBLoads + q) * 1024u + lane * 16u) = row_bytes(bp[q] - piece, byte + piece, a.in_bytes);
-    }
+  auto place_of = [&](uint32_t q) { return q < kALoads ? (wave * kALoads + q) * 1024u : kRows * 128u + (wave * kBLoads + (q - kALoads)) * 1024u; };
+  auto bring = [&](uint32_t step, uint32_t q) { async16(from[q] + step * 128u, step % Stages * kStage + place_of(q)); };
+  auto bring_end = [&](uint32_t step) {  // the rows' end lies in this step: zeros behind it in both
+    for (uint32_t q = 0; q < kLoads; ++q)
+      *reinterpret_cast<u32x4*>(lds + step % Stages * kStage + place_of(q) + lane * 16u) = row_bytes(from[q] - piece, step * 128u + piece, a.in_bytes);
   };
 
+  const uint32_t row_at = (wm * MI * 16u + i) * 128u, col_at = kRows * 128u + (wn * NI * 16u + i) * 128u;
+  const uint32_t half_at[2] = {(g ^ (i & 7u)) * 16u, ((4u + g) ^ (i & 7u)) * 16u};
+  u32x4 av[2][MI], bv[2][NI];
+  auto read = [&](uint32_t step, int half, int k) {  // operand k of both
+    const char* at = lds + step % Stages * kStage + half_at[half];
+    if (k < NI) bv[half][k] = *reinterpret_cast<const u32x4*>(at + col_at + k * 2048);
+    if (k < MI) av[half][k] = *reinterpret_cast<const u32x4*>(at + row_at + k * 2048);
+  };
   Sum sum[MI][NI] = {};
-  bring(0u, 0u);
-  for (uint32_t step = 0; step < steps; ++step) {
-    const uint32_t buffer = step & 1u;
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (step + 1u < steps) bring(step + 1u, buffer ^ 1u);
-    const char* rows = lds + buffer * kStage + (wm * MI * 16u + i) * 128u;
-    const char* cols = lds + buffer * kStage + kRows * 128u + (wn * NI * 16u + i) * 128u;
+  auto multiply = [&](int half, int m) {
 #pragma unroll
-    for (uint32_t ks = 0; ks < 2u; ++ks) {
-      const uint32_t place = ((ks * 4u + g) ^ (i & 7u)) * 16u;
-      u32x4 av[MI], bv[NI];
-#pragma unroll
-      for (int n = 0; n < NI; ++n) bv[n] = *reinterpret_cast<const u32x4*>(cols + n * 2048 + place);
-#pragma unroll
-      for (int m = 0; m < MI; ++m) av[m] = *reinterpret_cast<const u32x4*>(rows + m * 2048 + place);
-#pragma unroll
-      for (int m = 0; m < MI; ++m)
-#pragma unroll
-        for (int n = 0; n < NI; ++n) sum[m][n] = Operand<T>::mfma(bv[n], av[m], sum[m][n]);
-    }
-  }
+    for (int n = 0; n < NI; ++n) sum[m][n] = Operand<T>::mfma(bv[half][n], av[half][m], sum[m][n]);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  constexpr int kReads = MI > NI ? MI : NI;
 
 #pragma unroll
-  for (int m = 0; m < MI; ++m) {
-    const uint32_t r = wm * MI * 16u + m * 16u + i, col = n0 + wn * (H * 16u) + g * (4u * H);
-    if (r >= t.rows || col >= a.n_out) continue;
-    bool ok;
-    const uint32_t source = source_row(a, t.begin + r, ok);
-    if (!ok) {
-      atomicOr(a.status, MAASO_INST_BAD_ROW);
-      continue;
+  for (uint32_t s = 0; s < (uint32_t)Stages; ++s) {
+    if (s < whole) {
+#pragma unroll
+      for (uint32_t q = 0; q < kLoads; ++q) bring(s, q);
+    } else if (s < steps) {
+      bring_end(s);
     }
-    float y[4 * H], up[4 * H];
+  }
+  meet_behind<kLoads, Stages - 1>(steps - 1u);
 #pragma unroll
-    for (int n = 0; n < H; ++n)
+  for (int k = 0; k < kReads; ++k) read(0u, 0, k);
+  for (uint32_t step = 0; step < steps; ++step) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        y[4 * n + k] = (float)sum[m][n][k];
-        up[4 * n + k] = Gated ? (float)sum[m][n + (Gated ? H : 0)][k] : 0.0f;
+    for (int m = 0; m < MI; ++m) {
+#pragma unroll
+      for (int k = m * kReads / MI; k < (m + 1) * kReads / MI; ++k) read(step, 1, k);
+      multiply(0, m);
+    }
+    if (step + 1u < steps) meet_behind<kLoads, Stages - 2>(steps - 2u - step);
+    const uint32_t next = step + Stages;
+    if (next >= whole && next < steps) bring_end(next);
+#pragma unroll
+    for (int m = 0; m < MI; ++m) {
+#pragma unroll
+      for (int k = m * kReads / MI; k < (m + 1) * kReads / MI; ++k) read(step + 1u, 0, k);  // (behind the last step what is read is not used)
+      if (next < whole) {
+#pragma unroll
+        for (uint32_t q = m * kLoads / MI; q < (m + 1) * kLoads / MI; ++q) bring(next, q);
       }
-    finish<T, 4 * H, Gated>(a, t.expert, t.begin + r, source, col, y, up);
+      multiply(1, m);
+    }
+  }
+  bool ok[MI];
+  float row_scale[MI];
+#pragma unroll
+  for (int m = 0; m < MI; ++m) {
+    const uint32_t r = wm * MI * 16u + m * 16u + i;
+    ok[m] = r < t.rows;
+    bool there = true;
+    const uint32_t source = source_row(a, t.begin + (ok[m] ? r : 0u), there);
+    row_scale[m] = sizeof(T) == 1 && a.a_scale ? a.a_scale[source] : 1.0f;
+    if (ok[m] && !there) {
+      ok[m] = false;
+      atomicOr(a.status, MAASO_INST_BAD_ROW);
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < H; n += (int)kTwo) {
+    const uint32_t col = n0 + wn * (H * 16u) + (uint32_t)n * 16u + g * (kTwo * 4u);
+    if (col >= a.n_out) continue;
+    Channels<T, 4 * (int)kTwo, Gated> c;
+    c.load(a, t.expert, col);
+#pragma unroll
+    for (int m = 0; m < MI; ++m) {
+      if (!ok[m]) continue;
+      float y[4 * kTwo], up[4 * kTwo];
+#pragma unroll
+      for (int k = 0; k < 4 * (int)kTwo; ++k) {
+        y[k] = (float)sum[m][n + k / 4][k % 4];
+        up[k] = Gated ? (float)sum[m][n + k / 4 + (Gated ? H : 0)][k % 4] : 0.0f;
+      }
+      finish<T, 4 * (int)kTwo, Gated>(a, c, t.begin + wm * MI * 16u + m * 16u + i, row_scale[m], col, y, up);
+    }
   }
 }
 
