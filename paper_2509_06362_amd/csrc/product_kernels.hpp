@@ -401,7 +401,12 @@ __global__ void __launch_bounds__(64 * WM * WN, Stages * (WM * MI + WN * NI) * 2
   };
 #pragma clang diagnostic pop
   auto place_of = [&](uint32_t q) { return q < kALoads ? (wave * kALoads + q) * 1024u : kRows * 128u + (wave * kBLoads + (q - kALoads)) * 1024u; };
-  auto bring = [&](uint32_t step, uint32_t q) { async16(from[q] + step * 128u, step % Stages * kStage + place_of(q)); };
+  // (Rows that are not there are not brought, where every wait is for all that is under way: what lies in their place meets no sum that is kept.)
+  constexpr bool kSkips = Stages == 2;
+  auto bring = [&](uint32_t step, uint32_t q) {
+    if (kSkips && q < kALoads && (wave * kALoads + q) * 8u >= t.rows) return;
+    async16(from[q] + step * 128u, step % Stages * kStage + place_of(q));
+  };
   auto bring_end = [&](uint32_t step) {  // the rows' end lies in this step: zeros behind it in both
     for (uint32_t q = 0; q < kLoads; ++q)
       *reinterpret_cast<u32x4*>(lds + step % Stages * kStage + place_of(q) + lane * 16u) = row_bytes(from[q] - piece, step * 128u + piece, a.in_bytes);
@@ -432,7 +437,21 @@ __global__ void __launch_bounds__(64 * WM * WN, Stages * (WM * MI + WN * NI) * 2
       bring_end(s);
     }
   }
-  meet_behind<kLoads, Stages - 1>(steps - 1u);
+  if (kSkips && (wave * kALoads + kALoads - 1u) * 8u >= t.rows) meet<0>();  // (fewer loads a step than are counted)
+  else meet_behind<kLoads, Stages - 1>(steps - 1u);
+  if (wm * MI * 16u >= t.rows) {  // none of this wave's rows are there: it brings its share and leaves the matrix unit to the others
+    for (uint32_t step = 0; step + 1u < steps; ++step) {
+      meet_behind<kLoads, Stages - 2>(steps - 2u - step);
+      const uint32_t next = step + Stages;
+      if (next < whole) {
+#pragma unroll
+        for (uint32_t q = 0; q < kLoads; ++q) bring(next, q);
+      } else if (next < steps) {
+        bring_end(next);
+      }
+    }
+    return;
+  }
 #pragma unroll
   for (int k = 0; k < kReads; ++k) read(0u, 0, k);
   for (uint32_t step = 0; step < steps; ++step) {
