@@ -75,7 +75,8 @@ __global__ void __launch_bounds__(Threads == 64 ? 256 : Threads) quantize_kernel
     }
     if (first) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) top = max(top, __builtin_bit_cast(uint32_t, y[k]) & 0x7fffffffu);
+      for (int k = 0; k < 8; k += 2)
+        top = max(max(__builtin_bit_cast(uint32_t, y[k]) & 0x7fffffffu, __builtin_bit_cast(uint32_t, y[k + 1]) & 0x7fffffffu), top);
     }
   };
   float held[Held][8];
@@ -116,19 +117,26 @@ __global__ void __launch_bounds__(Threads == 64 ? 256 : Threads) quantize_kernel
       good = most < __builtin_huge_valf();
     }
   }
-  const float scale = good ? most / 127.0f : __builtin_nanf("");
+  if (thread == 0u) a.scale[row] = good ? most / 127.0f : __builtin_nanf("");
   // Rows of very small numbers are raised by 2^100 first: 127 / m would be no number for them.
-  const float raise = most < 0x1p-100f ? 0x1p100f : 1.0f;
-  const float per = good && most > 0.0f ? 127.0f / (most * raise) : 0.0f;
-  if (thread == 0u) a.scale[row] = scale;
+  const float raise = most < 0x1p-100f ? 0x1p100f : 1.0f, per = good && most > 0.0f ? 127.0f / (most * raise) : 0.0f;
   int8_t* q = a.q + row * a.q_stride;
-  auto store = [&](uint32_t turn, const float (&y)[8]) {
+  // Added to 1.5 * 2^23 a number up to 2^22 is rounded to a whole one, ties to even, whose lowest byte is the sum's.
+  auto store = [&](uint32_t turn, float (&y)[8]) {
+    constexpr float kWhole = 12582912.0f;
     const uint32_t at = (turn * Threads + thread) * 8u;
     uint32_t b[2] = {0u, 0u};
+    if (per != 0.0f) {  // (the same for the row)
+      if (raise != 1.0f) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const float v = per == 0.0f ? 0.0f : rintf(y[k] * by * raise * per);
-      b[k / 4] |= ((uint32_t)(int)v & 255u) << (8 * (k % 4));
+        for (int k = 0; k < 8; ++k) y[k] *= raise;
+      }
+      uint32_t v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = __builtin_bit_cast(uint32_t, Form == MAASO_ROWS_NORM ? fmaf(y[k] * by, per, kWhole) : fmaf(y[k], per, kWhole));
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        b[h] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(v[4 * h + 3], v[4 * h + 2], 0x0c0c0400u), __builtin_amdgcn_perm(v[4 * h + 1], v[4 * h], 0x0c0c0400u), 0x05040100u);
     }
     if (at + 8u <= a.width) {
       *reinterpret_cast<u32x2*>(q + at) = (u32x2){b[0], b[1]};
