@@ -5,9 +5,11 @@ A small decoder of random weights serves `level` requests behind one prompt: the
 step grows the rows by a token (extend, copy on write), writes its keys and values with the heads' norms and the rotation
 (append), attends (the shared beginning read once for all), and chooses tokens (penalties, temperature).  A step is
 captured into a graph and replayed; nothing goes through the host between steps.  The seconds per step against the load
-are what maaso_profile_fit makes the table from that maaso_profile_tables_load takes.
+are what maaso_profile_fit makes the table from that maaso_profile_tables_load takes.  With --experts the feed-forward is
+one of experts (route, products by expert, combine); with --eight its weights and the projections' are held in 8 bits
+(rows quantized behind the norm, products with scales).
 
-    python examples/measure_instance.py [--layers 4] [--levels 1,2,4,8,16,32,64] [--prompt 900] [--steps 32]
+    python examples/measure_instance.py [--layers 4] [--levels 1,2,4,8,16,32,64] [--prompt 900] [--steps 32] [--experts 0] [--chosen 2] [--eight]
 """
 from __future__ import annotations
 
@@ -26,10 +28,20 @@ import torch
 from paper_2509_06362_amd import binding, instance as I
 
 
-class Decoder:
-    """Weights of a decoder with grouped heads, head norms and rotation; plain products are torch's."""
+class Eight:
+    """Weights [..., channels, in] in 8 bits, a scale for each channel."""
 
-    def __init__(self, layers=4, heads=16, kv_heads=4, dim=128, vocab=32000, max_len=4096, dtype=torch.bfloat16, seed=0):
+    def __init__(self, w):
+        w = w.float()
+        self.scale = w.abs().amax(-1) / 127
+        self.w = (w / self.scale.unsqueeze(-1)).round().to(torch.int8)
+
+
+class Decoder:
+    """Weights of a decoder with grouped heads, head norms and rotation; plain products are torch's.  experts: of the
+    feed-forward, 0 for none, `chosen` of them for each token; eight: projections and experts in 8 bits."""
+
+    def __init__(self, layers=4, heads=16, kv_heads=4, dim=128, vocab=32000, max_len=4096, dtype=torch.bfloat16, seed=0, experts=0, chosen=2, eight=False):
         g = torch.Generator().manual_seed(seed)
         self.layers, self.heads, self.kv_heads, self.dim, self.vocab, self.dtype = layers, heads, kv_heads, dim, vocab, dtype
         self.hidden = hidden = heads * dim
@@ -40,12 +52,20 @@ class Decoder:
         self.embedding = torch.randn(vocab, hidden, generator=g).to(dtype).cuda()
         self.qkv = [weight((heads + 2 * kv_heads) * dim, hidden) for _ in range(layers)]
         self.out = [weight(hidden, hidden) for _ in range(layers)]
-        self.up = [weight(2 * hidden, hidden) for _ in range(layers)]
-        self.down = [weight(hidden, 2 * hidden) for _ in range(layers)]
+        self.experts, self.chosen, self.eight, self.inner = experts, chosen, eight, hidden
+        if not experts:
+            self.up = [weight(2 * hidden, hidden) for _ in range(layers)]
+            self.down = [weight(hidden, 2 * hidden) for _ in range(layers)]
         self.q_norm = [(1 + 0.1 * torch.randn(dim, generator=g)).to(dtype).cuda() for _ in range(layers)]
         self.k_norm = [(1 + 0.1 * torch.randn(dim, generator=g)).to(dtype).cuda() for _ in range(layers)]
         angle = torch.arange(max_len, dtype=torch.float64)[:, None] * 10000.0 ** (-torch.arange(dim // 2, dtype=torch.float64) / (dim // 2))
         self.cos_sin = torch.cat([angle.cos(), angle.sin()], 1).float().cuda()
+        if experts:
+            self.router = [weight(experts, hidden) for _ in range(layers)]
+            self.up = [weight(experts * 2 * self.inner, hidden).view(experts, 2 * self.inner, hidden) for _ in range(layers)]
+            self.down = [weight(experts * hidden, self.inner).view(experts, hidden, self.inner) for _ in range(layers)]
+        if eight:
+            self.qkv, self.out, self.up, self.down = ([Eight(w) for w in ws] for ws in (self.qkv, self.out, self.up, self.down))
 
     def normed(self, x):
         x = x.float()
@@ -68,11 +88,53 @@ class Serving:
         """The tensors of a step of these rows (a list) with `tokens` new ones each."""
         m, n, cuda = self.model, len(rows), dict(device="cuda")
         total = n * tokens
-        return dict(rows=torch.tensor(rows, dtype=torch.int32, **cuda), q_start=torch.arange(0, total + 1, tokens, dtype=torch.int32, **cuda),
+        more = {}
+        if m.experts or m.eight:
+            places, i32 = total * max(1, m.chosen if m.experts else 1), dict(dtype=torch.int32, **cuda)
+            wide = max(m.hidden, m.inner, 2 * m.hidden)
+            more = dict(expert=torch.empty(total, m.chosen, **i32), place=torch.empty(total, m.chosen, **i32), token=torch.empty(total * m.chosen, **i32),
+                        start=torch.empty(m.experts + 1, **i32), weight=torch.empty(total, m.chosen, **cuda), q8=torch.empty(places * wide, dtype=torch.int8, **cuda),
+                        scale=torch.empty(places, **cuda))
+        return dict(more, rows=torch.tensor(rows, dtype=torch.int32, **cuda), q_start=torch.arange(0, total + 1, tokens, dtype=torch.int32, **cuda),
                     slot=torch.empty(total, dtype=torch.int64, **cuda), pos=torch.empty(total, dtype=torch.int32, **cuda),
                     copies=torch.empty(n, 2, dtype=torch.int32, **cuda), q=torch.empty(total, m.heads, m.dim, dtype=m.dtype, **cuda),
                     o=torch.empty(total, m.heads, m.dim, dtype=m.dtype, **cuda), last=torch.arange(tokens - 1, total, tokens, **cuda),
                     chosen=torch.empty(n, dtype=torch.int32, **cuda), tokens=tokens)
+
+    def quantized(self, x, b, norm=False, gated=False):
+        """Rows in 8 bits and their scales."""
+        width = x.shape[1] // (2 if gated else 1)
+        q = b["q8"][:x.shape[0] * width].view(x.shape[0], width)
+        I.maaso_rows_quantize(self.inst, x=x, q=q, scale=b["scale"], norm=norm, gated=gated)
+        return dict(a=q, a_scale=b["scale"][:x.shape[0]])
+
+    def project(self, x, w, b, norm=False):
+        """x, normed or not, with a layer's weights, in 16 or in 8 bits."""
+        m = self.model
+        if not m.eight:
+            return (m.normed(x) if norm else x) @ w.T
+        out = torch.empty(x.shape[0], w.w.shape[0], dtype=m.dtype, device="cuda")
+        I.maaso_scaled_product(self.inst, **self.quantized(x, b, norm), w=w.w, w_scale=w.scale, out=out)
+        return out
+
+    def feed_forward(self, layer, x, b):
+        m, inst = self.model, self.inst
+        if not m.experts:
+            return x + self.project(torch.relu(self.project(x, m.up[layer], b, norm=True)), m.down[layer], b)
+        normed, places = m.normed(x), x.shape[0] * m.chosen
+        I.maaso_expert_route(inst, logits=normed @ m.router[layer].T, expert=b["expert"], weight=b["weight"], start=b["start"], token=b["token"], place=b["place"])
+        up, down = m.up[layer], m.down[layer]
+        h = torch.empty(places, m.inner, dtype=m.dtype, device="cuda")
+        y = torch.empty(places, m.hidden, dtype=m.dtype, device="cuda")
+        if m.eight:
+            I.maaso_expert_product(inst, **self.quantized(x, b, norm=True), w=up.w, w_scale=up.scale, out=h, start=b["start"], token=b["token"], gated=True)
+            I.maaso_expert_product(inst, **self.quantized(h, b), w=down.w, w_scale=down.scale, out=y, start=b["start"])
+        else:
+            I.maaso_expert_product(inst, a=normed, w=up, out=h, start=b["start"], token=b["token"], gated=True)
+            I.maaso_expert_product(inst, a=h, w=down, out=y, start=b["start"])
+        out = torch.empty_like(x)
+        I.maaso_expert_combine(inst, y=y, place=b["place"], weight=b["weight"], out=out, residual=x)
+        return out
 
     def step(self, ids, b, group=None, adjust=None):
         """Logits behind the rows' new tokens `ids`, the chosen tokens in b["chosen"]; group: (group_start, shared, most)."""
@@ -82,14 +144,14 @@ class Serving:
         I.maaso_kv_copy(inst, self.cache, pairs=b["copies"])
         x, wide, side = m.embedding[ids], m.heads * m.dim, m.kv_heads * m.dim
         for layer in range(m.layers):
-            qkv = m.normed(x) @ m.qkv[layer].T
+            qkv = self.project(x, m.qkv[layer], b, norm=True)
             q, k, v = (t.unflatten(1, (-1, m.dim)) for t in (qkv[:, :wide], qkv[:, wide:wide + side], qkv[:, wide + side:]))
             I.maaso_kv_append(inst, self.cache, layer=layer, q=q, k=k, v=v, q_out=b["q"], slot=b["slot"], pos=b["pos"], cos_sin=m.cos_sin,
                               q_weight=m.q_norm[layer], k_weight=m.k_norm[layer])
             I.maaso_kv_attention(inst, self.cache, self.pages, layer=layer, q=b["q"], out=b["o"], q_start=b["q_start"], rows=b["rows"], scale=m.dim ** -0.5,
                                  max_q=b["tokens"], max_len=self.max_len, group_start=start, shared=shared, max_shared=most)
-            x = x + b["o"].flatten(1) @ m.out[layer].T
-            x = x + torch.relu(m.normed(x) @ m.up[layer].T) @ m.down[layer].T
+            x = x + self.project(b["o"].flatten(1), m.out[layer], b)
+            x = self.feed_forward(layer, x, b)
         logits = m.normed(x[b["last"]]) @ m.embedding.T
         I.maaso_logits_adjust(inst, logits=logits, chosen=b["chosen"], **(adjust or {}))
         return logits
@@ -145,9 +207,12 @@ def main(argv=None):
     p.add_argument("--levels", default="1,2,4,8,16,32,64")
     p.add_argument("--prompt", type=int, default=900)
     p.add_argument("--steps", type=int, default=32)
+    p.add_argument("--experts", type=int, default=0)
+    p.add_argument("--chosen", type=int, default=2)
+    p.add_argument("--eight", action="store_true")
     a = p.parse_args(argv)
     levels = [int(x) for x in a.levels.split(",")]
-    model = Decoder(layers=a.layers)
+    model = Decoder(layers=a.layers, experts=a.experts, chosen=a.chosen, eight=a.eight)
     seconds = [measure(model, level, a.prompt, a.steps) for level in levels]
     # a request's tokens per second against the load, as the profiler's fit takes them
     params, tbt = binding.maaso_profile_fit([0, len(levels)], np.array(levels), 1.0 / np.array(seconds), b_cap=max(levels))
