@@ -244,7 +244,8 @@ int maaso_logits_adjust(maaso_instance* inst, const maaso_logits_args* a, void* 
  *   MAASO_ROWS_PLAIN:  x
  *   MAASO_ROWS_NORM:   x / sqrt(mean(x^2) + eps) * weight           (weight NULL: 1)
  *   MAASO_ROWS_GATED:  silu(x[i]) * x[width + i], silu(x) = x / (1 + exp(-x)); x has 2 * width elements
- * and with m = max |y|:   scale[t] = m / 127,   q[t][i] = y * (127 / m), rounded to the nearest, ties to even.
+ * and with m = max |y|:   scale[t] = m / 127,   q[t][i] = y * (1 / m * 127), each step in binary32, then
+ * rounded to the nearest whole number, ties to even.
  * A row of zeros has q = 0, scale = 0.  A row that holds a NaN or an infinity in y, or whose sum of squares passes
  * binary32, has q = 0, scale = NaN: products of it are NaN and nothing else is.  All DEVICE.
  * Errors: INVALID_ARG, SHAPE, BUSY, HIP. */

@@ -118,10 +118,11 @@ __global__ void __launch_bounds__(Threads == 64 ? 256 : Threads) quantize_kernel
     }
   }
   if (thread == 0u) a.scale[row] = good ? most / 127.0f : __builtin_nanf("");
-  // Rows of very small numbers are raised by 2^100 first: 127 / m would be no number for them.
-  const float raise = most < 0x1p-100f ? 0x1p100f : 1.0f, per = good && most > 0.0f ? 127.0f / (most * raise) : 0.0f;
+  // Rows of very small numbers are raised by 2^100 first: 1 / m would be no number for them.
+  const float raise = most < 0x1p-100f ? 0x1p100f : 1.0f, per = good && most > 0.0f ? 1.0f / (most * raise) * 127.0f : 0.0f;
   int8_t* q = a.q + row * a.q_stride;
-  // Added to 1.5 * 2^23 a number up to 2^22 is rounded to a whole one, ties to even, whose lowest byte is the sum's.
+  // Added to 1.5 * 2^23 a number up to 2^22 is rounded to a whole one, ties to even, whose lowest byte is the sum's.  (The
+  // reciprocal and both products are rounded to binary32 first, as the interface has it: whoever works a row out in binary32 gets the same bytes.)
   auto store = [&](uint32_t turn, float (&y)[8]) {
     constexpr float kWhole = 12582912.0f;
     const uint32_t at = (turn * Threads + thread) * 8u;
@@ -133,7 +134,7 @@ __global__ void __launch_bounds__(Threads == 64 ? 256 : Threads) quantize_kernel
       }
       uint32_t v[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = __builtin_bit_cast(uint32_t, Form == MAASO_ROWS_NORM ? fmaf(y[k] * by, per, kWhole) : fmaf(y[k], per, kWhole));
+      for (int k = 0; k < 8; ++k) v[k] = __builtin_bit_cast(uint32_t, (Form == MAASO_ROWS_NORM ? y[k] * by * per : y[k] * per) + kWhole);
 #pragma unroll
       for (int h = 0; h < 2; ++h)
         b[h] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(v[4 * h + 3], v[4 * h + 2], 0x0c0c0400u), __builtin_amdgcn_perm(v[4 * h + 1], v[4 * h], 0x0c0c0400u), 0x05040100u);
