@@ -33,13 +33,9 @@ struct RouteArgs {
 constexpr uint32_t kChunk = 64;      // tokens whose places are worked out together
 constexpr uint32_t kOneBlock = 256;  // tokens that one block chooses for and puts in order alone
 
-template <int Ctrl> __device__ inline float dpp(float v) {
-  const int b = __builtin_bit_cast(int, v);
-  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(b, b, Ctrl, 0xf, 0xf, false));
-}
-template <int Ctrl> __device__ inline uint32_t dpp(uint32_t v) {
-  return (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, Ctrl, 0xf, 0xf, false);
-}
+// Every control used here reads a lane that is there.
+template <int Ctrl> __device__ inline uint32_t dpp(uint32_t v) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, Ctrl, 0xf, 0xf, true); }
+template <int Ctrl> __device__ inline float dpp(float v) { return __builtin_bit_cast(float, dpp<Ctrl>(__builtin_bit_cast(uint32_t, v))); }
 
 // Over groups of Lanes neighbouring lanes (16, 32 or 64); every lane ends with the group's value.
 template <int Lanes, typename V, typename Op> __device__ inline V join(V v, Op op) {
@@ -51,18 +47,22 @@ template <int Lanes, typename V, typename Op> __device__ inline V join(V v, Op o
   if constexpr (Lanes >= 64) v = op(v, (V)__shfl_xor(v, 32));
   return v;
 }
-template <int Lanes> __device__ inline float largest(float v) {
-  return join<Lanes>(v, [](float a, float b) { return fmaxf(a, b); });
+template <int Lanes> __device__ inline uint32_t largest(uint32_t v) {
+  return join<Lanes>(v, [](uint32_t a, uint32_t b) { return max(a, b); });
 }
 template <int Lanes> __device__ inline uint32_t lowest(uint32_t v) {
   return join<Lanes>(v, [](uint32_t a, uint32_t b) { return min(a, b); });
 }
-template <int Lanes> __device__ inline uint32_t in_all(uint32_t v) {
-  return join<Lanes>(v, [](uint32_t a, uint32_t b) { return a + b; });
-}
 template <int Lanes> __device__ inline float in_all(float v) {
   return join<Lanes>(v, [](float a, float b) { return a + b; });
 }
+
+// A score as a whole number that is larger where the score is; 0, which none has, is below them all.  (0 is added: -0 is 0.)
+__device__ inline uint32_t key_of(float s) {
+  const uint32_t b = __builtin_bit_cast(uint32_t, s + 0.0f);
+  return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
+__device__ inline float score_of(uint32_t key) { return __builtin_bit_cast(float, key ^ ((uint32_t)((int32_t)~key >> 31) | 0x80000000u)); }
 
 constexpr float kNever = -__builtin_huge_valf();  // the score of what is not chosen, or has been
 
@@ -79,54 +79,46 @@ template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) Four { 
 template <typename T, int Lanes, int Quads, bool Biased> struct Chooser {
   static constexpr int kHeld = 4 * Quads, kSlots = Lanes >= 32 ? 1 : 2;
   uint32_t lane;
-  float x[kHeld];
-  float mine[kSlots];      // the logits of choices lane, lane + Lanes
-  int32_t which[kSlots];
-  uint32_t rank[kSlots];   // where they stand
+  const T* row;
+  int32_t which[kSlots];  // choices lane, lane + Lanes
+  uint32_t rank[kSlots];  // where they stand
 
   __device__ inline uint32_t expert(int i) const { return 4u * lane + 4u * Lanes * (uint32_t)(i / 4) + (uint32_t)(i % 4); }
+  static __device__ inline float tidy(float x) { return fminf(x != x ? kNever : x, 3.40282347e38f); }
+  __device__ inline float logit(int32_t e) const { return tidy((float)row[e < 0 ? 0 : e]); }
 
-  __device__ inline void keep(uint32_t j, uint32_t at, float logit) {
+  __device__ inline void keep(uint32_t j, uint32_t at) {
 #pragma unroll
-    for (int h = 0; h < kSlots; ++h) {
-      const bool is = j == lane + (uint32_t)(h * Lanes);
-      mine[h] = is ? logit : mine[h];
-      which[h] = is ? (int32_t)at : which[h];
-    }
+    for (int h = 0; h < kSlots; ++h) which[h] = j == lane + (uint32_t)(h * Lanes) ? (int32_t)at : which[h];
   }
 
-  // The rounds by scores s.  With a bias: true where all of them would have to be in 64 bits.
-  __device__ inline bool rounds(uint32_t k, const float* bias, float (&s)[kHeld]) {
+  // The rounds by keys s.  With a bias: true where all of them would have to be in 64 bits.
+  __device__ inline bool rounds(uint32_t k, const float* bias, uint32_t (&s)[kHeld]) {
     bool near = false, full = false;
     float before = __builtin_huge_valf();
     uint32_t j = 0;
     for (; Biased || j < k; ++j) {
-      float m = s[0];
+      uint32_t m = s[0];
 #pragma unroll
-      for (int i = 1; i < kHeld; ++i) m = fmaxf(m, s[i]);
-      m = largest<Lanes>(m);
+      for (int i = 1; i + 1 < kHeld; i += 2) m = max(max(s[i], s[i + 1]), m);
+      m = largest<Lanes>(max(m, s[kHeld - 1]));
       if constexpr (Biased) {
-        const bool follows = m > kNever && before - m <= 0x1p-21f * (1.0f + fabsf(m));
+        const float score = score_of(m);
+        const bool follows = m != 0u && before - score <= 0x1p-21f * (1.0f + fabsf(score));
         near = near || (follows && j <= k);
         if (j >= k && !__ballot(follows)) break;
         full = j == (uint32_t)(Lanes * kSlots);
         if (full) break;
-        before = m;
+        before = score;
       }
       uint32_t at = 0xffffffffu;
 #pragma unroll
       for (int i = kHeld - 1; i >= 0; --i) at = s[i] == m ? expert(i) : at;
       at = lowest<Lanes>(at);
-      if (m == kNever) at = 0xffffffffu;
-      float logit = Biased ? kNever : m;
+      if (m == 0u) at = 0xffffffffu;
 #pragma unroll
-      for (int i = 0; i < kHeld; ++i) {
-        const bool is = at == expert(i);
-        if constexpr (Biased) logit = is ? x[i] : logit;
-        s[i] = is ? kNever : s[i];
-      }
-      if constexpr (Biased) logit = largest<Lanes>(logit);
-      keep(j, at, logit);
+      for (int i = 0; i < kHeld; ++i) s[i] = at == expert(i) ? 0u : s[i];
+      keep(j, at);
     }
     if constexpr (!Biased) return false;
     if (!__ballot(near)) return false;
@@ -134,7 +126,7 @@ template <typename T, int Lanes, int Quads, bool Biased> struct Chooser {
     double d[kSlots];
 #pragma unroll
     for (int h = 0; h < kSlots; ++h) {
-      d[h] = which[h] < 0 ? (double)kNever : score64(mine[h], bias[which[h]]);
+      d[h] = which[h] < 0 ? (double)kNever : score64(logit(which[h]), bias[which[h]]);
       rank[h] = which[h] < 0 ? rank[h] : 0u;
     }
 #pragma unroll
@@ -149,36 +141,32 @@ template <typename T, int Lanes, int Quads, bool Biased> struct Chooser {
     return false;
   }
 
-  __device__ inline void rounds64(uint32_t k, const float* bias, const float (&s)[kHeld], bool again) {
+  __device__ inline void rounds64(uint32_t k, const float* bias, const uint32_t (&s)[kHeld], bool again) {
     double d[kHeld];
 #pragma unroll
-    for (int i = 0; i < kHeld; ++i) d[i] = s[i] > kNever ? score64(x[i], bias[expert(i)]) : (double)kNever;
+    for (int i = 0; i < kHeld; ++i) d[i] = s[i] ? score64(logit((int32_t)expert(i)), bias[expert(i)]) : (double)kNever;
     for (uint32_t j = 0; j < k; ++j) {
       double best = (double)kNever;
       uint32_t at = 0xffffffffu;
-      float logit = kNever;
 #pragma unroll
       for (int i = 0; i < kHeld; ++i) {
         if (d[i] > best) {
           best = d[i];
           at = expert(i);
-          logit = x[i];
         }
       }
 #pragma unroll
       for (int l = Lanes / 2; l > 0; l /= 2) {
         const double o = __shfl_xor(best, l);
         const uint32_t oa = (uint32_t)__shfl_xor((int)at, l);
-        const float ol = __shfl_xor(logit, l);
         if (o > best || (o == best && oa < at)) {
           best = o;
           at = oa;
-          logit = ol;
         }
       }
 #pragma unroll
       for (int i = 0; i < kHeld; ++i) d[i] = at == expert(i) ? (double)kNever : d[i];
-      if (again) keep(j, at, logit);
+      if (again) keep(j, at);
     }
   }
 };
@@ -190,60 +178,66 @@ __device__ inline void choose(const RouteArgs& a, uint32_t t, uint32_t* marks, u
   constexpr int kHeld = C::kHeld, kSlots = C::kSlots;
   C c;
   c.lane = threadIdx.x % Lanes;
-  const T* row = static_cast<const T*>(a.logits) + t * a.stride;
-  float s[kHeld];
+  c.row = static_cast<const T*>(a.logits) + t * a.stride;
+  float x[kHeld];
+  uint32_t s[kHeld];
 #pragma unroll
   for (int q = 0; q < Quads; ++q) {
     const uint32_t e = c.expert(4 * q);
     if (e + 4u <= a.n_experts) {
-      const Four<T> f = *reinterpret_cast<const Four<T>*>(row + e);
+      const Four<T> f = *reinterpret_cast<const Four<T>*>(c.row + e);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) c.x[4 * q + i] = (float)f.v[i];
-      if constexpr (Biased) {
-        const Four<float> b = *reinterpret_cast<const Four<float>*>(a.bias + e);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[4 * q + i] = b.v[i];
-      }
+      for (int i = 0; i < 4; ++i) x[4 * q + i] = (float)f.v[i];
     } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const bool in = e + (uint32_t)i < a.n_experts;
-        c.x[4 * q + i] = in ? (float)row[e + i] : kNever;
-        if constexpr (Biased) s[4 * q + i] = in ? a.bias[e + i] : 0.0f;
-      }
+      for (int i = 0; i < 4; ++i) x[4 * q + i] = e + (uint32_t)i < a.n_experts ? (float)c.row[e + i] : kNever;
     }
   }
 #pragma unroll
-  for (int i = 0; i < kHeld; ++i) {
-    float& x = c.x[i];
-    x = fminf(x != x ? kNever : x, 3.40282347e38f);
+  for (int q = 0; q < Quads; ++q) {
+    Four<float> b{};
     if constexpr (Biased) {
-      const float both = sigmoid(x) + s[i];
-      s[i] = x > kNever && both == both ? both : kNever;
-    } else {
-      s[i] = x;
+      const uint32_t e = c.expert(4 * q);
+      if (e + 4u <= a.n_experts) {
+        b = *reinterpret_cast<const Four<float>*>(a.bias + e);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) b.v[i] = e + (uint32_t)i < a.n_experts ? a.bias[e + i] : 0.0f;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float& v = x[4 * q + i];
+      v = C::tidy(v);
+      float score = v;
+      if constexpr (Biased) {
+        score = sigmoid(v) + b.v[i];
+        score = v > kNever && score == score ? score : kNever;
+      }
+      s[4 * q + i] = score > kNever ? key_of(score) : 0u;
     }
   }
   float sum = 1.0f, top = kNever;
-  if (!a.sigmoid) {
+  if (!a.sigmoid) {  // (the keys are the logits')
+    uint32_t m = s[0];
 #pragma unroll
-    for (int i = 0; i < kHeld; ++i) top = fmaxf(top, c.x[i]);
-    top = largest<Lanes>(top);
+    for (int i = 1; i < kHeld; ++i) m = max(m, s[i]);
+    m = largest<Lanes>(m);
+    top = m ? score_of(m) : kNever;
     if (!a.renorm) {  // (where the chosen are divided by their sum, that of all is no part of it)
       sum = 0.0f;
 #pragma unroll
-      for (int i = 0; i < kHeld; ++i) sum += c.x[i] > kNever ? exp_below(c.x[i] - top) : 0.0f;
+      for (int i = 0; i < kHeld; ++i) sum += x[i] > kNever ? exp_below(x[i] - top) : 0.0f;
       sum = in_all<Lanes>(sum);
     }
   }
 #pragma unroll
   for (int h = 0; h < kSlots; ++h) {
-    c.mine[h] = kNever;
     c.which[h] = -1;
     c.rank[h] = c.lane + (uint32_t)(h * Lanes);
   }
   if constexpr (Biased) {
-    float once[kHeld];
+    uint32_t once[kHeld];
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) once[i] = s[i];
     const bool again = c.rounds(a.k, a.bias, once);
@@ -251,11 +245,13 @@ __device__ inline void choose(const RouteArgs& a, uint32_t t, uint32_t* marks, u
   } else {
     c.rounds(a.k, nullptr, s);
   }
-  float chosen = 0.0f;
+  float p[kSlots], chosen = 0.0f;
 #pragma unroll
   for (int h = 0; h < kSlots; ++h) {
-    c.mine[h] = c.which[h] < 0 || c.rank[h] >= a.k ? 0.0f : a.sigmoid ? sigmoid(c.mine[h]) : exp_below(c.mine[h] - top);
-    chosen += c.mine[h];
+    const bool is = c.which[h] >= 0 && c.rank[h] < a.k;
+    const float l = c.logit(is ? c.which[h] : 0);
+    p[h] = is ? a.sigmoid ? sigmoid(l) : exp_below(l - top) : 0.0f;
+    chosen += p[h];
   }
   chosen = in_all<Lanes>(chosen);
   const float by = a.renorm ? chosen : sum;
@@ -264,7 +260,7 @@ __device__ inline void choose(const RouteArgs& a, uint32_t t, uint32_t* marks, u
     const uint32_t j = c.rank[h];
     if (j >= a.k) continue;
     a.expert[(uint64_t)t * a.k + j] = c.which[h];
-    a.weight[(uint64_t)t * a.k + j] = c.which[h] < 0 || by == 0.0f ? 0.0f : c.mine[h] / by * a.scale;
+    a.weight[(uint64_t)t * a.k + j] = c.which[h] < 0 || by == 0.0f ? 0.0f : p[h] / by * a.scale;
     if (marks && c.which[h] >= 0) atomicOr(&marks[(uint32_t)c.which[h] * words + bit / 32u], 1u << (bit & 31u));
   }
 }
