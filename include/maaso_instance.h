@@ -267,7 +267,7 @@ int maaso_rows_quantize(maaso_instance* inst, const maaso_rows_quantize_args* a,
  *   y[t][c] = a_scale[t] * w_scale[c] * sum_i a[t][i] w[c][i] + bias[c]
  * and, where `gated` is not 0, w has 2 * n_out rows and out[t][c] = silu(y[t][c]) * y[t][n_out + c], else out = y.
  * Sums of 8-bit integers are exact, those of 16-bit types binary32.  What lies between a row's n_in elements and the next
- * row has no part in it, whatever it holds.  No rows may be 0: nothing is done then. */
+ * row has no part in it, whatever it holds.  out overlaps nothing that is read.  Without rows nothing is done. */
 typedef struct {
   uint32_t type;     /* of a and w: INT8, or, of experts, BF16 or FP16                              */
   uint32_t out_type; /* FP32 or, of INT8, BF16 or FP16, of these the same                           */

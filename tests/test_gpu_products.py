@@ -112,6 +112,33 @@ def test_large(inst, name, n_in, gated):  # noqa: F811
         assert torch.equal(out.double(), y)
 
 
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("name", ["int8", "bf16"])
+def test_large_and_ragged(inst, name, gated):  # noqa: F811
+    """The largest tiles, some of them hardly filled: whole numbers, exact but for the gate; rows of no expert as they were."""
+    counts, n = [700, 3, 0, 1030, 129, 250, 900, 1100], 500
+    n_in, n_out, rows = 2000 if name == "int8" else 1000, 2048 if gated else 4096, sum(counts) + 9
+    g = torch.Generator().manual_seed(17)
+    a, w = whole(g, n, n_in, high=7), whole(g, len(counts), n_out * (2 if gated else 1), n_in, high=7)
+    if name == "int8":
+        a, w, scales = padded(a, 16, 1), padded(w, 16, 1), dict(a_scale=torch.full((n,), 2.0 ** -11, device="cuda"))
+    else:
+        a, w, scales = padded(a.to(torch.bfloat16) / 64, 8, math.nan), padded(w.to(torch.bfloat16) / 32, 8, math.nan), {}
+    token = torch.randint(n, (rows,), generator=g, dtype=torch.int32).cuda()
+    out = torch.full((rows, n_out), -7.0, device="cuda")
+    I.maaso_expert_product(inst, a=a, w=w, out=out, start=starts(counts, 4), token=token, gated=gated, **scales)
+    assert (out[:4] == -7).all() and (out[4 + sum(counts):] == -7).all()
+    at = 4
+    for i, c in enumerate(counts):
+        t = token[at:at + c].long()
+        y, lost = expected(a[t], w[i], gated=gated, **({"a_scale": scales["a_scale"][t]} if scales else {}))
+        if gated:
+            close(out[at:at + c], y, lost)
+        else:
+            assert torch.equal(out[at:at + c].double(), y)
+        at += c
+
+
 COUNTS = {
     "one": [5], "few": [3, 0, 1, 12], "empty": [0, 0, 0], "crowd": [0, 1000, 0, 1], "even": [40] * 6, "many": [k % 5 for k in range(70)], "wide": [150, 33, 0, 260],
     "most": [1 if k % 3 else 0 for k in range(1024)],

@@ -139,3 +139,13 @@ def test_other_alignments_of_the_weight(inst):
     held = (1 + 0.5 * torch.randn(30, generator=torch.Generator().manual_seed(7))).to(torch.float16).cuda()
     for at in range(6):
         check(x, *run(inst, x, 24, "norm", held[at:at + 24]), "norm", held[at:at + 24])
+
+
+def test_bytes_are_those_of_binary32(inst):
+    """A row as it is: the reciprocal, the product and the rounding step by step."""
+    for name, dtype in TYPES.items():
+        x = (torch.randn(300, 1000, generator=torch.Generator().manual_seed(8)) * 5).to(dtype).cuda()
+        q, scale = run(inst, x, 1000, "plain")
+        most = x.float().abs().amax(1)
+        assert torch.equal(scale, most / torch.full_like(most, 127.0))
+        assert torch.equal(q.float(), torch.round(x.float() * (torch.ones_like(most) / most * 127.0)[:, None]))
