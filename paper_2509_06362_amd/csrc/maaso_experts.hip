@@ -128,6 +128,8 @@ uint32_t best_form(const ProductArgs& a, uint32_t n_cu) {
   return best;
 }
 
+// Of 96 MiB of weights or more the tiles begin at unlike steps: 64 rows of 67 MB (of 16 bits) 14.1 us either way, of 100 MB 26.1 to 23.8, of 134 MB 36.8 to
+// 26.2; of 32 MiB (8 bits, in the cache) 11.1 to 12.0.
 // Few rows go through waves that hold their operands in registers only: up to 16 of one matrix or of an expert where its weights are no more than 32
 // MiB, which many small blocks bring sooner (8 bits, 8 MiB, 16 rows 4.7 us for 7.3 in tiles; 32 MiB 11.4 and 11.3), and up to 4 whatever the weights, for
 // rows beside the last are read again by each block (64 experts of 2.3 MiB, a row each 30.6 us for 35.7, 6 rows 37.8 and 36.3; 8 experts of 32 MiB, 8 rows
@@ -135,6 +137,7 @@ uint32_t best_form(const ProductArgs& a, uint32_t n_cu) {
 template <typename T, bool Gated>
 int launch_product(ProductArgs& a, uint32_t n_cu, hipStream_t s) {
   const uint64_t rows = (a.n_rows + a.n_experts - 1u) / a.n_experts, weights = (uint64_t)a.n_experts * a.channels * a.in_bytes;
+  a.turned = weights >= (96u << 20);
   if (rows <= 4u || (rows <= 16u && weights <= (32u << 20))) return launch_stream<T, Gated>(a, s);
   switch (best_form(a, n_cu)) {
     case 0:
