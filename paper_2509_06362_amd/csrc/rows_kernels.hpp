@@ -1,5 +1,6 @@
 // Rows of activations to 8-bit integers with a scale each, behind a norm or a gate; and the joining of experts' rows.
-// Both are bound by memory.
+// Both are bound by memory: 8192 rows of 4096, 16 bits, 20.8 us, 4.85 TB/s, what a large copy reaches; with a norm 25, for its weight comes from
+// the cache for each row; the gate (4096 rows of 2 x 8192) 36, 4.6 TB/s.  8192 tokens' eight rows of 4096, joined, 144.5 us, 4.65 TB/s.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -37,6 +38,8 @@ template <typename T> __device__ inline void load8(const T* row, uint32_t at, ui
   }
 }
 
+// Registers hold no more than a row needs (4096 with a norm: two turns 25.0 us, room for four 29.4), and a block takes one row: blocks that take
+// one after the other, the next one's loads under way, have fewer beside them and were slower (31.7).
 // One row to `Threads` threads, eight neighbouring elements of each in turn, the first Held turns in registers; what is
 // longer is read, and its gate worked out, a second time.  One reduction: with a norm, max |x * weight| and the sum of squares are
 // taken together, for y = (x * weight) / sqrt(...) is largest where x * weight is.
@@ -193,7 +196,7 @@ template <typename T> __device__ inline void store8(T* row, uint32_t at, uint32_
   }
 }
 
-// A thread is eight neighbouring elements of a token; the token's rows are read at once, four at a time.
+// A thread is eight neighbouring elements of a token; the token's rows are read four at a time, for loads under way are what it waits for.
 template <typename T> __global__ void __launch_bounds__(256) combine_kernel(CombineArgs a) {
   const uint32_t per = (a.width + 7u) / 8u;
   const uint64_t at = (uint64_t)blockIdx.x * 256u + threadIdx.x;
