@@ -33,7 +33,8 @@ struct RouteArgs {
 };
 
 constexpr uint32_t kChunk = 64;      // tokens whose places are worked out together
-constexpr uint32_t kOneBlock = 256;  // tokens that one block chooses for and puts in order alone
+constexpr uint32_t kOneBlock = 64;   // tokens by quads held that one block chooses for and puts in order alone
+constexpr uint32_t kOrderTokens = 512, kOrderChoices = 2560, kOrderRoom = 48u << 10;  // that one block puts in order; bytes of shared memory
 
 // Every control used here reads a lane that is there.
 template <int Ctrl> __device__ inline uint32_t dpp(uint32_t v) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, Ctrl, 0xf, 0xf, true); }
@@ -305,16 +306,18 @@ __device__ inline uint32_t block_before(uint32_t v, uint32_t* meet, uint32_t& al
   return below + upto - v;
 }
 
-// Few tokens: chosen and put in order by one block.  Shared memory: bits [n_experts][words], then before [n_experts].
-template <typename T, int Lanes, int Quads, bool Biased> __global__ void __launch_bounds__(1024) route_kernel(RouteArgs a) {
-  extern __shared__ uint32_t room[];
-  __shared__ uint32_t meet[16];
-  const uint32_t words = (a.n + 31u) / 32u;
-  uint32_t* before = room + a.n_experts * words;
-  for (uint32_t i = threadIdx.x; i < a.n_experts * words; i += 1024u) room[i] = 0u;
-  __syncthreads();
-  for (uint32_t t = threadIdx.x / Lanes; t < a.n; t += 1024u / Lanes) choose<T, Lanes, Quads, Biased>(a, t, room, words, t);
+__device__ inline void mark_chosen(const RouteArgs& a, uint32_t first, uint32_t tokens, uint32_t* bits, uint32_t words) {
+  for (uint32_t i = threadIdx.x; i < tokens * a.k; i += blockDim.x) {
+    const int32_t e = a.expert[(uint64_t)first * a.k + i];
+    const uint32_t t = i / a.k;
+    if (e >= 0) atomicOr(&bits[(uint32_t)e * words + t / 32u], 1u << (t & 31u));
+  }
   lds_atomics_barrier();
+}
+
+// All tokens in order by one block of 1024, from their bits.  Shared memory: bits [n_experts][words], then before [n_experts].
+__device__ inline void order_all(const RouteArgs& a, uint32_t* room, uint32_t words, uint32_t* meet) {
+  uint32_t* before = room + a.n_experts * words;
   uint32_t mine = 0u, all;
   if (threadIdx.x < a.n_experts) {
     for (uint32_t w = 0; w < words; ++w) mine += (uint32_t)__builtin_popcount(room[threadIdx.x * words + w]);
@@ -330,17 +333,42 @@ template <typename T, int Lanes, int Quads, bool Biased> __global__ void __launc
   for (uint32_t i = all + threadIdx.x; i < a.n * a.k; i += 1024u) a.token[i] = -1;
 }
 
-// A chunk of tokens to a block, and, where an order is asked for, how many of them go to each expert.
+// A handful of tokens: chosen and put in order by one block.
+template <typename T, int Lanes, int Quads, bool Biased> __global__ void __launch_bounds__(1024) route_kernel(RouteArgs a) {
+  extern __shared__ uint32_t room[];
+  __shared__ uint32_t meet[16];
+  const uint32_t words = (a.n + 31u) / 32u;
+  for (uint32_t i = threadIdx.x; i < a.n_experts * words; i += 1024u) room[i] = 0u;
+  __syncthreads();
+  for (uint32_t t = threadIdx.x / Lanes; t < a.n; t += 1024u / Lanes) choose<T, Lanes, Quads, Biased>(a, t, room, words, t);
+  lds_atomics_barrier();
+  order_all(a, room, words, meet);
+}
+
+// Some more: put in order by one block when all are chosen.
+__global__ void __launch_bounds__(1024) route_order_kernel(RouteArgs a) {
+  extern __shared__ uint32_t room[];
+  __shared__ uint32_t meet[16];
+  const uint32_t words = (a.n + 31u) / 32u;
+  for (uint32_t i = threadIdx.x; i < a.n_experts * words; i += 1024u) room[i] = 0u;
+  __syncthreads();
+  mark_chosen(a, 0u, a.n, room, words);
+  order_all(a, room, words, meet);
+}
+
+// A chunk of tokens to a block of 1024 threads, and how many of them go to each expert; where that is not asked for, a block of any size chooses
+// for as many as it can at once.
 template <typename T, int Lanes, int Quads, bool Biased> __global__ void __launch_bounds__(1024) route_choose_kernel(RouteArgs a) {
   __shared__ uint32_t marks[2 * MAASO_EXPERT_MAX];
-  const uint32_t first = blockIdx.x * kChunk;
-  if (a.before) {
-    for (uint32_t i = threadIdx.x; i < 2u * a.n_experts; i += 1024u) marks[i] = 0u;
-    __syncthreads();
+  if (!a.before) {
+    const uint32_t t = (blockIdx.x * blockDim.x + threadIdx.x) / Lanes;
+    if (t < a.n) choose<T, Lanes, Quads, Biased>(a, t, nullptr, 0u, 0u);
+    return;
   }
-  for (uint32_t t = threadIdx.x / Lanes; t < kChunk && first + t < a.n; t += 1024u / Lanes)
-    choose<T, Lanes, Quads, Biased>(a, first + t, a.before ? marks : nullptr, 2u, t);
-  if (!a.before) return;
+  const uint32_t first = blockIdx.x * kChunk;
+  for (uint32_t i = threadIdx.x; i < 2u * a.n_experts; i += 1024u) marks[i] = 0u;
+  __syncthreads();
+  for (uint32_t t = threadIdx.x / Lanes; t < kChunk && first + t < a.n; t += 1024u / Lanes) choose<T, Lanes, Quads, Biased>(a, first + t, marks, 2u, t);
   lds_atomics_barrier();
   for (uint32_t e = threadIdx.x; e < a.n_experts; e += 1024u)
     a.before[(uint64_t)blockIdx.x * a.n_experts + e] = (uint32_t)(__builtin_popcount(marks[2u * e]) + __builtin_popcount(marks[2u * e + 1u]));
@@ -387,12 +415,7 @@ __global__ void __launch_bounds__(1024) route_place_kernel(RouteArgs a) {
     if (blockIdx.x == 0u) a.start[e] = (int32_t)at;
   }
   if (blockIdx.x == 0u && e == 0u) a.start[a.n_experts] = (int32_t)all;
-  for (uint32_t i = threadIdx.x; i < tokens * a.k; i += 1024u) {
-    const int32_t x = a.expert[(uint64_t)first * a.k + i];
-    const uint32_t t = i / a.k;
-    if (x >= 0) atomicOr(&marks[(uint32_t)x * 2u + t / 32u], 1u << (t & 31u));
-  }
-  lds_atomics_barrier();
+  mark_chosen(a, first, tokens, marks, 2u);
   put_chosen(a, first, tokens, marks, 2u, before);
   for (uint32_t i = first * a.k + threadIdx.x; i < (first + tokens) * a.k; i += 1024u)
     if (i >= all) a.token[i] = -1;
