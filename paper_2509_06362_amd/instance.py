@@ -290,8 +290,8 @@ def maaso_logits_adjust(inst: Instance, *, logits, out=None, chosen=None, repeti
 
 
 def maaso_rows_quantize(inst: Instance, *, x, q, scale, weight=None, norm=False, gated=False, eps=1e-6, stream=None) -> None:
-    """x [rows, width] (gated: [rows, 2 width]), q [rows, width] (int8), scale [rows] (float32); rows 16 bytes apart or a
-    multiple of that.  norm: x / sqrt(mean x^2 + eps) * weight; gated: silu of the first half times the second."""
+    """x [rows, width] (gated: [rows, 2 width]), q [rows, width] (int8, rows a multiple of 16 apart), scale [rows]
+    (float32).  norm: x / sqrt(mean x^2 + eps) * weight; gated: silu of the first half times the second."""
     _check((_native or _load_native()).quantize(inst.handle, x, q, scale, weight, norm, gated, eps, stream),
            "maaso_rows_quantize")
 

@@ -139,6 +139,51 @@ def test_large_and_ragged(inst, name, gated):  # noqa: F811
         at += c
 
 
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("n, n_in, n_out", [(1000, 2050, 3900), (1010, 4000, 1900), (1900, 2000, 3900), (130, 8000, 4000), (510, 4000, 8000)])
+@pytest.mark.parametrize("name", ["int8", "fp16"])
+def test_middling(inst, name, n, n_in, n_out, gated):  # noqa: F811
+    """Tiles of 128 in four stages and in two, and of 64, at one matrix; whole numbers as above."""
+    g = torch.Generator(device="cuda").manual_seed(n + n_in)
+    channels = n_out // 2 * 2
+    a = torch.randint(-3, 4, (n, n_in), generator=g, device="cuda", dtype=torch.int8)
+    w = torch.randint(-3, 4, (channels, n_in), generator=g, device="cuda", dtype=torch.int8)
+    out = torch.full((n, channels // (2 if gated else 1)), -7.0, device="cuda")
+    if name == "int8":
+        a, w, scale = padded(a, 16, 1), padded(w, 16, 1), torch.full((n,), 2.0 ** -11, device="cuda")
+        I.maaso_scaled_product(inst, a=a, w=w, out=out, a_scale=scale, gated=gated)
+        y, lost = expected(a, w, a_scale=scale, gated=gated)
+    else:
+        a, w = padded(a.to(torch.float16) / 64, 8, math.nan), padded(w.to(torch.float16) / 32, 8, math.nan)
+        I.maaso_expert_product(inst, a=a, w=w[None], out=out, start=starts([n]), gated=gated)
+        y, lost = expected(a, w, gated=gated)
+    if gated:
+        close(out, y, lost)
+    else:
+        assert torch.equal(out.double(), y)
+
+
+@pytest.mark.parametrize("counts", [[3, 0, 40, 17, 64, 1, 9, 30], [150, 33, 0, 400, 260, 190, 1, 250]])
+@pytest.mark.parametrize("name", ["int8", "bf16"])
+def test_many_weights(inst, name, counts):  # noqa: F811
+    """More than the tiles read in one order: they begin at unlike steps, and the rows' end lies inside the last."""
+    n, n_out, n_in = 100, 4096, 3210 if name == "int8" else 1610
+    g = torch.Generator(device="cuda").manual_seed(23)
+    a = torch.randint(-7, 8, (n, n_in), generator=g, device="cuda", dtype=torch.int8)
+    w = torch.randint(-7, 8, (len(counts), n_out, n_in), generator=g, device="cuda", dtype=torch.int8)
+    if name == "bf16":
+        a, w = a.to(torch.bfloat16), w.to(torch.bfloat16)
+    a, w = padded(a, 16, 1), padded(w, 16, 1)
+    assert w.numel() * w.element_size() >= 96 << 20
+    token = torch.randint(n, (sum(counts),), generator=g, device="cuda", dtype=torch.int32)
+    out = torch.full((sum(counts), n_out), -7.0, device="cuda")
+    I.maaso_expert_product(inst, a=a, w=w, out=out, start=starts(counts), token=token)
+    at = 0
+    for i, c in enumerate(counts):
+        assert torch.equal(out[at:at + c].double(), a[token[at:at + c].long()].double() @ w[i].double().T)
+        at += c
+
+
 COUNTS = {
     "one": [5], "few": [3, 0, 1, 12], "empty": [0, 0, 0], "crowd": [0, 1000, 0, 1], "even": [40] * 6, "many": [k % 5 for k in range(70)], "wide": [150, 33, 0, 260],
     "most": [1 if k % 3 else 0 for k in range(1024)],
