@@ -273,7 +273,7 @@ typedef struct {
   uint32_t out_type; /* FP32 or, of INT8, BF16 or FP16, of these the same                           */
   uint32_t n_a;      /* rows of a                                                                   */
   uint32_t n_in;     /* 1 .. MAASO_PRODUCT_MAX_IN                                                   */
-  uint32_t n_out, gated;
+  uint32_t n_out, gated; /* n_out < 2^27; rows by channels in tiles of 64 by 64 fewer than 2^24     */
   uint64_t a_stride, w_stride; /* elements between rows; multiples of 16 bytes, as the pointers are */
   uint64_t out_stride;         /* any                                                               */
   const void* a;
@@ -300,7 +300,7 @@ int maaso_scaled_product(maaso_instance* inst, const maaso_product* p, void* hip
  * Errors: INVALID_ARG, SHAPE, WORKSPACE, BUSY, HIP. */
 typedef struct {
   uint32_t type;             /* of the logits: BF16, FP16 or FP32                          */
-  uint32_t n, n_experts, k;  /* k <= n_experts, MAASO_EXPERT_MAX_CHOSEN                    */
+  uint32_t n, n_experts, k;  /* n < 2^26; k <= n_experts, MAASO_EXPERT_MAX_CHOSEN          */
   uint32_t sigmoid, renorm;
   float scale;
   uint64_t stride;           /* elements between the tokens' logits                        */

@@ -15,6 +15,11 @@ using namespace maaso;
 
 namespace {
 
+// A launch holds fewer than 2^32 threads.  Rows beyond kPieceRows of one launch, and threads beyond kPieceThreads, go to another; tokens that are put in
+// order cannot (16 threads to a token at least), and channels have a launch's x to themselves (16 threads to a channel).
+constexpr uint32_t kPieceRows = 1u << 22, kMostTokens = (1u << 26) - 1u, kMostOut = (1u << 27) - 1u;
+constexpr uint64_t kPieceThreads = 1u << 30;
+
 bool whole16(uint64_t elements, uint64_t size) { return elements % (16u / size) == 0; }
 
 template <typename T, int Form, int Threads, int Held>
@@ -54,7 +59,7 @@ int check_product(const maaso_product* p) {
   if (p->type != MAASO_INT8 && p->type != MAASO_BF16 && p->type != MAASO_FP16) return MAASO_E_INVALID_ARG;
   if (p->out_type > MAASO_FP32 || (p->type != MAASO_INT8 && p->out_type != MAASO_FP32 && p->out_type != p->type)) return MAASO_E_INVALID_ARG;
   if (p->type != MAASO_INT8 && (p->a_scale || p->w_scale)) return MAASO_E_INVALID_ARG;
-  if (p->n_in == 0 || p->n_in > MAASO_PRODUCT_MAX_IN || p->n_out == 0 || p->n_out > 0x3fffffffu) return MAASO_E_SHAPE;
+  if (p->n_in == 0 || p->n_in > MAASO_PRODUCT_MAX_IN || p->n_out == 0 || p->n_out > kMostOut) return MAASO_E_SHAPE;
   const uint64_t size = element_size(p->type), channels = (uint64_t)p->n_out * (p->gated ? 2u : 1u);
   if (p->n_a > 1u && (!whole16(p->a_stride, size) || p->a_stride < p->n_in)) return MAASO_E_SHAPE;
   if (channels > 1u && (!whole16(p->w_stride, size) || p->w_stride < p->n_in)) return MAASO_E_SHAPE;
@@ -94,7 +99,7 @@ int launch_tiles(ProductArgs& a, hipStream_t s) {
   const uint32_t cols = WN * NI * 16u / (Gated ? 2u : 1u);
   a.col_tiles = (a.n_out + cols - 1u) / cols;
   const uint64_t most = (most_tiles(a, WM * MI * 16u) * a.col_tiles + 7u) / 8u * 8u;
-  if (most > 0x7fffffffull) return MAASO_E_SHAPE;
+  if (most * (64u * WM * WN) > 0xffffffffull) return MAASO_E_SHAPE;
   hipLaunchKernelGGL((product_tile_kernel<T, WM, WN, MI, NI, Stages, Gated>), dim3((uint32_t)most), dim3(64 * WM * WN), 0, s, a);
   return launched();
 }
@@ -170,7 +175,7 @@ int launch_product(uint32_t type, ProductArgs& a, bool gated, uint32_t n_cu, hip
 // some two thousand choices; beyond that counts by chunks, their sums, and places by chunks.  256 experts, 8 chosen, with a bias, us by one block, by two
 // launches, by three: 16 tokens 8.8, 10.3, 17; 64 tokens 13.2, 10.6, 17; 256 tokens 41, 12.6, 17; 512 tokens -, 20.3, 17.3; 64 experts, 6 chosen,
 // 64 tokens 5.4, 6.4, 9; 512 tokens -, 12.3, 9.5; 8 experts, 2 chosen, 512 tokens -, 6.7, 9.0; 1024 tokens -, 10.6, 8.8.
-bool one_block(const RouteArgs& a, uint32_t held) { return a.start && a.n * held <= kOneBlock; }
+bool one_block(const RouteArgs& a, uint32_t held) { return a.start && a.n <= kOneBlock / held; }
 uint32_t order_room(const RouteArgs& a) { return a.n_experts * ((a.n + 31u) / 32u + 1u) * 4u; }
 bool one_order(const RouteArgs& a) { return a.n <= kOrderTokens && a.n * a.k <= kOrderChoices && order_room(a) <= kOrderRoom; }
 
@@ -221,13 +226,16 @@ int maaso_rows_quantize(maaso_instance* inst, const maaso_rows_quantize_args* p,
   const uint64_t size = element_size(p->type), elements = (uint64_t)p->width * (p->form == MAASO_ROWS_GATED ? 2u : 1u);
   if (!aligned(p->x, size) || !aligned(p->q, 16) || !aligned(p->weight, size)) return MAASO_E_SHAPE;
   if (p->n > 1u && (p->q_stride % 16u || p->x_stride < elements || p->q_stride < p->width)) return MAASO_E_SHAPE;
-  const QuantizeArgs a{p->x, p->weight, p->q, p->scale, p->x_stride, p->q_stride, p->n, p->width, p->eps};
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
   InstanceCall call(inst, s);
   if (call.rc != MAASO_OK) return call.rc;
-  if (p->type == MAASO_BF16) launch_quantize<__bf16>(p->form, a, (uint32_t)inst->n_cu, s);
-  else if (p->type == MAASO_FP16) launch_quantize<_Float16>(p->form, a, (uint32_t)inst->n_cu, s);
-  else launch_quantize<float>(p->form, a, (uint32_t)inst->n_cu, s);
+  for (uint64_t first = 0; first < p->n; first += kPieceRows) {
+    const QuantizeArgs a{static_cast<const char*>(p->x) + first * p->x_stride * size, p->weight, p->q + first * p->q_stride, p->scale + first,
+                         p->x_stride, p->q_stride, (uint32_t)std::min<uint64_t>(p->n - first, kPieceRows), p->width, p->eps};
+    if (p->type == MAASO_BF16) launch_quantize<__bf16>(p->form, a, (uint32_t)inst->n_cu, s);
+    else if (p->type == MAASO_FP16) launch_quantize<_Float16>(p->form, a, (uint32_t)inst->n_cu, s);
+    else launch_quantize<float>(p->form, a, (uint32_t)inst->n_cu, s);
+  }
   return launched();
 }
 
@@ -269,7 +277,7 @@ int maaso_expert_route(maaso_instance* inst, const maaso_expert_route_args* p, v
   const bool order = p->start || p->token || p->place;
   if (order && !(p->start && p->token && p->place) && p->n) return MAASO_E_INVALID_ARG;
   if (p->n && (!p->logits || !p->expert || !p->weight)) return MAASO_E_INVALID_ARG;
-  if ((uint64_t)p->n * p->k > 0x7fffffffull || (p->n > 1u && p->stride < p->n_experts)) return MAASO_E_SHAPE;
+  if (p->n > kMostTokens || (uint64_t)p->n * p->k > 0x7fffffffull || (p->n > 1u && p->stride < p->n_experts)) return MAASO_E_SHAPE;
   if (p->n == 0 && !p->start) return MAASO_OK;
   RouteArgs a{p->logits, p->bias, p->expert, p->weight, p->start, p->token, p->place, p->stride, p->n, p->n_experts, p->k,
               p->sigmoid != 0u, p->renorm != 0u, p->scale, (p->n + kChunk - 1u) / kChunk, nullptr, nullptr};
@@ -294,19 +302,24 @@ int maaso_expert_combine(maaso_instance* inst, const maaso_expert_combine_args* 
   if (p->width == 0 || p->width > 0x3fffffffu || p->k == 0 || p->k > MAASO_EXPERT_MAX_CHOSEN) return MAASO_E_SHAPE;
   if (p->n == 0) return MAASO_OK;
   if (!p->out || !p->place || (!p->y && p->n_rows)) return MAASO_E_INVALID_ARG;
-  const uint64_t size = element_size(p->type), blocks = ((uint64_t)p->n * ((p->width + 7u) / 8u) + 255u) / 256u;
-  if (p->n > 0x7fffffffu || p->n_rows > 0x7fffffffu || blocks > 0x7fffffffull) return MAASO_E_SHAPE;
+  const uint64_t size = element_size(p->type), per = (p->width + 7u) / 8u, piece = kPieceThreads / per;
+  if (p->n > 0x7fffffffu || p->n_rows > 0x7fffffffu) return MAASO_E_SHAPE;
   if (!aligned(p->y, size) || !aligned(p->residual, size) || !aligned(p->out, size)) return MAASO_E_SHAPE;
   auto rows_ok = [&](uint32_t rows, uint64_t stride) { return rows <= 1u || stride >= p->width; };
   if (!rows_ok(p->n_rows, p->y_stride) || !rows_ok(p->n, p->out_stride) || (p->residual && !rows_ok(p->n, p->residual_stride))) return MAASO_E_SHAPE;
   if (p->residual == p->out && p->n > 1u && p->residual_stride != p->out_stride) return MAASO_E_INVALID_ARG;
-  const CombineArgs a{p->y, p->residual, p->out, p->place, p->weight, p->y_stride, p->residual_stride, p->out_stride, p->n, p->k, p->width, p->n_rows, inst->status};
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
   InstanceCall call(inst, s);
   if (call.rc != MAASO_OK) return call.rc;
-  if (p->type == MAASO_BF16) hipLaunchKernelGGL(combine_kernel<__bf16>, dim3((uint32_t)blocks), dim3(256), 0, s, a);
-  else if (p->type == MAASO_FP16) hipLaunchKernelGGL(combine_kernel<_Float16>, dim3((uint32_t)blocks), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL(combine_kernel<float>, dim3((uint32_t)blocks), dim3(256), 0, s, a);
+  for (uint64_t first = 0; first < p->n; first += piece) {
+    const uint32_t n = (uint32_t)std::min<uint64_t>(p->n - first, piece), blocks = (uint32_t)((n * per + 255u) / 256u);
+    const CombineArgs a{p->y, p->residual ? static_cast<const char*>(p->residual) + first * p->residual_stride * size : nullptr,
+                        static_cast<char*>(p->out) + first * p->out_stride * size, p->place + first * p->k, p->weight ? p->weight + first * p->k : nullptr,
+                        p->y_stride, p->residual_stride, p->out_stride, n, p->k, p->width, p->n_rows, inst->status};
+    if (p->type == MAASO_BF16) hipLaunchKernelGGL(combine_kernel<__bf16>, dim3(blocks), dim3(256), 0, s, a);
+    else if (p->type == MAASO_FP16) hipLaunchKernelGGL(combine_kernel<_Float16>, dim3(blocks), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL(combine_kernel<float>, dim3(blocks), dim3(256), 0, s, a);
+  }
   return launched();
 }
 

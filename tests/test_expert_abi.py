@@ -89,7 +89,7 @@ def test_quantizing_refused(lib, inst, over, status):  # noqa: F811
 PRODUCTS = [
     (dict(type=2), INVALID), (dict(type=3), INVALID), (dict(out_type=3), INVALID), (dict(out_type=4), INVALID), (dict(a=None), INVALID), (dict(w=None), INVALID),
     (dict(out=None), INVALID), (dict(n_in=0), SHAPE), (dict(n_in=131072, a_stride=1 << 18, w_stride=1 << 18), SHAPE), (dict(n_out=0), SHAPE),
-    (dict(n_out=1 << 30), SHAPE), (dict(n_a=1 << 31), SHAPE), (dict(a_stride=104), SHAPE), (dict(a_stride=96), SHAPE), (dict(w_stride=104), SHAPE),
+    (dict(n_out=1 << 30), SHAPE), (dict(n_out=1 << 27, out_stride=1 << 27), SHAPE), (dict(n_a=1 << 31), SHAPE), (dict(a_stride=104), SHAPE), (dict(a_stride=96), SHAPE), (dict(w_stride=104), SHAPE),
     (dict(w_stride=96), SHAPE), (dict(out_stride=49), SHAPE), (dict(a=PTR + 8), SHAPE), (dict(w=PTR + 8), SHAPE), (dict(out=PTR + 1), SHAPE),
     (dict(out=PTR + 2, out_type=2), SHAPE)]
 
@@ -117,7 +117,7 @@ def test_experts_refused(lib, inst, over, status):  # noqa: F811
     (dict(type=3), INVALID), (dict(sigmoid=0), INVALID), (dict(scale=float("nan")), INVALID), (dict(logits=None), INVALID), (dict(expert=None), INVALID),
     (dict(weight=None), INVALID), (dict(start=None), INVALID), (dict(token=None), INVALID), (dict(place=None), INVALID), (dict(start=None, token=None), INVALID),
     (dict(n_experts=0), SHAPE), (dict(n_experts=1025, stride=2000), SHAPE), (dict(k=0), SHAPE), (dict(k=9), SHAPE), (dict(k=33, n_experts=64, stride=64), SHAPE),
-    (dict(stride=7), SHAPE), (dict(n=1 << 30), SHAPE), (dict(n=0, start=None, token=None, place=None), 0)])
+    (dict(stride=7), SHAPE), (dict(n=1 << 30), SHAPE), (dict(n=1 << 26, k=1), SHAPE), (dict(n=1 << 28, k=1, start=None, token=None, place=None), SHAPE), (dict(n=0, start=None, token=None, place=None), 0)])
 def test_routing_refused(lib, inst, over, status):  # noqa: F811
     assert lib.maaso_expert_route(inst, route(**over), None) == status
 

@@ -168,3 +168,15 @@ def test_places_outside(inst):  # noqa: F811
     assert out[:, 0].tolist() == [1.0, 1.0, 0.0]
     I.maaso_expert_combine(inst, y=torch.empty(0, 16, device="cuda"), place=torch.full((3, 2), -1, dtype=torch.int32, device="cuda"), out=out)
     assert (out == 0).all()
+
+
+def test_joining_by_several_launches(inst):  # noqa: F811
+    """Out of more than 2^33 elements, which takes two launches: the tokens on either side of the seam, and the last."""
+    width, n = 1 << 20, (1 << 13) + 3
+    y = torch.arange(4 * width, device="cuda").remainder(251).view(4, width).to(torch.bfloat16)  # whole numbers: every step is exact
+    place = torch.arange(n, device="cuda", dtype=torch.int32).remainder(4).unsqueeze(1)
+    weight = torch.arange(n, device="cuda").remainder(3).sub(1).float().unsqueeze(1)
+    out = torch.empty(n, width, dtype=torch.bfloat16, device="cuda")
+    I.maaso_expert_combine(inst, y=y, place=place, out=out, weight=weight)
+    for t in (0, 1, 4095, 8190, 8191, 8192, 8193, n - 1):
+        assert torch.equal(out[t], y[t % 4] * (t % 3 - 1)), t

@@ -149,3 +149,13 @@ def test_bytes_are_those_of_binary32(inst):
         most = x.float().abs().amax(1)
         assert torch.equal(scale, most / torch.full_like(most, 127.0))
         assert torch.equal(q.float(), torch.round(x.float() * (torch.ones_like(most) / most * 127.0)[:, None]))
+
+
+def test_rows_of_several_launches(inst):
+    """More rows than one launch takes (2^22): those on either side of the seam, and the last."""
+    n = (1 << 22) + 1030
+    x = torch.arange(n, device="cuda", dtype=torch.float32).remainder(1009).sub(504).unsqueeze(1)
+    q, scale = torch.full((n, 16), 99, dtype=torch.int8, device="cuda")[:, :1], torch.full((n,), -5.0, device="cuda")
+    I.maaso_rows_quantize(inst, x=x, q=q, scale=scale)
+    assert (q[:, 0] == 127 * x[:, 0].sign()).all()
+    assert ((scale.double() - x[:, 0].double().abs() / 127).abs() <= 2 * HALF * scale.double()).all()
