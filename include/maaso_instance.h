@@ -291,7 +291,8 @@ int maaso_scaled_product(maaso_instance* inst, const maaso_product* p, void* hip
  *   softmax:  p[e] = exp(x[e]) / sum exp(x),     the score that experts are chosen by is x[e]
  *   sigmoid:  p[e] = 1 / (1 + exp(-x[e])),       the score is x[e], or with a bias p[e] + bias[e] in 64 bits
  * The k largest scores are chosen, the lowest expert of equals first: expert[t][j], and weight[t][j] =
- * scale * p[expert[t][j]], divided by the sum of the chosen p where `renorm` is not 0 (0 where that sum is 0).  An expert
+ * scale * p[expert[t][j]], divided by the sum of the chosen p where `renorm` is not 0 (0 where that sum is 0; in it p of a
+ * logit below -690, which 64 bits hardly hold, is 0).  An expert
  * whose logit or score is NaN or -infinity is not chosen and has p = 0 (a logit of +infinity is the largest finite one); where fewer than k are left,
  * the rest of the row has expert = -1, weight = 0.
  * token holds the tokens of expert 0 in ascending order, then those of expert 1, ...: expert e's are

@@ -25,6 +25,11 @@ __device__ inline float sigmoid(float x) {
   const Halves h = halves(x);
   return x < 0.0f ? h.e * h.r : h.r;
 }
+// sigmoid(x) / exp(s) for s <= 0, x <= s or s = 0: what shares of a sum can be taken of where sigmoid(x) itself is no number any more.
+__device__ inline float sigmoid_over(float x, float s) {
+  const float r = halves(x).r;
+  return x < 0.0f ? exp_below(x - s) * r : r;
+}
 __device__ inline float silu(float x) { return x * sigmoid(x); }
 
 }  // namespace maaso

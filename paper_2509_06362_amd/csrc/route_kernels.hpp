@@ -68,6 +68,7 @@ __device__ inline uint32_t key_of(float s) {
 __device__ inline float score_of(uint32_t key) { return __builtin_bit_cast(float, key ^ ((uint32_t)((int32_t)~key >> 31) | 0x80000000u)); }
 
 constexpr float kNever = -__builtin_huge_valf();  // the score of what is not chosen, or has been
+constexpr float kNoShare = -690.0f;               // a sigmoid of what is below it, 2^-995, counts as 0
 
 __device__ inline double score64(float x, float bias) { return 1.0 / (1.0 + exp(-(double)x)) + (double)bias; }
 
@@ -248,12 +249,19 @@ __device__ inline void choose(const RouteArgs& a, uint32_t t, uint32_t* marks, u
   } else {
     c.rounds(a.k, nullptr, s);
   }
-  float p[kSlots], chosen = 0.0f;
+  float p[kSlots], l[kSlots], chosen = 0.0f, most = kNever, over = 0.0f;
 #pragma unroll
   for (int h = 0; h < kSlots; ++h) {
     const bool is = c.which[h] >= 0 && c.rank[h] < a.k;
-    const float l = c.logit(is ? c.which[h] : 0);
-    p[h] = is ? a.sigmoid ? sigmoid(l) : exp_below(l - top) : 0.0f;
+    l[h] = is ? c.logit(c.which[h]) : kNever;
+    most = fmaxf(most, l[h]);
+  }
+  // Sigmoids that are divided by their sum are divided by exp(`over`) first, the chosen's largest logit where that is below 0: 64 bits would hold them,
+  // 32 do not.  (Where 64 would not either, they are 0, so that a row of the type's lowest value has no weights.)
+  if (a.sigmoid && a.renorm) over = fminf(join<Lanes>(most, [](float x, float y) { return fmaxf(x, y); }), 0.0f);
+#pragma unroll
+  for (int h = 0; h < kSlots; ++h) {
+    p[h] = l[h] < (a.sigmoid ? kNoShare : -3.40282347e38f) ? 0.0f : a.sigmoid ? sigmoid_over(l[h], over) : exp_below(l[h] - top);
     chosen += p[h];
   }
   chosen = in_all<Lanes>(chosen);

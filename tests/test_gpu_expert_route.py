@@ -122,6 +122,24 @@ def test_scores_next_to_each_other(inst):  # noqa: F811
         check(inst, logits.cuda(), 8, bias=(torch.randint(-2, 3, (96,), generator=g) * 2.0 ** -24).cuda(), sigmoid=True)
 
 
+@pytest.mark.parametrize("n", [6, 300])
+def test_shares_of_logits_far_below_zero(inst, n):  # noqa: F811
+    """Their sigmoids are no numbers of 32 bits any more, the quotients by their sum are; the lowest value is none."""
+    g = torch.Generator().manual_seed(4)
+    logits = torch.randn(n, 90, generator=g) * 4
+    for t, by in enumerate((-60.0, -90.0, -100.0, -200.0, -600.0)):
+        logits[t] += by
+    logits[5, 1:] -= 75.0  # one expert that is liked and others whose shares are still numbers
+    logits[5, 0] = -12.0
+    for k in (1, 3, 8):
+        check(inst, logits.cuda(), k, sigmoid=True)
+        check(inst, logits.cuda(), k, sigmoid=True, bias=(torch.randn(90, generator=g) * 0.1).cuda(), scale=2.5)
+        check(inst, logits.cuda(), k, sigmoid=True, renorm=False)
+    low = torch.full((n, 90), torch.finfo(torch.float32).min)
+    low[0, 7] = -300.0
+    check(inst, low.cuda(), 4, sigmoid=True)
+
+
 def test_no_tokens(inst):  # noqa: F811
     start = torch.full((9,), -9, dtype=torch.int32, device="cuda")
     none = torch.empty(0, dtype=torch.int32, device="cuda")
