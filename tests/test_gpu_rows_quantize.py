@@ -159,3 +159,57 @@ def test_rows_of_several_launches(inst):
     I.maaso_rows_quantize(inst, x=x, q=q, scale=scale)
     assert (q[:, 0] == 127 * x[:, 0].sign()).all()
     assert ((scale.double() - x[:, 0].double().abs() / 127).abs() <= 2 * HALF * scale.double()).all()
+
+
+@pytest.mark.parametrize("name", list(TYPES))
+@pytest.mark.parametrize("n, width", [(5, 200), (1030, 100), (3, 40001), (300, 9001)])
+def test_norms_of_very_small_rows(inst, n, width, name):
+    """Squares below every number of 32 bits, with eps 0 and with one next to it: rows of finite numbers have finite scales."""
+    g = torch.Generator().manual_seed(9)
+    x = torch.randn(n, width, generator=g).clamp(-4, 4).double()
+    least = torch.finfo(TYPES[name]).smallest_normal / 4
+    for t, by in enumerate((2.0 ** -80, 2.0 ** -64, 1e-25 if name != "fp16" else 2.0 ** -14, 0.0, least)):
+        x[t % n] *= max(by, least) if by else 0.0
+    x = x.to(TYPES[name]).cuda()
+    weight = (1 + 0.3 * torch.randn(width, generator=g)).to(TYPES[name]).cuda()
+    for eps in (0.0, 1e-36, 2.0 ** -149, 1e-6):
+        for w in (weight, None):
+            q, scale = run(inst, x, width, "norm", w, eps)
+            some = (x != 0).any(1)
+            assert (q[~some] == 0).all() and (scale[~some] == 0).all()
+            check(x[some], q[some], scale[some], "norm", w, eps)
+
+
+@pytest.mark.parametrize("n, width", [(6, 200), (1030, 100), (300, 9001)])
+def test_norms_with_weights_far_from_one(inst, n, width):
+    """Products with the weight that are beyond 32 bits, or below, where the normed numbers are neither."""
+    g = torch.Generator().manual_seed(10)
+    rows, signs = torch.randn(n, width, generator=g).clamp(-4, 4).double(), torch.randn(width, generator=g).double()
+    for x_by, w_by, eps in ((1e16, 1e25, 1e-6), (1e16, 1e25, 0.0), (1e-10, 1e-34, 0.0), (1e-12, 1e-34, 1e-24), (1e-30, 1e20, 0.0), (1e-28, 1e-14, 1e-6), (1e-42, 1e36, 0.0)):
+        x, weight = (rows * x_by).float(), (signs * w_by).float().cuda()
+        x[0] = 0
+        x = x.cuda()
+        q, scale = run(inst, x, width, "norm", weight, eps)
+        assert (q[0] == 0).all() and scale[0] == 0
+        check(x[1:], q[1:], scale[1:], "norm", weight, eps)
+    x = rows.float().cuda()
+    weight = torch.ones(width, device="cuda")
+    weight[3] = math.inf  # what is infinite stays no number
+    q, scale = run(inst, x, width, "norm", weight)
+    assert (q == 0).all() and scale.isnan().all()
+    weight = torch.zeros(width, device="cuda")
+    q, scale = run(inst, x, width, "norm", weight)
+    assert (q == 0).all() and (scale == 0).all()
+
+
+@pytest.mark.parametrize("n, width", [(300, 4100), (300, 8200), (300, 9001), (300, 16500), (3, 32776), (3, 40001), (2, 70003)])
+@pytest.mark.parametrize("form", ["plain", "norm", "gated"])
+@pytest.mark.parametrize("name", list(TYPES))
+def test_rows_longer_than_the_registers(inst, name, form, n, width):
+    """What is read and worked out a second time, by 256, 512 and 1024 threads to a row."""
+    g = torch.Generator().manual_seed(width)
+    x = (torch.randn(n, width * (2 if form == "gated" else 1), generator=g) * 3).to(TYPES[name]).cuda()
+    weight = (1 + 0.3 * torch.randn(width, generator=g)).to(TYPES[name]).cuda() if form == "norm" else None
+    for step in (8, 3):
+        x = padded(x, step, math.nan)
+        check(x, *run(inst, x, width, form, weight), form, weight)
