@@ -15,8 +15,8 @@ using namespace maaso;
 
 namespace {
 
-// A launch holds fewer than 2^32 threads.  Rows beyond kPieceRows of one launch, and threads beyond kPieceThreads, go to another; tokens that are put in
-// order cannot (16 threads to a token at least), and channels have a launch's x to themselves (16 threads to a channel).
+// A launch holds fewer than 2^32 threads.  Rows beyond kPieceRows of one launch, and threads beyond kPieceThreads, go to another, and so do tokens that are
+// chosen for alone; tokens that are put in order cannot (16 threads to a token), and channels have a launch's x to themselves (16 threads to a channel).
 constexpr uint32_t kPieceRows = 1u << 22, kMostTokens = (1u << 26) - 1u, kMostOut = (1u << 27) - 1u;
 constexpr uint64_t kPieceThreads = 1u << 30;
 
@@ -185,8 +185,18 @@ void launch_route(const RouteArgs& a, hipStream_t s) {
     hipLaunchKernelGGL((route_kernel<T, Lanes, Quads, Biased>), dim3(1), dim3(1024), order_room(a), s, a);
     return;
   }
-  if (a.before) hipLaunchKernelGGL((route_choose_kernel<T, Lanes, Quads, Biased>), dim3(a.chunks), dim3(1024), 0, s, a);
-  else hipLaunchKernelGGL((route_choose_kernel<T, Lanes, Quads, Biased>), dim3((a.n + 256u / Lanes - 1u) / (256u / Lanes)), dim3(256), 0, s, a);
+  if (a.before) {
+    hipLaunchKernelGGL((route_choose_kernel<T, Lanes, Quads, Biased>), dim3(a.chunks), dim3(1024), 0, s, a);
+  } else {
+    for (uint32_t first = 0; first < a.n; first += kPieceRows) {
+      RouteArgs piece = a;
+      piece.logits = static_cast<const T*>(a.logits) + first * a.stride;
+      piece.expert = a.expert + (uint64_t)first * a.k;
+      piece.weight = a.weight + (uint64_t)first * a.k;
+      piece.n = std::min(a.n - first, kPieceRows);
+      hipLaunchKernelGGL((route_choose_kernel<T, Lanes, Quads, Biased>), dim3((piece.n + 256u / Lanes - 1u) / (256u / Lanes)), dim3(256), 0, s, piece);
+    }
+  }
   if (!a.start) return;
   if (!a.before) {
     hipLaunchKernelGGL(route_order_kernel, dim3(1), dim3(1024), order_room(a), s, a);

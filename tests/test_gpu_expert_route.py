@@ -147,6 +147,23 @@ def test_no_tokens(inst):  # noqa: F811
     assert (start == 0).all()
 
 
+@pytest.mark.parametrize("n, e, k", [((1 << 22) + 1030, 9, 2), ((1 << 23) + 5, 70, 1), ((1 << 26) - 1, 513, 1)])
+def test_choosing_by_several_launches(inst, n, e, k):  # noqa: F811
+    """More tokens than one launch takes (2^22), up to the most with 64 lanes to each: token t likes expert t % e, then the next."""
+    t = torch.arange(n, device="cuda")
+    logits = torch.zeros(n, e, dtype=torch.bfloat16, device="cuda")
+    for j in range(k):
+        logits.view(-1)[t * e + (t + j) % e] = 3.0 - j
+    expert, weight = torch.full((n, k), -9, dtype=torch.int32, device="cuda"), torch.full((n, k), -9.0, device="cuda")
+    I.maaso_expert_route(inst, logits=logits, expert=expert, weight=weight, renorm=True)
+    share = torch.tensor([3.0 - j for j in range(k)], dtype=torch.float64).softmax(0)
+    for j in range(k):
+        assert torch.equal(expert[:, j], ((t + j) % e).int())
+        assert (weight[:, j].double() - share[j].item()).abs().max().item() <= 32 * HALF
+    del logits, t, expert, weight
+    torch.cuda.empty_cache()
+
+
 @pytest.mark.parametrize("name", list(TYPES))
 @pytest.mark.parametrize("n, k, width", [(1, 1, 1), (3, 2, 7), (16, 2, 2048), (33, 8, 100), (5, 32, 130), (200, 3, 513)])
 def test_joining(inst, n, k, width, name):  # noqa: F811
