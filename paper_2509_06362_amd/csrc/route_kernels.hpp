@@ -287,8 +287,10 @@ __device__ inline void put_chosen(const RouteArgs& a, uint32_t first, uint32_t t
       const uint32_t* b = bits + (uint32_t)e * words;
       uint32_t rank = before[e] + (uint32_t)__builtin_popcount(b[t / 32u] & ((1u << (t & 31u)) - 1u));
       for (uint32_t w = 0; w < t / 32u; ++w) rank += (uint32_t)__builtin_popcount(b[w]);
-      to = (int32_t)rank;
-      a.token[rank] = (int32_t)(first + t);
+      if (rank < a.n * a.k) {  // (counts that another replay wrote into the same workspace meanwhile are not followed out of token)
+        to = (int32_t)rank;
+        a.token[rank] = (int32_t)(first + t);
+      }
     }
     a.place[(uint64_t)first * a.k + i] = to;
   }

@@ -142,6 +142,37 @@ def test_other_streams(inst):  # noqa: F811
         layer.check()
 
 
+def test_replays_that_the_caller_has_not_ordered(inst):  # noqa: F811
+    """Two graphs that share the workspace and run at once may give wrong orders, but write nothing outside their tensors; calls behind them are right."""
+    graphs, held = [], []
+    for n, e, k in ((3000, 12, 2), (40000, 60, 4), (1500, 200, 3)):
+        logits = torch.randn(n, e, generator=torch.Generator().manual_seed(n)).cuda()
+        around = torch.full((4 * n * k,), -77, dtype=torch.int32, device="cuda")
+        o = dict(expert=torch.empty(n, k, dtype=torch.int32, device="cuda"), weight=torch.empty(n, k, device="cuda"), start=torch.empty(e + 1, dtype=torch.int32, device="cuda"),
+                 token=around[n * k:2 * n * k], place=torch.empty(n, k, dtype=torch.int32, device="cuda"))
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            I.maaso_expert_route(inst, logits=logits, **o)
+        graphs.append((graph, torch.cuda.Stream()))
+        held.append((logits, around, o, n, k))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for graph, stream in graphs:
+            with torch.cuda.stream(stream):
+                graph.replay()
+    torch.cuda.synchronize()
+    for logits, around, o, n, k in held:
+        assert (around[:n * k] == -77).all() and (around[2 * n * k:] == -77).all()
+        assert ((o["place"] >= -1) & (o["place"] < n * k)).all()
+        I.maaso_expert_route(inst, logits=logits, **o)
+        best = torch.sort(logits.cpu(), dim=1, descending=True, stable=True)[1][:, :k]
+        order = torch.sort(best.flatten(), stable=True)[1]
+        assert torch.equal(o["expert"].cpu().long(), best) and torch.equal(o["token"].cpu().long(), order // k)
+        assert torch.equal(o["place"].cpu().long().flatten()[order], torch.arange(n * k))
+    assert I.maaso_instance_status(inst) == 0
+
+
 def test_repeats_are_the_same_bits(inst):  # noqa: F811
     layer = Layer(700, 256, 96, 16, 4, False, seed=5)
     first = layer.run(inst).clone()
