@@ -245,7 +245,9 @@ int maaso_logits_adjust(maaso_instance* inst, const maaso_logits_args* a, void* 
  *   MAASO_ROWS_NORM:   x / sqrt(mean(x^2) + eps) * weight           (weight NULL: 1)
  *   MAASO_ROWS_GATED:  silu(x[i]) * x[width + i], silu(x) = x / (1 + exp(-x)); x has 2 * width elements
  * and with m = max |y|:   scale[t] = m / 127,   q[t][i] = y * (1 / m * 127), each step in binary32, then
- * rounded to the nearest whole number, ties to even.
+ * rounded to the nearest whole number, ties to even.  y itself is worked out in binary32: with a norm the sum has an order of its own and
+ * the weight may come before the division, the gate has its own exponential, so that a number next to a rounding's border may
+ * go to the other side than a program's that follows the formula step by step.
  * A row of zeros has q = 0, scale = 0.  A row that holds a NaN or an infinity in y, or whose sum of squares passes
  * binary32, has q = 0, scale = NaN: products of it are NaN and nothing else is.  All DEVICE.
  * Errors: INVALID_ARG, SHAPE, BUSY, HIP. */
@@ -275,7 +277,8 @@ typedef struct {
   uint32_t n_in;     /* 1 .. MAASO_PRODUCT_MAX_IN                                                   */
   uint32_t n_out, gated; /* n_out < 2^27; rows by channels in tiles of 64 by 64 fewer than 2^24     */
   uint64_t a_stride, w_stride; /* elements between rows; multiples of 16 bytes, as the pointers are */
-  uint64_t out_stride;         /* any                                                               */
+  uint64_t out_stride;         /* any; rows that do not all begin at 16 bytes (an odd width) are written element by element,
+                                  which takes up to twice as long                                   */
   const void* a;
   const void* w;
   const float* a_scale; /* [n_a], INT8 only, NULL for 1                                             */

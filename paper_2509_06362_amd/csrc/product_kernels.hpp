@@ -335,9 +335,11 @@ template <uint32_t Loads, uint32_t Most> __device__ inline void meet_behind(uint
   }
 }
 
-// More rows.  In the largest tiles matrix units are busy 64 % of the time (8 bits, 8192 x 4096 x 8192: 254 us, 2160 T/s, where the library's plain product
-// of 8192 cubed reaches 2060; 16 bits, 8192 x 2048 x 8192: 243 us, 1130 T/s, the library 1320).  Without the loads a step is 15 % shorter, without the reads of
-// shared memory 2 %, without both and the barrier 24 %; begin and end of a tile are 13 us of 61 at 4096 bytes.  Slower were four waves of 128 by 128 (3 %), steps of
+// More rows.  In the largest tiles matrix units are busy 53 % of a launch (8 bits, 8192 x 4096 x 8192, gated: 247 us, 2220 T/s, where the library's plain
+// product of 8192 cubed reaches 2060) or 64 % (16 bits, 8192 cubed: 829 us, 1330 T/s, the library 671 and 84 %); 16 bits, 8192 x 2048 x 8192
+// 243 us, 1130 T/s.  The 829 us are 705 without the loads, 798 without the reads of shared memory, 626 without both, 646 on another card without the barrier as well:
+// loads are what a step waits for.  Begin and end of a tile are 13 us of 61 at 4096 bytes.  The largest tiles have 14 registers too few: the rows' ends, which whole
+// steps do without, find their addresses in scratch and are brought one by one (8192 x 4104 x 8192 264 us, 4096 236).  Slower were four waves of 128 by 128 (3 %), steps of
 // 64 bytes in three to five stages (7 to 30 %, half lines), blocks that go from tile to tile (12 %, registers), lines brought to the cache ahead (8 %).
 // A block is kRows rows by kCols channels, a wave MI by NI times 16 of each.  Steps of 128 bytes of both come to shared
 // memory asynchronously, Stages of them under way or in use.  A step is two halves: while one is multiplied the operands of the next
